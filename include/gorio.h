@@ -367,6 +367,160 @@ gorio_status gorio_set_query_order(gorio_index *ix, const float *centroids, uint
  */
 void gorio_free_index(gorio_index *ix);
 
+/* ---------------------------------------------------------------------------
+ * Keys and values of passages, in pages.
+ *
+ * What a search finds is read next: a program that answers from the nodes
+ * found keeps the attention keys and values of each node's text in pages in
+ * HBM, beside the index, and runs its model's new tokens over the pages of the
+ * nodes that the search returned.  Four calls do that, once a step (attach,
+ * plan) and once a layer (store, attend):
+ *
+ *   gorio_kv_attach  a search's ids -> each request's table of pages
+ *   gorio_kv_plan    request lengths -> starts, positions and slots of the new
+ *                    tokens, and the tables grown by pages of a free list
+ *   gorio_kv_store   the new tokens' keys and values -> their slots
+ *   gorio_kv_attend  attention of the new tokens over the pages
+ *
+ * A request's tokens have virtual positions 0, 1, ...; position j is place
+ * j % page_tokens of the page that entry j / page_tokens of the request's row
+ * of the table names.  An entry outside [0, num_pages) names no page.
+ * A token's slot is page * page_tokens + place.
+ *
+ * Conventions, besides those above: every array is in device memory (of one
+ * GPU, which the call switches to); the calls allocate nothing, wait for
+ * nothing and only enqueue kernels on `stream`, so they can be captured into
+ * a HIP graph.  A size of zero (no request, no token) is a no-op.  Lengths are
+ * read on the GPU: a value there that makes no sense (negative, past a
+ * capacity) is clamped as each call says and never reaches memory outside the
+ * arrays.  Errors: GORIO_EINVAL (NULL or host pointers, sizes out of range,
+ * misaligned pointers or strides), GORIO_EUNSUPPORTED (a combination of types
+ * that there is no kernel for), GORIO_EDEVICE.
+ * ------------------------------------------------------------------------- */
+
+typedef enum { GORIO_KV_BF16 = 0, GORIO_KV_F16 = 1, GORIO_KV_E4M3 = 2 } gorio_kv_dtype;
+
+/* The pages of one layer.  Element d of head h's key at place i of page p is
+ * keys[p * page_stride + h * head_stride + i * token_stride + d]; values alike. */
+typedef struct {
+    uint32_t dtype;         /* gorio_kv_dtype of keys and values */
+    uint32_t heads;         /* key and value heads, 1..1024 */
+    uint32_t D;             /* elements of a head: a multiple of 8, 8..256 */
+    uint32_t page_tokens;   /* 1..65536 */
+    uint64_t num_pages;     /* 1..2^31 - 1 */
+    void *keys, *values;    /* 16-byte aligned */
+    uint64_t page_stride, head_stride, token_stride;  /* elements, multiples of 8; all three
+                               0 = packed pages, [page][head][token][D] */
+    const float *key_scale, *value_scale;  /* GORIO_KV_E4M3: `heads` factors each; an element
+                               stands for its 8-bit value times its head's factor.  NULL = 1 */
+} gorio_kv_cache;
+
+/* One call's new tokens, and what they see. */
+typedef struct {
+    uint32_t dtype;         /* gorio_kv_dtype of q and out: GORIO_KV_BF16 or GORIO_KV_F16, and that
+                               of the pages unless they are GORIO_KV_E4M3 */
+    uint32_t heads;         /* query heads, a multiple of the cache's; head h reads head
+                               h / (heads / cache heads) */
+    uint32_t requests, width;  /* rows and columns of tables */
+    uint64_t tokens;        /* rows of q and out */
+    const void *q;          /* token t's head h at q + t * q_stride + h * D, 16-byte aligned */
+    void *out;              /* laid out alike, with out_stride */
+    uint64_t q_stride, out_stride;  /* elements, multiples of 8; 0 = heads * D */
+    float *lse;             /* tokens x heads out, or NULL: log of the sum of exp(score) */
+    const int32_t *starts;  /* requests + 1: request b's new tokens are rows starts[b]..starts[b+1] */
+    const int32_t *lens;    /* requests: all of its tokens, the new ones last */
+    const int32_t *tables;  /* requests x width pages */
+    const int32_t *fills;   /* requests x width: tokens that a page holds, from its first place
+                               (NULL: page_tokens) */
+    const int32_t *prefix;  /* requests: its first positions, which every new token sees (NULL: 0) */
+    const float *slopes;    /* heads: see below (NULL: 0) */
+    float scale, cap;       /* cap 0 = none */
+    uint32_t window;        /* 0 = none */
+    uint32_t max_new;       /* the most new tokens of a request, if the caller knows it (0: not);
+                               chooses a kernel, and changes no result beyond rounding */
+} gorio_kv_attention;
+
+/*
+ * A search's answers -> tables of pages.  Passage (node) v has tokens[v]
+ * tokens in ceil(tokens[v] / page_tokens) pages from first_page[v] on.  Row b
+ * of the table gets the pages of nodes[b][0], nodes[b][1], ... one passage
+ * after the other, each from a page's first place, as long as whole passages
+ * fit into `limit` entries: the first that does not fit ends the row.  Ids at
+ * or past n (a search's padding) are passed over.
+ *   nodes:    requests x k (1 <= k <= 1024), e.g. from gorio_search.
+ *   tables, fills: requests x width out: pages and the tokens that each holds;
+ *             entries past the passages get -1 and page_tokens.
+ *   lens:     requests out: page_tokens times the entries taken, which is the
+ *             next position (a passage's last page is never written to by a
+ *             request), and the prefix for gorio_kv_attend.
+ *   attached: requests out, or NULL: passages in the row.
+ */
+gorio_status gorio_kv_attach(const uint32_t *nodes, uint64_t requests, uint32_t k,
+                             const int32_t *first_page, const int32_t *tokens, uint64_t n,
+                             uint32_t page_tokens, uint32_t width, uint32_t limit,
+                             int32_t *tables, int32_t *fills, int32_t *lens, int32_t *attached,
+                             void *stream);
+
+/*
+ * A step's plan from request lengths: request b has before[b] tokens and
+ * takes added[b] new ones (negative values count as 0).
+ *   free_pages: n_free pages that no request holds; request by request, in
+ *             order, each takes as many as its entries need from the front.
+ *   tables:   requests x width, in and out: the new entries are written.  An
+ *             entry for which no page is left gets -1; entries at or past
+ *             width are not kept, and take no page.
+ *   lens:     requests out: before + added.
+ *   starts:   requests + 1 out: exclusive sums of added.
+ *   positions, slots: `tokens` out: each new token's position and slot (-1
+ *             where it has no page; -1 both past the last new token; new
+ *             tokens past `tokens` are left out).
+ *   taken:    1 out: pages that the entries needed, which may pass n_free.
+ * positions, slots and taken may be NULL.  lens and before are different arrays.
+ */
+gorio_status gorio_kv_plan(const int32_t *before, const int32_t *added, uint64_t requests,
+                           uint32_t page_tokens, const int32_t *free_pages, uint64_t n_free,
+                           int32_t *tables, uint32_t width, uint64_t tokens, int32_t *lens,
+                           int32_t *starts, int32_t *positions, int64_t *slots, int32_t *taken,
+                           void *stream);
+
+/*
+ * Keys and values of new tokens -> their slots.  Token t's head h is at
+ * keys + t * key_stride + h * D (elements, multiples of 8; 0 = heads * D; 16-byte
+ * aligned), values alike.  A slot outside the pages stores nothing; slots of
+ * one call are distinct.  Into GORIO_KV_E4M3 pages an element is divided by its
+ * head's factor, clamped to +-448 and rounded to the nearest (ties to even).
+ *   dtype: of keys and values: the pages' type, or either 16-bit type for
+ *          GORIO_KV_E4M3 pages.
+ */
+gorio_status gorio_kv_store(const gorio_kv_cache *cache, gorio_kv_dtype dtype, const void *keys,
+                            const void *values, uint64_t tokens, uint64_t key_stride,
+                            uint64_t value_stride, const int64_t *slots, void *stream);
+
+/*
+ * Attention of new tokens over pages.  New token i of request b stands at
+ * position p = lens[b] - (starts[b+1] - starts[b]) + i; its keys and values
+ * are read from the pages like all others (store them first).  Key j is
+ * visible to it if its table entry names a page, j % page_tokens is below the
+ * page's fill, j < lens[b], and (j <= p and p - j < window, or j < prefix[b]).
+ *   s_j = scale * (q . k_j); with a cap, s_j = cap * tanh(s_j / cap); then
+ *   s_j -= slopes[h] * |p - j|
+ *   out = sum_j exp(s_j) v_j / sum_j exp(s_j) over the visible keys
+ * Sums and the softmax are held in 32 bits, its weights rounded to q's type
+ * for the product with the values.  A row that sees no key (or whose scores
+ * are all -inf) gives zeros and an lse of -inf.  Keys and values that a row
+ * does not see do not reach it, whatever they hold.  Rows of q past starts[requests] are left
+ * as they are in out.  starts is clamped to [0, tokens] and has to ascend.
+ *   workspace: gorio_kv_workspace bytes of device memory, 16-byte aligned, for
+ *              this call alone until it has run (NULL if 0).  Rows of few new
+ *              tokens over long texts are computed in parts, which it holds.
+ */
+gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio_kv_attention *a,
+                             void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that gorio_kv_attend needs; from the sizes alone, no pointer is read. */
+gorio_status gorio_kv_workspace(const gorio_kv_cache *cache, const gorio_kv_attention *a,
+                                uint64_t *bytes);
+
 /*
  * Message for the last failing call on this thread ("" if none).  Errors are
  * returned as status codes so that no failure of the transport path (Sec. 4)

@@ -11,6 +11,9 @@ from pathlib import Path
 
 import numpy as np
 
+from . import kv
+from .kv import KVCache, KVPlan, kv_attach, kv_plan
+
 _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libgorio.so"
 
@@ -58,7 +61,8 @@ class IndexInfo(ctypes.Structure):
 # every symbol include/gorio.h declares
 EXPORTS = ("gorio_build_index", "gorio_set_cache", "gorio_set_backing", "gorio_set_query_order",
            "gorio_search", "gorio_search_noalloc", "gorio_index_info_get", "gorio_copy_pages", "gorio_locality_order",
-           "gorio_cluster_order", "gorio_set_scheduler", "gorio_free_index", "gorio_last_error")
+           "gorio_cluster_order", "gorio_set_scheduler", "gorio_kv_attach", "gorio_kv_plan", "gorio_kv_store",
+           "gorio_kv_attend", "gorio_kv_workspace", "gorio_free_index", "gorio_last_error")
 
 _lib = None
 
@@ -99,6 +103,7 @@ def lib() -> ctypes.CDLL:
         L.gorio_free_index.argtypes = [v]
         L.gorio_last_error.restype = ctypes.c_char_p
         L.gorio_last_error.argtypes = []
+        kv.declare(L)
         _lib = L
     return _lib
 
