@@ -1,108 +1,12 @@
 // gorio_kv_attend: attention of new tokens over the pages of their requests.
 #include <algorithm>
 
-#include "kv.hpp"
+#include "kv_attend_few.hpp"
+#include "kv_launch.hpp"
 
 using namespace gorio;
 
 namespace {
-
-struct AttendParams {
-  const uint16_t *q;
-  uint16_t *out;
-  float *lse;
-  const uint8_t *keys, *values;
-  const float *key_scale, *value_scale;
-  const int32_t *starts, *lens, *tables, *fills, *prefix;
-  const float *slopes;
-  uint64_t tokens, q_stride, out_stride;
-  uint64_t page_stride, head_stride, token_stride;  // elements
-  uint32_t num_pages, requests, width, heads, kv_heads, group, D;
-  FastDiv page_tokens;
-  float scale, cap;
-  uint32_t window;
-};
-
-__device__ __forceinline__ float from_bits(uint16_t b, bool f16) {
-  return f16 ? (float)__builtin_bit_cast(_Float16, b) : __uint_as_float((uint32_t)b << 16);
-}
-
-__device__ __forceinline__ uint16_t to_bits(float x, bool f16) {
-  return f16 ? __builtin_bit_cast(uint16_t, (_Float16)x) : __builtin_bit_cast(uint16_t, (__bf16)x);
-}
-
-__device__ __forceinline__ float element(const uint8_t *pages, uint64_t at, bool e4m3, bool f16) {
-  if (e4m3) return __builtin_amdgcn_cvt_f32_fp8((int)pages[at], 0);
-  return from_bits(reinterpret_cast<const uint16_t *>(pages)[at], f16);
-}
-
-// A wave computes one row of one head, a key a lane and 64 keys at a time.
-__global__ __launch_bounds__(64) void attend_rows(AttendParams p, bool e4m3, bool f16) {
-  const uint32_t h = blockIdx.y, lane = threadIdx.x;
-  const int64_t t = blockIdx.x;
-  uint32_t lo = 0, hi = p.requests;  // the last request that starts at or before t
-  while (lo < hi) {
-    const uint32_t mid = (lo + hi + 1) / 2;
-    if (p.starts[mid] <= t) lo = mid;
-    else hi = mid - 1;
-  }
-  if (lo >= p.requests || t < p.starts[lo]) return;
-  const uint32_t b = lo;
-  const int64_t s0 = p.starts[b], s1 = min((int64_t)p.starts[b + 1], (int64_t)p.tokens);
-  const int64_t len = max(p.lens[b], 0), pos = len - (s1 - s0) + (t - s0);
-  const int64_t prefix = p.prefix ? p.prefix[b] : 0;
-  const int64_t window = p.window ? p.window : (int64_t)1 << 40;
-  const int64_t last = min(min(len, max(pos + 1, prefix)), (int64_t)p.width * p.page_tokens.d);
-  const uint32_t kh = h / p.group;
-  const uint16_t *q = p.q + t * p.q_stride + (uint64_t)h * p.D;
-  const float scale = p.scale * (p.key_scale ? p.key_scale[kh] : 1.f);
-  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t j0 = 0; j0 < last; j0 += 64) {
-    const int64_t j = j0 + lane;
-    bool seen = j < last && ((j <= pos && pos - j < window) || j < prefix);
-    uint64_t at = 0;
-    if (seen) {
-      const uint32_t e = fastdiv((uint32_t)j, p.page_tokens), place = (uint32_t)j - e * p.page_tokens.d;
-      const int32_t page = p.tables[(uint64_t)b * p.width + e];
-      seen = (uint32_t)page < p.num_pages && (!p.fills || (int32_t)place < p.fills[(uint64_t)b * p.width + e]);
-      if (seen) at = (uint64_t)page * p.page_stride + kh * p.head_stride + place * p.token_stride;
-    }
-    float s = -INFINITY;
-    if (seen) {
-      float dot = 0.f;
-      for (uint32_t d = 0; d < p.D; ++d) dot = fmaf(from_bits(q[d], f16), element(p.keys, at + d, e4m3, f16), dot);
-      s = dot * scale;
-      if (p.cap > 0.f) s = p.cap * tanhf(s / p.cap);
-      if (p.slopes) s -= p.slopes[h] * fabsf((float)(pos - j));
-    }
-    float most = s;
-    for (int d = 32; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-    const float to = fmaxf(m, most);
-    const float by = to == -INFINITY ? 0.f : to;
-    const float w = expf(s - by), keep = expf(m - by);
-    float sum = w;
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    l = l * keep + sum;
-    m = to;
-    for (int i = 0; i < 4; ++i) o[i] *= keep;
-    for (int src = 0; src < 64; ++src) {
-      if (!__shfl((int)seen, src)) continue;
-      const float ws = __shfl(w, src);
-      const uint64_t row = __shfl(at, src);
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t d = lane + 64 * i;
-        if (d < p.D) o[i] = fmaf(ws, element(p.values, row + d, e4m3, f16), o[i]);
-      }
-    }
-  }
-  const float norm = l != 0.f ? (p.value_scale ? p.value_scale[kh] : 1.f) / l : 0.f;
-  uint16_t *out = p.out + t * p.out_stride + (uint64_t)h * p.D;
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t d = lane + 64 * i;
-    if (d < p.D) out[d] = to_bits(o[i] * norm, f16);
-  }
-  if (p.lse && lane == 0) p.lse[t * p.heads + h] = l != 0.f ? m + logf(l) : -INFINITY;
-}
 
 // The sizes and types of a call, with the strides filled in.
 gorio_status check(const gorio_kv_cache *cache, const gorio_kv_attention *a, gorio_kv_cache *c, gorio_kv_attention *out) {
@@ -118,6 +22,9 @@ gorio_status check(const gorio_kv_cache *cache, const gorio_kv_attention *a, gor
   if (a->requests > kKvMost || a->tokens > kKvMost) return fail(GORIO_EINVAL, "requests and tokens must be below 2^31");
   if (a->width == 0 || (uint64_t)a->width * c->page_tokens > kKvMost)
     return fail(GORIO_EINVAL, "width=%u: a row holds 1..2^31-1 positions", a->width);
+  if (a->tokens * (a->heads / c->heads) > kKvMost)
+    return fail(GORIO_EINVAL, "tokens=%llu x %u heads a key head: need at most 2^31-1", (unsigned long long)a->tokens,
+                a->heads / c->heads);
   *out = *a;
   if (a->q_stride == 0) out->q_stride = (uint64_t)a->heads * c->D;
   if (a->out_stride == 0) out->out_stride = (uint64_t)a->heads * c->D;
@@ -128,6 +35,32 @@ gorio_status check(const gorio_kv_cache *cache, const gorio_kv_attention *a, gor
   return GORIO_OK;
 }
 
+constexpr uint32_t kLeast = 4, kMost = 2048;
+
+// What a call launches and keeps, from the sizes that the host knows: the
+// lengths are on the GPU, so these are bounds, and blocks without work return.
+// With W the key blocks of all tiles, a part has c >= W heads / most blocks, so
+// there are at most most / heads parts more than tiles; a divided tile has
+// less than 2 blocks / c parts, so divided tiles have at most 2 most / heads.
+struct Division {
+  uint32_t grid, join, slots;
+  uint64_t bytes;
+};
+
+Division divide(const gorio_kv_cache &c, const gorio_kv_attention &a) {
+  Division d{};
+  const uint64_t tiles = a.tokens * (a.heads / c.heads) / kFewRows + std::min<uint64_t>(a.requests, a.tokens);
+  const uint64_t blocks = ((uint64_t)a.width * c.page_tokens + kFewBlock - 1) / kFewBlock;
+  const uint64_t parts = (blocks + kLeast - 1) / kLeast, extra = kMost / c.heads + 1;
+  const uint64_t items = std::min(tiles * parts, tiles + extra);
+  const uint64_t slots = parts > 1 ? std::min(tiles * parts, 2 * extra) : 0;
+  d.grid = (uint32_t)std::min<uint64_t>(items * c.heads, kKvMost);
+  d.slots = (uint32_t)slots;
+  d.join = (uint32_t)std::min<uint64_t>(slots / 2 * c.heads, kKvMost);
+  d.bytes = slots * c.heads * kFewRows * (c.D + 2) * sizeof(float);
+  return d;
+}
+
 }  // namespace
 
 extern "C" gorio_status gorio_kv_workspace(const gorio_kv_cache *cache, const gorio_kv_attention *a, uint64_t *bytes) {
@@ -136,7 +69,7 @@ extern "C" gorio_status gorio_kv_workspace(const gorio_kv_cache *cache, const go
   const gorio_status st = check(cache, a, &c, &at);
   if (st != GORIO_OK) return st;
   if (!bytes) return fail(GORIO_EINVAL, "bytes is NULL");
-  *bytes = 0;
+  *bytes = divide(c, at).bytes;
   return GORIO_OK;
 }
 
@@ -146,8 +79,6 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
   gorio_kv_attention at;
   gorio_status st = check(cache, a, &c, &at);
   if (st != GORIO_OK) return st;
-  (void)workspace;
-  (void)workspace_bytes;
   if (at.tokens == 0 || at.requests == 0) return GORIO_OK;
   KvDevice dev;
   st = dev.use({{"q", at.q, 16, false},
@@ -162,8 +93,14 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
                 {"cache keys", c.keys, 16, false},
                 {"cache values", c.values, 16, false},
                 {"key_scale", c.key_scale, 4, true},
-                {"value_scale", c.value_scale, 4, true}});
+                {"value_scale", c.value_scale, 4, true},
+                {"workspace", workspace, 16, workspace_bytes == 0}});
   if (st != GORIO_OK) return st;
+  const Division d = divide(c, at);
+  if (d.bytes > workspace_bytes)
+    return fail(GORIO_EINVAL, "workspace of %llu bytes, need %llu", (unsigned long long)workspace_bytes,
+                (unsigned long long)d.bytes);
+  const uint32_t group = at.heads / c.heads, element = c.dtype == GORIO_KV_E4M3 ? 1 : 2;
   AttendParams p;
   p.q = static_cast<const uint16_t *>(at.q);
   p.out = static_cast<uint16_t *>(at.out);
@@ -178,24 +115,35 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
   p.fills = at.fills;
   p.prefix = at.prefix;
   p.slopes = at.slopes;
-  p.tokens = at.tokens;
+  p.parts = static_cast<float *>(workspace);
   p.q_stride = at.q_stride;
   p.out_stride = at.out_stride;
-  p.page_stride = c.page_stride;
-  p.head_stride = c.head_stride;
-  p.token_stride = c.token_stride;
+  p.page_stride = c.page_stride * element;
+  p.head_stride = c.head_stride * element;
+  p.token_stride = c.token_stride * element;
+  p.tokens = (uint32_t)at.tokens;
   p.num_pages = (uint32_t)c.num_pages;
   p.requests = at.requests;
   p.width = at.width;
   p.heads = at.heads;
   p.kv_heads = c.heads;
-  p.group = at.heads / c.heads;
   p.D = c.D;
   p.page_tokens = make_fastdiv(c.page_tokens);
+  p.group = make_fastdiv(group);
+  p.by_kv = make_fastdiv(c.heads);
   p.scale = at.scale;
   p.cap = at.cap;
-  p.window = at.window;
-  const dim3 grid((uint32_t)at.tokens, at.heads);
-  attend_rows<<<grid, 64, 0, static_cast<hipStream_t>(stream)>>>(p, c.dtype == GORIO_KV_E4M3, at.dtype == GORIO_KV_F16);
-  return kv_launched("gorio_kv_attend");
+  p.window = at.window ? at.window : (uint32_t)kKvMost;
+  p.rows = kFewRows;
+  p.least = kLeast;
+  p.most = kMost;
+  p.part_slots = d.slots;
+  AttendLaunch l;
+  l.e4m3 = c.dtype == GORIO_KV_E4M3;
+  l.more = at.cap > 0.f || at.slopes;
+  l.few_grid = d.grid;
+  l.join_grid = d.join;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = at.dtype == GORIO_KV_F16 ? launch_attend_f16(p, l, s) : launch_attend_bf16(p, l, s);
+  return e == hipSuccess ? GORIO_OK : fail(GORIO_EDEVICE, "gorio_kv_attend: %s", hipGetErrorString(e));
 }

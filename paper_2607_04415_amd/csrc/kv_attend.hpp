@@ -1,0 +1,324 @@
+// Device code that the attention kernels of gorio_kv_attend share: the types
+// of the matrix instructions, how a call's work is divided, and where keys and
+// values lie.
+//
+// Transposed products.  A kernel computes S^T = K Q^T and O^T = V^T P^T on the
+// matrix units.  In the result of a matrix instruction a lane holds several
+// rows of ONE column, so with queries as columns everything the softmax needs
+// of a query (its maximum, its sum, its rescaling factor, its position) is one
+// value in its lanes, and the weights come out where the second product wants
+// them: a lane holds the weights of its query for a set of keys, and that set
+// may be any, as long as the values are loaded in the same order.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "kv.hpp"
+
+namespace gorio {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Queries' element types.
+struct KvBf16 {
+  static constexpr bool kF16 = false;
+  static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                   0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float x, float y) {
+    const bf16x2 v = {(__bf16)x, (__bf16)y};
+    return __builtin_bit_cast(uint32_t, v);
+  }
+  template <bool kHi>
+  static __device__ __forceinline__ uint32_t widen(uint32_t w) {  // two 8-bit values, exactly
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, kHi));
+  }
+};
+
+struct KvF16 {
+  static constexpr bool kF16 = true;
+  static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+                                                  0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float x, float y) {
+    const f16x2 v = {(_Float16)x, (_Float16)y};
+    return __builtin_bit_cast(uint32_t, v);
+  }
+  template <bool kHi>
+  static __device__ __forceinline__ uint32_t widen(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, kHi));
+  }
+};
+
+struct AttendParams {
+  const uint16_t *q;
+  uint16_t *out;
+  float *lse;
+  const uint8_t *keys, *values;
+  const float *key_scale, *value_scale;
+  const int32_t *starts, *lens, *tables, *fills, *prefix;
+  const float *slopes;
+  float *parts;  // workspace
+  uint64_t q_stride, out_stride;                    // elements
+  uint64_t page_stride, head_stride, token_stride;  // bytes
+  uint32_t tokens, num_pages, requests, width, heads, kv_heads, D;
+  FastDiv page_tokens, group, by_kv;
+  float scale, cap;
+  uint32_t window;  // 2^31 - 1: none
+  // division of the work (see WorkItem)
+  uint32_t rows;         // query rows of a tile
+  uint32_t least, most;  // key blocks of a part, at least; parts to aim at, all heads together
+  uint32_t part_slots;   // parts that the workspace holds, of one head
+};
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Zeros that lanes without a key (or past a head's D) read instead of memory
+// that is not theirs: a 0 from here, times any weight, adds nothing.
+__device__ __align__(16) static uint32_t kv_zeros[4];
+
+// A request as the kernels see it: every value clamped into its range.
+struct Request {
+  int32_t start, added, len, prefix;
+};
+
+__device__ __forceinline__ Request request_of(const AttendParams &p, uint32_t b) {
+  Request r;
+  r.start = min(max(p.starts[b], 0), (int32_t)p.tokens);
+  r.added = max(min(max(p.starts[b + 1], 0), (int32_t)p.tokens) - r.start, 0);
+  r.len = max(p.lens[b], 0);
+  r.prefix = p.prefix ? max(p.prefix[b], 0) : 0;
+  return r;
+}
+
+// The key blocks of kBlock keys that a run of tokens at positions first..last
+// sees something of: `head` blocks from 0 (the prefix), then those from `near`
+// on (the window), `count` in all.
+struct KeyRange {
+  int32_t head, near, count, end;  // end: no key from here on is seen
+  __device__ __forceinline__ int32_t block(int32_t x) const { return x < head ? x : x - head + near; }
+};
+
+template <int kBlock>
+__device__ __forceinline__ KeyRange key_range(const AttendParams &p, const Request &r, int32_t first, int32_t last) {
+  KeyRange k;
+  const int32_t held = (int32_t)min((int64_t)r.len, (int64_t)p.width * p.page_tokens.d);
+  const int32_t prefix = min(r.prefix, held);
+  k.end = min(held, max(last + 1, prefix));
+  const int32_t from = (int32_t)max((int64_t)first - p.window + 1, (int64_t)0);
+  k.head = (prefix + kBlock - 1) / kBlock;
+  k.near = max(k.head, from / kBlock);
+  const int32_t ends = (k.end + kBlock - 1) / kBlock;
+  k.count = k.head + max(ends - k.near, 0);
+  return k;
+}
+
+// ---------------------------------------------------------------------------
+// Division of the work.  A tile is `rows` query rows (token x head of the
+// group) of one request and key head; a part is a run of key blocks of a
+// tile.  How long the requests are is known on the GPU only, so every block
+// of threads finds its own part: it sums the key blocks of all tiles, takes
+// from that the length c of a part (so that about `most` parts come out, none
+// shorter than `least`), and walks the requests' numbers of parts up to its
+// own index.  That is two passes over a few lengths in L2; a kernel that did
+// it once before would cost a launch.
+// ---------------------------------------------------------------------------
+struct WorkItem {
+  uint32_t request, tile, part;
+  uint32_t parts;      // of each of the request's tiles, 1: undivided
+  uint32_t slot;       // in the workspace, if divided
+  uint32_t c;          // key blocks of a part
+  Request r;
+};
+
+__device__ __forceinline__ uint32_t tiles_of(const AttendParams &p, const Request &r) {
+  return (uint32_t)(((uint64_t)r.added * p.group.d + p.rows - 1) / p.rows);
+}
+
+template <int kThreads>
+__device__ __forceinline__ uint32_t scan_threads(uint32_t v, uint32_t *sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t up = __shfl_up(v, d);
+    if (lane >= d) v += up;
+  }
+  __syncthreads();
+  if (lane == 63) sums[wave] = v;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w)
+    if (w < wave) v += sums[w];
+  return v;
+}
+
+// Item number `index` of the call, or false if there are not as many.  With
+// kJoin the items are the divided tiles themselves (which a second kernel
+// joins), and part is 0.  Every thread of the block gets the same answer.
+template <int kThreads, int kBlock, bool kJoin>
+__device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item) {
+  __shared__ uint32_t s_sums[kThreads / 64];
+  __shared__ uint64_t s_work[kThreads / 64];
+  __shared__ WorkItem s_item;
+  __shared__ int s_found;
+  uint64_t work = 0;
+  for (uint32_t b = threadIdx.x; b < p.requests; b += kThreads) {
+    const Request r = request_of(p, b);
+    const uint32_t tiles = tiles_of(p, r);
+    if (tiles) work += (uint64_t)tiles * key_range<kBlock>(p, r, r.len - r.added, r.len - 1).count;
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d);
+  if ((threadIdx.x & 63) == 0) s_work[threadIdx.x >> 6] = work;
+  if (threadIdx.x == 0) s_found = 0;
+  __syncthreads();
+  work = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) work += s_work[w];
+  const uint64_t each = (work * p.kv_heads + p.most - 1) / p.most;
+  const uint32_t c = (uint32_t)min(max(each, (uint64_t)p.least), (uint64_t)1 << 30);
+  uint32_t items0 = 0, slots0 = 0;
+  for (uint32_t b0 = 0; b0 < p.requests; b0 += kThreads) {
+    const uint32_t b = b0 + threadIdx.x;
+    WorkItem mine;
+    uint32_t tiles = 0, items = 0, slots = 0;
+    mine.parts = 1;
+    if (b < p.requests) {
+      mine.r = request_of(p, b);
+      tiles = tiles_of(p, mine.r);
+      if (tiles) {
+        const uint32_t blocks = key_range<kBlock>(p, mine.r, mine.r.len - mine.r.added, mine.r.len - 1).count;
+        mine.parts = max((blocks + c - 1) / c, 1u);
+        slots = mine.parts > 1 ? tiles * mine.parts : 0;
+        items = kJoin ? (mine.parts > 1 ? tiles : 0) : tiles * mine.parts;
+      }
+    }
+    const uint32_t items1 = items0 + scan_threads<kThreads>(items, s_sums);
+    const uint32_t slots1 = slots0 + scan_threads<kThreads>(slots, s_sums);
+    if (index < items1 && index >= items1 - items) {
+      const uint32_t at = index - (items1 - items), per = kJoin ? 1 : mine.parts;
+      mine.request = b;
+      // the last tiles of a chunk see the most keys: they begin first
+      const uint32_t from_end = at / per;
+      mine.tile = tiles - 1 - from_end;
+      mine.part = at - from_end * per;
+      mine.slot = slots1 - slots + from_end * mine.parts + mine.part;
+      mine.c = c;
+      s_item = mine;
+      s_found = 1;
+    }
+    __syncthreads();
+    if (s_found) break;
+    if (threadIdx.x == kThreads - 1) s_sums[0] = items1, s_work[0] = slots1;
+    __syncthreads();
+    items0 = s_sums[0];
+    slots0 = (uint32_t)s_work[0];
+    __syncthreads();
+  }
+  if (!s_found) return false;
+  item = s_item;
+  return true;
+}
+
+// Rows of a tile: row n is token n / group of the request's new ones, head
+// n % group of the key head's.
+struct Tile {
+  uint32_t row0, rows;    // first row, rows
+  int32_t first, last;    // positions of its first and last token
+};
+
+__device__ __forceinline__ Tile tile_of(const AttendParams &p, const WorkItem &w) {
+  Tile t;
+  const uint32_t all = (uint32_t)w.r.added * p.group.d;
+  t.row0 = w.tile * p.rows;
+  t.rows = min(p.rows, all - t.row0);
+  const int32_t base = w.r.len - w.r.added;
+  t.first = base + (int32_t)fastdiv(t.row0, p.group);
+  t.last = base + (int32_t)fastdiv(t.row0 + t.rows - 1, p.group);
+  return t;
+}
+
+__device__ __forceinline__ float xor32(float x, float (*op)(float, float)) {
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return op(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+__device__ __forceinline__ float xor16(float x, float (*op)(float, float)) {
+  const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return op(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+__device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+
+// 2^x; -inf gives 0.
+__device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// cap * tanh(x / cap) for x = s: with e = 2^(-2 |x / cap| log2 e), tanh = (1 - e) / (1 + e).
+// 1 - e is exact to 2^-24 of 1, so the result to about 2^-23 of the cap.
+__device__ __forceinline__ float capped(float s, float cap, float by) {  // by = -2 log2 e / cap
+  const float e = pow2(fabsf(s) * by);
+  return copysignf(cap * ((1.f - e) * __builtin_amdgcn_rcpf(1.f + e)), s);
+}
+
+// Values that are NaN or inf, two 16-bit elements a word.
+template <typename Q>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {  // all ones where an element is
+  const uint32_t e = Q::kF16 ? 0x7C00u : 0x7F80u;
+  return ((w & e) == e ? 0xFFFFu : 0u) | ((w >> 16 & e) == e ? 0xFFFF0000u : 0u);
+}
+template <typename Q>
+__device__ __forceinline__ bool any_not_finite(uint32_t w) {
+  return not_finite<Q>(w) != 0;
+}
+template <typename Q>
+__device__ __forceinline__ u32x4 finite_only(u32x4 a) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] &= ~not_finite<Q>(a[i]);
+  return a;
+}
+// What the NaN and inf among values `a` give a sum over the keys with a 1 in `seen`: the
+// values of +inf or NaN and those of -inf or NaN are counted by two products, and a count
+// stands for +inf, or -inf, whose sum is NaN where both are.
+template <typename Q>
+__device__ __forceinline__ u32x4 sign_ones(u32x4 a, bool negative) {
+  u32x4 ones;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int h = 0; h < 32; h += 16) {
+      const uint32_t x = a[i] >> h & 0xFFFFu, e = Q::kF16 ? 0x7C00u : 0x7F80u;
+      const bool nan = (x & 0x7FFFu) > e, inf = (x & 0x7FFFu) == e && (x >> 15) == (negative ? 1u : 0u);
+      if (nan || inf) w |= (Q::kF16 ? 0x3C00u : 0x3F80u) << h;
+    }
+    ones[i] = w;
+  }
+  return ones;
+}
+template <typename Q>
+__device__ __forceinline__ f32x4 not_finite_part(u32x4 a, u32x4 seen) {
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  const f32x4 up = Q::mfma16(sign_ones<Q>(a, false), seen, zero), down = Q::mfma16(sign_ones<Q>(a, true), seen, zero);
+  f32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = (up[i] > 0.f ? INFINITY : 0.f) + (down[i] > 0.f ? -INFINITY : 0.f);
+  return r;
+}
+
+// LDS written by some lanes of a wave and read by others of the same wave:
+// the hardware keeps their order, the compiler has to.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+}  // namespace gorio

@@ -1,0 +1,362 @@
+// Attention of few query rows (up to 16 of a request and key head) over many
+// keys: the form for single tokens.
+//
+// Every key and value is read once for 16 rows or fewer, far below what the
+// matrix units could do with it, so the rate at which HBM gives them is the
+// bound.  Four waves share a part of the keys, 32 at a time each; a wave keeps
+// its own running maximum, sum and output, joined in LDS at the end, so no
+// wave waits for another in between.  Keys and values go from memory straight
+// into the operands of the matrix instructions (16x16x32):
+//   S^T = K Q^T: lane (m, g) = (lane % 16, lane / 16) holds elements 32 s + 8 g
+//     .. + 7 of key m, one 16-byte load; the result gives it the scores of
+//     query m for keys 4 g .. + 3 of each 16.
+//   O^T = V^T P^T: the lane's eight weights are those of keys 4 g .. + 3 and
+//     16 + 4 g .. + 3, so it loads elements 8 m .. + 7 of these eight values
+//     (one 16-byte load each) and transposes 8 x 8 in registers, a byte
+//     permutation a pair: product t then yields elements 8 m + t.
+// Where a key's row lies (table entry, page, place) is worked out by one lane
+// a key, a block ahead, and handed to the others through LDS.
+#pragma once
+
+#include <type_traits>
+
+#include "kv_attend.hpp"
+
+namespace gorio {
+
+constexpr int kFewThreads = 256;
+constexpr int kFewWaves = kFewThreads / 64;
+constexpr int kFewRows = 16;
+constexpr int kFewBlock = 32;  // keys
+
+// One lane's view of a key: its row in memory, or none.
+struct KeyPlace {
+  int32_t page;  // -1: not there
+  uint32_t place;
+};
+
+__device__ __forceinline__ KeyPlace key_place(const AttendParams &p, const WorkItem &w, const Tile &t, int32_t j,
+                                              int32_t end) {
+  KeyPlace k{-1, 0};
+  const uint32_t b = w.request;
+  // a key that no row of the tile sees is not there: whatever its value holds does not reach them
+  if (j < end && ((j <= t.last && (int64_t)t.first - j < p.window) || j < w.r.prefix)) {
+    const uint32_t e = fastdiv((uint32_t)j, p.page_tokens);
+    const uint64_t at = (uint64_t)b * p.width + e;
+    k.place = (uint32_t)j - e * p.page_tokens.d;
+    const int32_t page = p.tables[at];
+    if ((uint32_t)page < p.num_pages) k.page = page;
+    if (p.fills && (int32_t)k.place >= p.fills[at]) k.page = -1;
+  }
+  return k;
+}
+
+// kSteps: 32-element steps of a head, D <= 32 kSteps.  k8: pages of 8-bit values.
+// kMore: scores are capped or biased.
+template <typename Q, bool k8, int kSteps, bool kMore>
+__global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
+  constexpr int kHalves = (kSteps + 3) / 4;  // 128 elements of a value
+  constexpr int kDim = kHalves * 128;
+  constexpr int kPad = kDim + 4;
+  typedef typename std::conditional<k8, u32x2, u32x4>::type Raw;  // 8 elements as they lie
+  __shared__ uint64_t s_row[kFewWaves][2][2][kFewBlock];  // wave, turn, keys or values
+  __shared__ float s_o[kFewWaves][kFewRows][kPad];
+  __shared__ float s_m[kFewWaves][kFewRows], s_l[kFewWaves][kFewRows];
+
+  uint32_t head, index;
+  index = fastdiv(blockIdx.x, p.by_kv);
+  head = blockIdx.x - index * p.kv_heads;
+  WorkItem w;
+  if (!find_item<kFewThreads, kFewBlock, false>(p, index, w)) return;
+  const Tile tile = tile_of(p, w);
+  const KeyRange range = key_range<kFewBlock>(p, w.r, tile.first, tile.last);
+  const uint32_t parts = max(((uint32_t)range.count + w.c - 1) / w.c, 1u);  // of this tile
+  if (w.part >= parts) return;
+  const int32_t x_end = min((int64_t)range.count, (int64_t)(w.part + 1) * w.c);
+
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int m = lane & 15, g = lane >> 4;
+  const uint64_t zeros = (uint64_t)(uintptr_t)kv_zeros;
+  constexpr int kElem = k8 ? 1 : 2;
+
+  // this lane's query
+  const uint32_t n = min((uint32_t)m, tile.rows - 1);  // rows past the last repeat it
+  const uint32_t token = fastdiv(tile.row0 + n, p.group), gh = tile.row0 + n - token * p.group.d;
+  const int32_t pos = w.r.len - w.r.added + (int32_t)token;
+  const int32_t oldest = (int32_t)max((int64_t)pos - p.window + 1, (int64_t)0);  // the window's first key
+  const uint32_t qhead = head * p.group.d + gh;
+  u32x4 q[kSteps];
+  {
+    const uint16_t *row = p.q + (uint64_t)(w.r.start + token) * p.q_stride + (uint64_t)qhead * p.D;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const uint32_t d = s * 32 + g * 8;
+      q[s] = d < p.D ? *reinterpret_cast<const u32x4 *>(row + d) : u32x4{0, 0, 0, 0};
+    }
+  }
+  const float scale = p.scale * (p.key_scale ? p.key_scale[head] : 1.f);
+  const float to_log2 = kMore ? kLog2e : scale * kLog2e;
+  const float slope = kMore && p.slopes ? p.slopes[qhead] : 0.f;
+  const float cap = p.cap, cap_by = cap > 0.f ? -2.f * kLog2e / cap : 0.f;
+
+  float best = -INFINITY, sum = 0.f;
+  f32x4 o[kHalves * 8];
+#pragma unroll
+  for (int t = 0; t < kHalves * 8; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // Rows of block x into LDS, and its keys' bits: lanes 0..31 a key each.
+  auto place_of = [&](int32_t x) {
+    return key_place(p, w, tile, x < x_end && lane < kFewBlock ? range.block(x) * kFewBlock + lane : range.end,
+                     range.end);
+  };
+  auto hand_out = [&](const KeyPlace &k, int turn) -> uint32_t {
+    const bool there = k.page >= 0;
+    if (lane < kFewBlock) {
+      const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
+      s_row[wave][turn][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : 0;
+      s_row[wave][turn][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : 0;
+    }
+    wave_lds_order();
+    return (uint32_t)__ballot(there && lane < kFewBlock);
+  };
+  auto load_keys = [&](Raw (&k)[2][kSteps], int turn) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint64_t row = s_row[wave][turn][0][i * 16 + m];
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const uint32_t d = s * 32 + g * 8;
+        const uint64_t at = row && d < p.D ? row + d * kElem : zeros;
+        k[i][s] = *reinterpret_cast<const Raw *>(at);
+      }
+    }
+  };
+  auto load_values = [&](Raw (&v)[8], int half, int turn) {
+    const uint32_t d = half * 128 + m * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint64_t row = s_row[wave][turn][1][(i >> 2) * 16 + g * 4 + (i & 3)];
+      const uint64_t at = row && d < p.D ? row + d * kElem : zeros;
+      v[i] = *reinterpret_cast<const Raw *>(at);
+    }
+  };
+  auto wide = [](Raw r) -> u32x4 {
+    if constexpr (k8)
+      return u32x4{Q::template widen<false>(r.x), Q::template widen<true>(r.x), Q::template widen<false>(r.y),
+                   Q::template widen<true>(r.y)};
+    else
+      return r;
+  };
+
+  int32_t x = (int32_t)(w.part * w.c) + wave;
+  int turn = 0;
+  Raw k[2][kSteps];
+  uint32_t there = hand_out(place_of(x), 0);
+  load_keys(k, 0);
+  KeyPlace next = place_of(x + kFewWaves);
+  for (; x < x_end; x += kFewWaves) {
+    const int32_t j0 = range.block(x) * kFewBlock;
+    Raw v[kHalves][8];
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) load_values(v[h], h, turn);
+    // the next block's keys and, one further, its places are on their way during this one's products
+    u32x4 kw[2][kSteps];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) kw[i][s] = wide(k[i][s]);
+    const uint32_t there_now = there;
+    there = hand_out(next, turn ^ 1);
+    load_keys(k, turn ^ 1);
+    next = place_of(x + 2 * kFewWaves);
+
+    f32x4 s2[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      s2[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) s2[i] = Q::mfma16(kw[i][s], q[s], s2[i]);
+    }
+    float e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float y = s2[i >> 2][i & 3];
+      if constexpr (kMore) {
+        y *= scale;
+        if (cap > 0.f) y = capped(y, cap, cap_by);
+        const int32_t j = j0 + (i >> 2) * 16 + g * 4 + (i & 3);
+        y -= slope * fabsf((float)(pos - j));
+      }
+      e[i] = y * to_log2;
+    }
+    // all rows see all of these keys, or each row is asked for each key
+    const bool whole = there_now == 0xFFFFFFFFu &&
+                       ((j0 + kFewBlock - 1 <= tile.first && tile.last - j0 < (int64_t)p.window) ||
+                        j0 + kFewBlock <= w.r.prefix);
+    uint32_t sees = 0xFF;  // this lane's eight keys
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int at = (i >> 2) * 16 + g * 4 + (i & 3);
+        const int32_t j = j0 + at;
+        const uint32_t seen = (there_now >> at & 1u) & (((uint32_t)(j <= pos) & (uint32_t)(j >= oldest)) | (uint32_t)(j < w.r.prefix));
+        e[i] = seen ? e[i] : -INFINITY;
+        sees &= ~((seen ^ 1u) << i);
+      }
+    }
+    float top = fmaxf(fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])), fmaxf(fmaxf(e[4], e[5]), fmaxf(e[6], e[7])));
+    top = xor16(xor32(top, max_of), max_of);
+    if (__any(top > best)) {
+      const float to = fmaxf(best, top);
+      const float keep = to == -INFINITY ? 1.f : pow2(best - to);
+      best = to;
+      sum *= keep;
+#pragma unroll
+      for (int t = 0; t < kHalves * 8; ++t) o[t] *= keep;
+    }
+    const float base = best == -INFINITY ? 0.f : best;
+    float part = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      e[i] = pow2(e[i] - base);
+      part += e[i];
+    }
+    sum += part;
+    const u32x4 weights = {Q::pack(e[0], e[1]), Q::pack(e[2], e[3]), Q::pack(e[4], e[5]), Q::pack(e[6], e[7])};
+    u32x4 seen_weights;  // 1 where the row sees the key
+#pragma unroll
+    for (int i = 0; i < 4; ++i) seen_weights[i] = Q::pack(sees >> (2 * i) & 1, sees >> (2 * i + 1) & 1);
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
+      u32x4 vw[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) vw[i] = wide(v[h][i]);
+      // A weight of 0 keeps a value out of a row, unless the value is NaN or inf.  Such
+      // values in a block that some rows see only in part go in apart from the others.
+      bool odd = false;
+      if (!whole && tile.first != tile.last) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) odd |= any_not_finite<Q>(vw[i][c]);
+        odd = __any(odd);
+      }
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const uint32_t sel = t & 1 ? 0x07060302u : 0x05040100u;
+        u32x4 a;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(vw[2 * i + 1][t >> 1], vw[2 * i][t >> 1], sel);
+        if (odd) o[h * 8 + t] += not_finite_part<Q>(a, seen_weights);
+        if (odd) a = finite_only<Q>(a);
+        o[h * 8 + t] = Q::mfma16(a, weights, o[h * 8 + t]);
+      }
+    }
+    turn ^= 1;
+  }
+
+  // the four waves' results, joined
+  sum = xor16(xor32(sum, sum_of), sum_of);
+  if (g == 0) s_m[wave][m] = best, s_l[wave][m] = sum;
+#pragma unroll
+  for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float *to = &s_o[wave][m][h * 128 + (g * 4 + r) * 8];
+#pragma unroll
+      for (int t = 0; t < 8; t += 4)
+        *reinterpret_cast<f32x4 *>(to + t) =
+            f32x4{o[h * 8 + t][r], o[h * 8 + t + 1][r], o[h * 8 + t + 2][r], o[h * 8 + t + 3][r]};
+    }
+  __syncthreads();
+  const uint32_t row = threadIdx.x >> 4;
+  if (row >= tile.rows) return;
+  float most = s_m[0][row];
+#pragma unroll
+  for (int i = 1; i < kFewWaves; ++i) most = fmaxf(most, s_m[i][row]);
+  const float from = most == -INFINITY ? 0.f : most;
+  float by[kFewWaves], all = 0.f;
+#pragma unroll
+  for (int i = 0; i < kFewWaves; ++i) {
+    by[i] = pow2(s_m[i][row] - from);
+    all += s_l[i][row] * by[i];
+  }
+  const uint32_t tk = fastdiv(tile.row0 + row, p.group), hq = head * p.group.d + (tile.row0 + row - tk * p.group.d);
+  const uint64_t t_out = (uint64_t)(w.r.start + tk);
+  const float vs = p.value_scale ? p.value_scale[head] : 1.f;
+  const bool divided = parts > 1;
+  const float norm = divided ? 1.f : all != 0.f ? vs / all : 0.f;
+  const uint64_t slot = ((uint64_t)w.slot * p.kv_heads + head) * kFewRows + row;
+#pragma unroll
+  for (int h = 0; h < kHalves; ++h) {
+    const uint32_t d = h * 128 + (threadIdx.x & 15) * 8;
+    if (d >= p.D) break;
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      y[i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < kFewWaves; ++j) y[i] = fmaf(s_o[j][row][d + i], by[j], y[i]);
+      y[i] *= norm;
+    }
+    if (divided) {
+      float *to = p.parts + slot * p.D + d;
+      *reinterpret_cast<f32x4 *>(to) = f32x4{y[0], y[1], y[2], y[3]};
+      *reinterpret_cast<f32x4 *>(to + 4) = f32x4{y[4], y[5], y[6], y[7]};
+    } else {
+      *reinterpret_cast<u32x4 *>(p.out + t_out * p.out_stride + (uint64_t)hq * p.D + d) =
+          u32x4{Q::pack(y[0], y[1]), Q::pack(y[2], y[3]), Q::pack(y[4], y[5]), Q::pack(y[6], y[7])};
+    }
+  }
+  if ((threadIdx.x & 15) == 0) {
+    if (divided) {
+      float *ml = p.parts + (uint64_t)p.part_slots * p.kv_heads * kFewRows * p.D + slot * 2;
+      ml[0] = most;
+      ml[1] = all;
+    } else if (p.lse) {
+      p.lse[t_out * p.heads + hq] = all != 0.f ? (from + __log2f(all)) * kLn2 : -INFINITY;
+    }
+  }
+}
+
+// Joins the parts of divided tiles: a block a tile and head, 16 threads a row.
+template <typename Q, int kRows, int kBlock>
+__global__ __launch_bounds__(256) void attend_join(AttendParams p) {
+  const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
+  WorkItem w;
+  if (!find_item<256, kBlock, true>(p, index, w)) return;
+  const Tile tile = tile_of(p, w);
+  const KeyRange range = key_range<kBlock>(p, w.r, tile.first, tile.last);
+  const uint32_t parts = ((uint32_t)range.count + w.c - 1) / w.c;
+  if (parts <= 1) return;  // written by its one part
+  const float *ml0 = p.parts + (uint64_t)p.part_slots * p.kv_heads * kRows * p.D;
+  for (uint32_t row = threadIdx.x >> 4; row < tile.rows; row += 16) {
+    auto slot = [&](uint32_t i) { return ((uint64_t)(w.slot + i) * p.kv_heads + head) * kRows + row; };
+    float most = -INFINITY;
+    for (uint32_t i = 0; i < parts; ++i) most = fmaxf(most, ml0[slot(i) * 2]);
+    const float from = most == -INFINITY ? 0.f : most;
+    float all = 0.f;
+    for (uint32_t i = 0; i < parts; ++i) all += ml0[slot(i) * 2 + 1] * pow2(ml0[slot(i) * 2] - from);
+    const float vs = p.value_scale ? p.value_scale[head] : 1.f;
+    const float norm = all != 0.f ? vs / all : 0.f;
+    const uint32_t tk = fastdiv(tile.row0 + row, p.group), hq = head * p.group.d + (tile.row0 + row - tk * p.group.d);
+    const uint64_t t_out = (uint64_t)(w.r.start + tk);
+    for (uint32_t d = (threadIdx.x & 15) * 8; d < p.D; d += 128) {
+      f32x4 y[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      for (uint32_t i = 0; i < parts; ++i) {
+        const float by = pow2(ml0[slot(i) * 2] - from);
+        const f32x4 *o = reinterpret_cast<const f32x4 *>(p.parts + slot(i) * p.D + d);
+        y[0] += o[0] * by;
+        y[1] += o[1] * by;
+      }
+      y[0] *= norm;
+      y[1] *= norm;
+      *reinterpret_cast<u32x4 *>(p.out + t_out * p.out_stride + (uint64_t)hq * p.D + d) =
+          u32x4{Q::pack(y[0].x, y[0].y), Q::pack(y[0].z, y[0].w), Q::pack(y[1].x, y[1].y), Q::pack(y[1].z, y[1].w)};
+    }
+    if (p.lse && (threadIdx.x & 15) == 0)
+      p.lse[t_out * p.heads + hq] = all != 0.f ? (from + __log2f(all)) * kLn2 : -INFINITY;
+  }
+}
+
+}  // namespace gorio
