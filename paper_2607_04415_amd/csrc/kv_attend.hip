@@ -1,7 +1,6 @@
 // gorio_kv_attend: attention of new tokens over the pages of their requests.
 #include <algorithm>
 
-#include "kv_attend_few.hpp"
 #include "kv_launch.hpp"
 
 using namespace gorio;
@@ -35,30 +34,49 @@ gorio_status check(const gorio_kv_cache *cache, const gorio_kv_attention *a, gor
   return GORIO_OK;
 }
 
-constexpr uint32_t kLeast = 4, kMost = 2048;
+// Rows of a request and key head up to which the form for few rows takes it.
+constexpr uint32_t kFewUpto = 17;
 
 // What a call launches and keeps, from the sizes that the host knows: the
 // lengths are on the GPU, so these are bounds, and blocks without work return.
 // With W the key blocks of all tiles, a part has c >= W heads / most blocks, so
 // there are at most most / heads parts more than tiles; a divided tile has
 // less than 2 blocks / c parts, so divided tiles have at most 2 most / heads.
-struct Division {
-  uint32_t grid, join, slots;
-  uint64_t bytes;
-};
-
-Division divide(const gorio_kv_cache &c, const gorio_kv_attention &a) {
-  Division d{};
-  const uint64_t tiles = a.tokens * (a.heads / c.heads) / kFewRows + std::min<uint64_t>(a.requests, a.tokens);
-  const uint64_t blocks = ((uint64_t)a.width * c.page_tokens + kFewBlock - 1) / kFewBlock;
-  const uint64_t parts = (blocks + kLeast - 1) / kLeast, extra = kMost / c.heads + 1;
-  const uint64_t items = std::min(tiles * parts, tiles + extra);
+AttendForm divide(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t rows, uint32_t block, uint32_t least,
+                  uint32_t most) {
+  AttendForm f{};
+  const uint64_t tiles = a.tokens * (a.heads / c.heads) / rows + std::min<uint64_t>(a.requests, a.tokens);
+  const uint64_t blocks = ((uint64_t)a.width * c.page_tokens + block - 1) / block;
+  const uint64_t parts = (blocks + least - 1) / least, extra = most / c.heads + 1;
   const uint64_t slots = parts > 1 ? std::min(tiles * parts, 2 * extra) : 0;
-  d.grid = (uint32_t)std::min<uint64_t>(items * c.heads, kKvMost);
-  d.slots = (uint32_t)slots;
-  d.join = (uint32_t)std::min<uint64_t>(slots / 2 * c.heads, kKvMost);
-  d.bytes = slots * c.heads * kFewRows * (c.D + 2) * sizeof(float);
-  return d;
+  f.rows = rows;
+  f.from = 1;
+  f.upto = 0xFFFFFFFFu;
+  f.least = least;
+  f.most = most;
+  f.part_slots = (uint32_t)slots;
+  f.grid = (uint32_t)std::min<uint64_t>(std::min(tiles * parts, tiles + extra) * c.heads, kKvMost);
+  f.join = (uint32_t)std::min<uint64_t>(slots / 2 * c.heads, kKvMost);
+  return f;
+}
+
+// The forms that a call needs, and its workspace, which they use in turn.
+AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint64_t *bytes) {
+  AttendLaunch l{};
+  l.e4m3 = c.dtype == GORIO_KV_E4M3;
+  l.more = a.cap > 0.f || a.slopes;
+  const uint64_t group = a.heads / c.heads;
+  // the most and the fewest new tokens of a request that has any; exact for one request
+  const uint64_t most = a.max_new ? std::min<uint64_t>(a.max_new, a.tokens) : a.tokens;
+  const uint64_t others = (a.requests - 1) * most;
+  const uint64_t fewest = a.tokens > others ? a.tokens - others : 1;
+  const bool few = fewest * group < kFewUpto, many = most * group >= kFewUpto;
+  if (few) l.few = divide(c, a, kFewRows, kFewBlock, 4, 2048);
+  if (many) l.many = divide(c, a, kManyRows, kManyBlock, 4, 1024);
+  if (few && many) l.few.upto = l.many.from = kFewUpto;
+  const uint64_t row = (c.D + 2) * sizeof(float) * c.heads;
+  *bytes = std::max<uint64_t>(l.few.part_slots * kFewRows, (uint64_t)l.many.part_slots * kManyRows) * row;
+  return l;
 }
 
 }  // namespace
@@ -69,7 +87,8 @@ extern "C" gorio_status gorio_kv_workspace(const gorio_kv_cache *cache, const go
   const gorio_status st = check(cache, a, &c, &at);
   if (st != GORIO_OK) return st;
   if (!bytes) return fail(GORIO_EINVAL, "bytes is NULL");
-  *bytes = divide(c, at).bytes;
+  *bytes = 0;
+  if (at.tokens && at.requests) (void)forms_of(c, at, bytes);
   return GORIO_OK;
 }
 
@@ -96,10 +115,11 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
                 {"value_scale", c.value_scale, 4, true},
                 {"workspace", workspace, 16, workspace_bytes == 0}});
   if (st != GORIO_OK) return st;
-  const Division d = divide(c, at);
-  if (d.bytes > workspace_bytes)
+  uint64_t bytes = 0;
+  const AttendLaunch l = forms_of(c, at, &bytes);
+  if (bytes > workspace_bytes)
     return fail(GORIO_EINVAL, "workspace of %llu bytes, need %llu", (unsigned long long)workspace_bytes,
-                (unsigned long long)d.bytes);
+                (unsigned long long)bytes);
   const uint32_t group = at.heads / c.heads, element = c.dtype == GORIO_KV_E4M3 ? 1 : 2;
   AttendParams p;
   p.q = static_cast<const uint16_t *>(at.q);
@@ -134,16 +154,9 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
   p.scale = at.scale;
   p.cap = at.cap;
   p.window = at.window ? at.window : (uint32_t)kKvMost;
-  p.rows = kFewRows;
-  p.least = kLeast;
-  p.most = kMost;
-  p.part_slots = d.slots;
-  AttendLaunch l;
-  l.e4m3 = c.dtype == GORIO_KV_E4M3;
-  l.more = at.cap > 0.f || at.slopes;
-  l.few_grid = d.grid;
-  l.join_grid = d.join;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const hipError_t e = at.dtype == GORIO_KV_F16 ? launch_attend_f16(p, l, s) : launch_attend_bf16(p, l, s);
+  const bool f16 = at.dtype == GORIO_KV_F16;
+  const hipError_t e = l.e4m3 ? (f16 ? launch_attend_f16_e4m3(p, l, s) : launch_attend_bf16_e4m3(p, l, s))
+                              : (f16 ? launch_attend_f16(p, l, s) : launch_attend_bf16(p, l, s));
   return e == hipSuccess ? GORIO_OK : fail(GORIO_EDEVICE, "gorio_kv_attend: %s", hipGetErrorString(e));
 }

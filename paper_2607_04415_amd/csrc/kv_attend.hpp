@@ -33,6 +33,10 @@ struct KvBf16 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
                                                    0, 0);
   }
+  static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                   0, 0);
+  }
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
     const bf16x2 v = {(__bf16)x, (__bf16)y};
     return __builtin_bit_cast(uint32_t, v);
@@ -49,6 +53,10 @@ struct KvF16 {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
                                                   0);
   }
+  static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+                                                  0);
+  }
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
     const f16x2 v = {(_Float16)x, (_Float16)y};
     return __builtin_bit_cast(uint32_t, v);
@@ -58,6 +66,27 @@ struct KvF16 {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, kHi));
   }
 };
+
+// Eight elements as they lie in the pages -> eight of the queries' type.
+template <typename Q>
+__device__ __forceinline__ u32x4 widened(u32x4 r) {
+  return r;
+}
+template <typename Q>
+__device__ __forceinline__ u32x4 widened(u32x2 r) {
+  return u32x4{Q::template widen<false>(r.x), Q::template widen<true>(r.x), Q::template widen<false>(r.y),
+               Q::template widen<true>(r.y)};
+}
+
+// Two transposing LDS reads.  In each, lane l of 16 names the 8 bytes that hold
+// elements 4 (l % 4) .. + 3 of row l / 4, and gets element l of the four rows.
+__device__ __forceinline__ u32x4 transposed(const uint16_t *a, const uint16_t *b) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)a));
+  const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)b));
+  return u32x4{x.x, x.y, y.x, y.y};
+}
 
 struct AttendParams {
   const uint16_t *q;
@@ -76,6 +105,7 @@ struct AttendParams {
   uint32_t window;  // 2^31 - 1: none
   // division of the work (see WorkItem)
   uint32_t rows;         // query rows of a tile
+  uint32_t from, upto;   // requests with this many rows a key head, from <= rows < upto
   uint32_t least, most;  // key blocks of a part, at least; parts to aim at, all heads together
   uint32_t part_slots;   // parts that the workspace holds, of one head
 };
@@ -142,7 +172,8 @@ struct WorkItem {
 };
 
 __device__ __forceinline__ uint32_t tiles_of(const AttendParams &p, const Request &r) {
-  return (uint32_t)(((uint64_t)r.added * p.group.d + p.rows - 1) / p.rows);
+  const uint32_t rows = (uint32_t)r.added * p.group.d;
+  return (rows >= p.from) & (rows < p.upto) ? (rows + p.rows - 1) / p.rows : 0;
 }
 
 template <int kThreads>
@@ -248,6 +279,28 @@ __device__ __forceinline__ Tile tile_of(const AttendParams &p, const WorkItem &w
   return t;
 }
 
+// One lane's view of a key: its row in memory, or none.
+struct KeyPlace {
+  int32_t page;  // -1: not there
+  uint32_t place;
+};
+
+__device__ __forceinline__ KeyPlace key_place(const AttendParams &p, const WorkItem &w, const Tile &t, int32_t j,
+                                              int32_t end) {
+  KeyPlace k{-1, 0};
+  const uint32_t b = w.request;
+  // a key that no row of the tile sees is not there: whatever its value holds does not reach them
+  if (j < end && ((j <= t.last && (int64_t)t.first - j < p.window) || j < w.r.prefix)) {
+    const uint32_t e = fastdiv((uint32_t)j, p.page_tokens);
+    const uint64_t at = (uint64_t)b * p.width + e;
+    k.place = (uint32_t)j - e * p.page_tokens.d;
+    const int32_t page = p.tables[at];
+    if ((uint32_t)page < p.num_pages) k.page = page;
+    if (p.fills && (int32_t)k.place >= p.fills[at]) k.page = -1;
+  }
+  return k;
+}
+
 __device__ __forceinline__ float xor32(float x, float (*op)(float, float)) {
   const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return op(__uint_as_float(r.x), __uint_as_float(r.y));
@@ -280,6 +333,10 @@ __device__ __forceinline__ bool any_not_finite(uint32_t w) {
   return not_finite<Q>(w) != 0;
 }
 template <typename Q>
+__device__ __forceinline__ bool any_not_finite4(u32x4 a) {
+  return any_not_finite<Q>(a.x) | any_not_finite<Q>(a.y) | any_not_finite<Q>(a.z) | any_not_finite<Q>(a.w);
+}
+template <typename Q>
 __device__ __forceinline__ u32x4 finite_only(u32x4 a) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) a[i] &= ~not_finite<Q>(a[i]);
@@ -304,13 +361,27 @@ __device__ __forceinline__ u32x4 sign_ones(u32x4 a, bool negative) {
   }
   return ones;
 }
+__device__ __forceinline__ float not_finite_sum(float up, float down) {
+  return (up > 0.f ? INFINITY : 0.f) + (down > 0.f ? -INFINITY : 0.f);
+}
+template <typename Q>
+__device__ __forceinline__ f32x16 not_finite_part32(u32x4 a, u32x4 seen) {
+  f32x16 up, down;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) up[i] = down[i] = 0.f;
+  up = Q::mfma32(sign_ones<Q>(a, false), seen, up);
+  down = Q::mfma32(sign_ones<Q>(a, true), seen, down);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) up[i] = not_finite_sum(up[i], down[i]);
+  return up;
+}
 template <typename Q>
 __device__ __forceinline__ f32x4 not_finite_part(u32x4 a, u32x4 seen) {
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const f32x4 up = Q::mfma16(sign_ones<Q>(a, false), seen, zero), down = Q::mfma16(sign_ones<Q>(a, true), seen, zero);
   f32x4 r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = (up[i] > 0.f ? INFINITY : 0.f) + (down[i] > 0.f ? -INFINITY : 0.f);
+  for (int i = 0; i < 4; ++i) r[i] = not_finite_sum(up[i], down[i]);
   return r;
 }
 

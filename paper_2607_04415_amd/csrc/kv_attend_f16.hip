@@ -1,11 +1,10 @@
-// Attention kernels for f16 queries.
-#include "kv_attend_few.hpp"
+// Attention kernels of f16 queries over f16 pages.
 #include "kv_launch.hpp"
 
 namespace gorio {
 
 hipError_t launch_attend_f16(const AttendParams &p, const AttendLaunch &l, hipStream_t s) {
-  return launch_attend<KvF16>(p, l, s);
+  return launch_pages<KvF16, false>(p, l, s);
 }
 
 }  // namespace gorio

@@ -29,28 +29,6 @@ constexpr int kFewWaves = kFewThreads / 64;
 constexpr int kFewRows = 16;
 constexpr int kFewBlock = 32;  // keys
 
-// One lane's view of a key: its row in memory, or none.
-struct KeyPlace {
-  int32_t page;  // -1: not there
-  uint32_t place;
-};
-
-__device__ __forceinline__ KeyPlace key_place(const AttendParams &p, const WorkItem &w, const Tile &t, int32_t j,
-                                              int32_t end) {
-  KeyPlace k{-1, 0};
-  const uint32_t b = w.request;
-  // a key that no row of the tile sees is not there: whatever its value holds does not reach them
-  if (j < end && ((j <= t.last && (int64_t)t.first - j < p.window) || j < w.r.prefix)) {
-    const uint32_t e = fastdiv((uint32_t)j, p.page_tokens);
-    const uint64_t at = (uint64_t)b * p.width + e;
-    k.place = (uint32_t)j - e * p.page_tokens.d;
-    const int32_t page = p.tables[at];
-    if ((uint32_t)page < p.num_pages) k.page = page;
-    if (p.fills && (int32_t)k.place >= p.fills[at]) k.page = -1;
-  }
-  return k;
-}
-
 // kSteps: 32-element steps of a head, D <= 32 kSteps.  k8: pages of 8-bit values.
 // kMore: scores are capped or biased.
 template <typename Q, bool k8, int kSteps, bool kMore>
@@ -140,14 +118,6 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
       v[i] = *reinterpret_cast<const Raw *>(at);
     }
   };
-  auto wide = [](Raw r) -> u32x4 {
-    if constexpr (k8)
-      return u32x4{Q::template widen<false>(r.x), Q::template widen<true>(r.x), Q::template widen<false>(r.y),
-                   Q::template widen<true>(r.y)};
-    else
-      return r;
-  };
-
   int32_t x = (int32_t)(w.part * w.c) + wave;
   int turn = 0;
   Raw k[2][kSteps];
@@ -164,7 +134,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) kw[i][s] = wide(k[i][s]);
+      for (int s = 0; s < kSteps; ++s) kw[i][s] = widened<Q>(k[i][s]);
     const uint32_t there_now = there;
     there = hand_out(next, turn ^ 1);
     load_keys(k, turn ^ 1);
@@ -230,7 +200,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
     for (int h = 0; h < kHalves; ++h) {
       u32x4 vw[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) vw[i] = wide(v[h][i]);
+      for (int i = 0; i < 8; ++i) vw[i] = widened<Q>(v[h][i]);
       // A weight of 0 keeps a value out of a row, unless the value is NaN or inf.  Such
       // values in a block that some rows see only in part go in apart from the others.
       bool odd = false;

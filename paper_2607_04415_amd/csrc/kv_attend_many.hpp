@@ -1,0 +1,282 @@
+// Attention of many query rows over many keys: the form for chunks.
+//
+// With 128 rows to a tile every key is used often enough that the matrix units
+// are the bound, and next to them the vector units, which turn 2 x 32 x 32
+// products into exponentials for every 16 matrix instructions.  Each of four
+// waves owns 32 rows for the whole run; blocks of 64 keys and values pass
+// through LDS, two buffers deep, so that a block's loads run during the
+// products of the one before and a barrier a block suffices.  Two workgroups
+// fit a CU, and one's exponentials run beside the other's products.  On
+// 32x32x16 instructions:
+//   S^T = K Q^T: lane (m, g) = (lane % 32, lane / 32) reads elements 16 s + 8 g
+//     .. + 7 of key m; the result gives it, of query m, the scores of keys
+//     8 i + 4 g .. + 3 for i = 0..3.
+//   O^T = V^T P^T: sixteen keys at a time, of which the lane has the weights
+//     of 4 g .. + 3 and 8 + 4 g .. + 3; the transposing LDS read gives it the
+//     values of those keys at element m.
+// Key rows are padded by 16 bytes, so that 16 neighbouring keys' 16-byte reads
+// fall on different banks; value rows to 64 or 192 bytes past a multiple of
+// 256, so that four keys' 64-byte reads do.
+#pragma once
+
+#include <type_traits>
+
+#include "kv_attend.hpp"
+
+namespace gorio {
+
+constexpr int kManyWaves = 4;
+constexpr int kManyThreads = kManyWaves * 64;
+constexpr int kManyRows = kManyWaves * 32;
+constexpr int kManyBlock = 64;  // keys
+
+// A maximum is kept until a score passes it by 2^8 (weights stay far inside
+// f16's range, and a sum of them loses nothing): most blocks then rescale nothing.
+constexpr float kSlack = 8.f;
+
+// The low n bits, n of any size.
+__device__ __forceinline__ uint64_t low_bits(int32_t n) {
+  const uint64_t some = (1ull << (n & 63)) - 1;
+  return n <= 0 ? 0 : n >= 64 ? ~0ull : some;
+}
+
+// kSteps: D <= 32 kSteps.  k8: pages of 8-bit values.  kMore: scores are capped or biased.
+template <typename Q, bool k8, int kSteps, bool kMore>
+__global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(AttendParams p) {
+  constexpr int kDim = kSteps * 32, kChunks = kDim / 8;
+  constexpr int kKeyRow = kDim + 8;                                                  // elements
+  constexpr int kValueRow = (kDim * 2) % 256 == 192 ? kDim : kDim + 32;
+  constexpr int kPasses = kManyBlock * kChunks / kManyThreads;                       // 16-byte pieces a thread
+  static_assert(kPasses * kManyThreads == kManyBlock * kChunks, "pieces divide");
+  constexpr int kElem = k8 ? 1 : 2;
+  typedef typename std::conditional<k8, u32x2, u32x4>::type Raw;
+  __shared__ __align__(16) uint16_t s_k[2][kManyBlock * kKeyRow];
+  __shared__ __align__(16) uint16_t s_v[2][kManyBlock * kValueRow];
+  __shared__ uint64_t s_row[2][2][kManyBlock];  // turn, keys or values
+  __shared__ uint64_t s_there[4];
+
+  const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
+  WorkItem w;
+  if (!find_item<kManyThreads, kManyBlock, false>(p, index, w)) return;
+  const Tile tile = tile_of(p, w);
+  const KeyRange range = key_range<kManyBlock>(p, w.r, tile.first, tile.last);
+  const uint32_t parts = max(((uint32_t)range.count + w.c - 1) / w.c, 1u);
+  if (w.part >= parts) return;
+  const int32_t x0 = (int32_t)(w.part * w.c);
+  const int32_t x_end = (int32_t)min((int64_t)range.count, (int64_t)x0 + w.c);
+
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int m = lane & 31, g = lane >> 5;
+  const uint64_t zeros = (uint64_t)(uintptr_t)kv_zeros;
+
+  // this lane's query; rows past the last repeat it
+  const uint32_t wave_row = tile.row0 + min((uint32_t)wave * 32, tile.rows - 1);
+  const uint32_t wave_end = min(tile.row0 + (uint32_t)wave * 32 + 31, tile.row0 + tile.rows - 1);
+  const bool has_rows = (uint32_t)wave * 32 < tile.rows;
+  const uint32_t row = min(tile.row0 + (uint32_t)wave * 32 + m, tile.row0 + tile.rows - 1);
+  const uint32_t token = fastdiv(row, p.group), gh = row - token * p.group.d;
+  const int32_t base = w.r.len - w.r.added;
+  const int32_t pos = base + (int32_t)token;
+  const int32_t oldest = (int32_t)max((int64_t)pos - p.window + 1, (int64_t)0);  // the window's first key
+  const int32_t first = base + (int32_t)fastdiv(wave_row, p.group), last = base + (int32_t)fastdiv(wave_end, p.group);
+  const uint32_t qhead = head * p.group.d + gh;
+  const float scale = p.scale * (p.key_scale ? p.key_scale[head] : 1.f);
+  // the running maximum is taken of the products as they are, so the factor has to be positive:
+  // a negative one turns the queries' signs around
+  const uint32_t flip = !kMore && scale < 0.f ? 0x80008000u : 0u;
+  const float factor = scale == 0.f ? 1e-30f : fabsf(scale) * kLog2e;  // 0 times a masked score's -inf would be NaN
+  u32x4 q[kSteps * 2];
+  {
+    const uint16_t *at = p.q + (uint64_t)(w.r.start + token) * p.q_stride + (uint64_t)qhead * p.D;
+#pragma unroll
+    for (int s = 0; s < kSteps * 2; ++s) {
+      const uint32_t d = s * 16 + g * 8;
+      q[s] = d < p.D ? *reinterpret_cast<const u32x4 *>(at + d) : u32x4{0, 0, 0, 0};
+      q[s] ^= flip;
+    }
+  }
+  const float slope = kMore && p.slopes ? p.slopes[qhead] : 0.f;
+  const float cap = p.cap, cap_by = cap > 0.f ? -2.f * kLog2e / cap : 0.f;
+
+  // Where block x's keys lie: threads 0..63 look up a key each ...
+  auto look_up = [&](int32_t x) {
+    const int32_t j = x < x_end ? range.block(x) * kManyBlock + lane : range.end;
+    return key_place(p, w, tile, j, range.end);
+  };
+  // ... and hand its rows to all.
+  auto hand_out = [&](const KeyPlace &k, int32_t x) {
+    const bool there = k.page >= 0;
+    const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
+    s_row[x & 1][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : 0;
+    s_row[x & 1][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : 0;
+    const uint64_t bits = __ballot(there);
+    if (lane == 0) s_there[x & 3] = bits;
+  };
+  Raw stage[2][kPasses];
+  auto load = [&](int32_t x) {
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i) {
+        const uint32_t piece = i * kManyThreads + threadIdx.x, key = piece / kChunks, d = piece % kChunks * 8;
+        const uint64_t at = s_row[x & 1][kv][key];
+        stage[kv][i] = *reinterpret_cast<const Raw *>(at && d < p.D ? at + d * kElem : zeros);
+      }
+  };
+  auto put = [&](int32_t x) {
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      const uint32_t piece = i * kManyThreads + threadIdx.x, key = piece / kChunks, d = piece % kChunks * 8;
+      *reinterpret_cast<u32x4 *>(&s_k[x & 1][key * kKeyRow + d]) = widened<Q>(stage[0][i]);
+      *reinterpret_cast<u32x4 *>(&s_v[x & 1][key * kValueRow + d]) = widened<Q>(stage[1][i]);
+    }
+  };
+
+  float best = -INFINITY, sum = 0.f;  // best: of scores in log2, as last rescaled to
+  f32x16 o[kSteps];
+#pragma unroll
+  for (int t = 0; t < kSteps; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+
+  KeyPlace ahead{-1, 0};
+  if (wave == 0) {
+    hand_out(look_up(x0), x0);
+    hand_out(look_up(x0 + 1), x0 + 1);
+    ahead = look_up(x0 + 2);
+  }
+  __syncthreads();
+  load(x0);
+  put(x0);
+  __syncthreads();
+  for (int32_t x = x0; x < x_end; ++x) {
+    const bool more = x + 1 < x_end;
+    if (more) load(x + 1);
+    if (wave == 0) {
+      hand_out(ahead, x + 2);
+      ahead = look_up(x + 3);
+    }
+    const int32_t j0 = range.block(x) * kManyBlock;
+    const uint64_t there = s_there[x & 3];
+    const bool seen_any = has_rows && ((j0 <= last && (int64_t)j0 + kManyBlock - 1 > (int64_t)first - p.window) || j0 < w.r.prefix);
+    if (seen_any) {
+      const uint16_t *keys = s_k[x & 1], *values = s_v[x & 1];
+      f32x16 s[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kSteps * 2; ++k)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          s[t] = Q::mfma32(*reinterpret_cast<const u32x4 *>(&keys[(t * 32 + m) * kKeyRow + k * 16 + g * 8]), q[k], s[t]);
+      if constexpr (kMore) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float y = s[t][i] * scale;
+            if (cap > 0.f) y = capped(y, cap, cap_by);
+            const int32_t j = j0 + t * 32 + (i >> 2) * 8 + g * 4 + (i & 3);
+            s[t][i] = (y - slope * fabsf((float)(pos - j))) * kLog2e;
+          }
+      }
+      const float to_log2 = kMore ? 1.f : factor;
+      const bool whole = there == ~0ull && ((j0 + kManyBlock - 1 <= first && (int64_t)last - j0 < p.window) ||
+                                            j0 + kManyBlock <= w.r.prefix);
+      uint64_t sees = ~0ull;
+      if (!whole) {
+        sees = there & ((low_bits(pos - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(w.r.prefix - j0));
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const uint32_t bits = (uint32_t)(sees >> (t * 32)) >> (g * 4);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[t][i] = bits >> ((i >> 2) * 8 + (i & 3)) & 1u ? s[t][i] : -INFINITY;
+        }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+      top = xor32(top, max_of) * to_log2;
+      if (__any(top > best + kSlack) || __any(best == -INFINITY)) {
+        const float to = fmaxf(best, top);
+        const float keep = to == -INFINITY ? 1.f : pow2(best - to);
+        best = to;
+        sum *= keep;
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t) o[t] *= keep;
+      }
+      const float from = best == -INFINITY ? 0.f : best;
+      u32x4 weights[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int e = (i & 1) * 8 + c * 2;
+          const float w0 = pow2(__builtin_fmaf(s[i >> 1][e], to_log2, -from));
+          const float w1 = pow2(__builtin_fmaf(s[i >> 1][e + 1], to_log2, -from));
+          sum += w0 + w1;
+          weights[i][c] = Q::pack(w0, w1);
+        }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // lane l of 16 gives the address of elements 4 (l % 4) .. + 3 of key l / 4, and gets
+        // element l of four keys
+        const int key = i * 16 + g * 4 + ((lane & 15) >> 2), col = (lane & 16) + (lane & 3) * 4;
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t) {
+          const uint16_t *at = &values[key * kValueRow + t * 32 + col];
+          u32x4 a = transposed(at, at + 8 * kValueRow);
+          if (!whole && __any(any_not_finite4<Q>(a))) {
+            // a weight of 0 keeps a value out of a row, unless it is NaN or inf: those go in apart
+            const uint32_t bits = (uint32_t)(sees >> (i * 16)) >> (g * 4);
+            u32x4 seen;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const int e = (c >> 1) * 8 + (c & 1) * 2;
+              seen[c] = Q::pack((float)(bits >> e & 1u), (float)(bits >> (e + 1) & 1u));
+            }
+            o[t] += not_finite_part32<Q>(a, seen);
+            a = finite_only<Q>(a);
+          }
+          o[t] = Q::mfma32(a, weights[i], o[t]);
+        }
+      }
+    }
+    if (more) put(x + 1);
+    __syncthreads();
+  }
+
+  sum = xor32(sum, sum_of);
+  if ((uint32_t)wave * 32 + m >= tile.rows) return;
+  const bool divided = parts > 1;
+  const uint64_t t_out = (uint64_t)(w.r.start + token);
+  const float vs = p.value_scale ? p.value_scale[head] : 1.f;
+  const float norm = divided ? 1.f : sum != 0.f ? vs / sum : 0.f;
+  const uint64_t slot = ((uint64_t)w.slot * p.kv_heads + head) * kManyRows + wave * 32 + m;
+#pragma unroll
+  for (int t = 0; t < kSteps; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t d = t * 32 + i * 8 + g * 4;
+      if (d >= p.D) continue;
+      const f32x4 y = {o[t][i * 4] * norm, o[t][i * 4 + 1] * norm, o[t][i * 4 + 2] * norm, o[t][i * 4 + 3] * norm};
+      if (divided)
+        *reinterpret_cast<f32x4 *>(p.parts + slot * p.D + d) = y;
+      else
+        *reinterpret_cast<u32x2 *>(p.out + t_out * p.out_stride + (uint64_t)qhead * p.D + d) =
+            u32x2{Q::pack(y.x, y.y), Q::pack(y.z, y.w)};
+    }
+  if (g == 0) {
+    if (divided) {
+      float *ml = p.parts + (uint64_t)p.part_slots * p.kv_heads * kManyRows * p.D + slot * 2;
+      ml[0] = best;
+      ml[1] = sum;
+    } else if (p.lse) {
+      p.lse[t_out * p.heads + qhead] = sum != 0.f ? (best + __log2f(sum)) * kLn2 : -INFINITY;
+    }
+  }
+}
+
+}  // namespace gorio

@@ -244,6 +244,14 @@ def test_attend_masks(torch, type, cache, news, opts):
     holds(torch, a, call(torch, a, max_new=max(news)))
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1.5])
+@pytest.mark.parametrize("news", [[1, 4], [50, 30]])
+def test_attend_scales(torch, news, scale):
+    """A factor of 0 (the mean of what is seen), a negative one, one above 1."""
+    a = setup(torch, 17, "f16", "f16", 4, 2, 64, 16, news, [150, 130], scale=scale, window=60)
+    holds(torch, a, call(torch, a))
+
+
 @pytest.mark.parametrize("news", [[1, 1], [50, 3]])
 def test_attend_table_narrower_than_the_length(torch, news):
     a = setup(torch, 5, "bf16", "bf16", 4, 2, 64, 16, news, [150, 130], width=3)
