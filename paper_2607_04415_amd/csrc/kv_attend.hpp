@@ -315,12 +315,24 @@ __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 // 2^x; -inf gives 0.
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// cap * tanh(x / cap) for x = s: with e = 2^(-2 |x / cap| log2 e), tanh = (1 - e) / (1 + e).
-// 1 - e is exact to 2^-24 of 1, so the result to about 2^-23 of the cap.
-__device__ __forceinline__ float capped(float s, float cap, float by) {  // by = -2 log2 e / cap
-  const float e = pow2(fabsf(s) * by);
-  return copysignf(cap * ((1.f - e) * __builtin_amdgcn_rcpf(1.f + e)), s);
-}
+// Scores that are capped or biased, in log2: products x -> x * factor, or
+// cap tanh(x scale / cap) log2 e, less slope * distance * log2 e.  With
+// E = 2^(2 x scale / cap log2 e), tanh = 1 - 2 / (1 + E), which is right at
+// both ends of E's range too; the quotient is below 1 and good to 2^-23, so the
+// result to about 2^-22 of the cap.
+struct ScoreChange {
+  float factor, cap, twice, by, slope;
+  __device__ __forceinline__ ScoreChange(float scale, float cap_, float slope_)
+      : factor(scale * kLog2e), cap(cap_ * kLog2e), twice(-2.f * cap_ * kLog2e),
+        by(cap_ > 0.f ? 2.f * kLog2e * scale / cap_ : 0.f), slope(-slope_ * kLog2e) {}
+  __device__ __forceinline__ float capped(float x) const {
+    return __builtin_fmaf(twice, __builtin_amdgcn_rcpf(1.f + pow2(x * by)), cap);
+  }
+  // y less the bias at this distance
+  __device__ __forceinline__ float biased(float y, float distance) const {
+    return __builtin_fmaf(slope, fabsf(distance), y);
+  }
+};
 
 // Values that are NaN or inf, two 16-bit elements a word.
 template <typename Q>
@@ -363,17 +375,6 @@ __device__ __forceinline__ u32x4 sign_ones(u32x4 a, bool negative) {
 }
 __device__ __forceinline__ float not_finite_sum(float up, float down) {
   return (up > 0.f ? INFINITY : 0.f) + (down > 0.f ? -INFINITY : 0.f);
-}
-template <typename Q>
-__device__ __forceinline__ f32x16 not_finite_part32(u32x4 a, u32x4 seen) {
-  f32x16 up, down;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) up[i] = down[i] = 0.f;
-  up = Q::mfma32(sign_ones<Q>(a, false), seen, up);
-  down = Q::mfma32(sign_ones<Q>(a, true), seen, down);
-#pragma unroll
-  for (int i = 0; i < 16; ++i) up[i] = not_finite_sum(up[i], down[i]);
-  return up;
 }
 template <typename Q>
 __device__ __forceinline__ f32x4 not_finite_part(u32x4 a, u32x4 seen) {

@@ -73,9 +73,8 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
     }
   }
   const float scale = p.scale * (p.key_scale ? p.key_scale[head] : 1.f);
-  const float to_log2 = kMore ? kLog2e : scale * kLog2e;
-  const float slope = kMore && p.slopes ? p.slopes[qhead] : 0.f;
-  const float cap = p.cap, cap_by = cap > 0.f ? -2.f * kLog2e / cap : 0.f;
+  const float to_log2 = scale * kLog2e;
+  const ScoreChange change(scale, p.cap, kMore && p.slopes ? p.slopes[qhead] : 0.f);
 
   float best = -INFINITY, sum = 0.f;
   f32x4 o[kHalves * 8];
@@ -152,12 +151,12 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
     for (int i = 0; i < 8; ++i) {
       float y = s2[i >> 2][i & 3];
       if constexpr (kMore) {
-        y *= scale;
-        if (cap > 0.f) y = capped(y, cap, cap_by);
-        const int32_t j = j0 + (i >> 2) * 16 + g * 4 + (i & 3);
-        y -= slope * fabsf((float)(pos - j));
+        y = p.cap > 0.f ? change.capped(y) : y * to_log2;
+        if (p.slopes) y = change.biased(y, (float)(pos - j0 - g * 4) - (float)((i >> 2) * 16 + (i & 3)));
+      } else {
+        y *= to_log2;
       }
-      e[i] = y * to_log2;
+      e[i] = y;
     }
     // all rows see all of these keys, or each row is asked for each key
     const bool whole = there_now == 0xFFFFFFFFu &&

@@ -54,6 +54,11 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
   __shared__ __align__(16) uint16_t s_v[2][kManyBlock * kValueRow];
   __shared__ uint64_t s_row[2][2][kManyBlock];  // turn, keys or values
   __shared__ uint64_t s_there[4];
+  // Values that are NaN or inf in a block that not all rows see: a weight of 0 would not keep
+  // them out of a row.  They are 0 in s_v; here are the keys that have one at an element,
+  // +inf (or NaN) and -inf (or NaN).
+  __shared__ uint64_t s_odd[2][kDim];
+  __shared__ uint32_t s_any_odd[2][kManyWaves];  // turn, wave that found one
 
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
@@ -95,8 +100,7 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
       q[s] ^= flip;
     }
   }
-  const float slope = kMore && p.slopes ? p.slopes[qhead] : 0.f;
-  const float cap = p.cap, cap_by = cap > 0.f ? -2.f * kLog2e / cap : 0.f;
+  const ScoreChange change(scale, p.cap, kMore && p.slopes ? p.slopes[qhead] : 0.f);
 
   // Where block x's keys lie: threads 0..63 look up a key each ...
   auto look_up = [&](int32_t x) {
@@ -123,13 +127,46 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
         stage[kv][i] = *reinterpret_cast<const Raw *>(at && d < p.D ? at + d * kElem : zeros);
       }
   };
+  // every row of the tile sees every key of block x
+  auto all_see = [&](int32_t x) {
+    const int32_t j0 = range.block(x) * kManyBlock;
+    return s_there[x & 3] == ~0ull && ((j0 + kManyBlock - 1 <= tile.first && (int64_t)tile.last - j0 < p.window) ||
+                                       j0 + kManyBlock <= w.r.prefix);
+  };
+  auto set_apart = [&](u32x4 v, uint32_t key, uint32_t d) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t x = v[i >> 1] >> (i & 1) * 16 & 0xFFFFu, size = x & 0x7FFFu, inf = Q::kF16 ? 0x7C00u : 0x7F80u;
+      if (size > inf || x == inf) atomicOr((unsigned long long *)&s_odd[0][d + i], 1ull << key);
+      if (size > inf || x == (inf | 0x8000u)) atomicOr((unsigned long long *)&s_odd[1][d + i], 1ull << key);
+    }
+  };
   auto put = [&](int32_t x) {
+    const bool careful = !all_see(x);
+    uint32_t odd = 0;
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
       const uint32_t piece = i * kManyThreads + threadIdx.x, key = piece / kChunks, d = piece % kChunks * 8;
       *reinterpret_cast<u32x4 *>(&s_k[x & 1][key * kKeyRow + d]) = widened<Q>(stage[0][i]);
-      *reinterpret_cast<u32x4 *>(&s_v[x & 1][key * kValueRow + d]) = widened<Q>(stage[1][i]);
+      u32x4 v = widened<Q>(stage[1][i]);
+      if (careful && any_not_finite4<Q>(v)) {
+        set_apart(v, key, d);
+        v = finite_only<Q>(v);
+        odd = 1;
+      }
+      *reinterpret_cast<u32x4 *>(&s_v[x & 1][key * kValueRow + d]) = v;
     }
+    if (careful) {
+      odd = __any(odd);
+      if (lane == 0) s_any_odd[x & 1][wave] = odd;
+    }
+  };
+  // block x, which not all rows see, holds such values
+  auto is_odd = [&](int32_t x) {
+    uint32_t odd = 0;
+#pragma unroll
+    for (int i = 0; i < kManyWaves; ++i) odd |= s_any_odd[x & 1][i];
+    return odd != 0;
   };
 
   float best = -INFINITY, sum = 0.f;  // best: of scores in log2, as last rescaled to
@@ -139,6 +176,91 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
 
+  // One block's products: `sees` are the keys that this lane's query sees, all of them if kWhole.
+  auto block = [&](int32_t x, int32_t j0, uint64_t sees, bool odd, auto whole) {
+    constexpr bool kWhole = decltype(whole)::value;
+    const uint16_t *keys = s_k[x & 1], *values = s_v[x & 1];
+    f32x16 s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kSteps * 2; ++k)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        s[t] = Q::mfma32(*reinterpret_cast<const u32x4 *>(&keys[(t * 32 + m) * kKeyRow + k * 16 + g * 8]), q[k], s[t]);
+    if constexpr (kMore) {
+      if (p.cap > 0.f) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = change.capped(s[i >> 4][i & 15]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] *= change.factor;
+      }
+      if (p.slopes) {
+        const float distance = (float)(pos - j0 - g * 4);
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          s[i >> 4][i & 15] = change.biased(s[i >> 4][i & 15],
+                                            distance - (float)((i >> 4) * 32 + ((i & 15) >> 2) * 8 + (i & 3)));
+      }
+    }
+    const float to_log2 = kMore ? 1.f : factor;
+    if constexpr (!kWhole) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t bits = (uint32_t)(sees >> (t * 32)) >> (g * 4);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[t][i] = bits >> ((i >> 2) * 8 + (i & 3)) & 1u ? s[t][i] : -INFINITY;
+      }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+    top = xor32(top, max_of) * to_log2;
+    if (__any(top > best + kSlack) || __any(best == -INFINITY)) {
+      const float to = fmaxf(best, top);
+      const float keep = to == -INFINITY ? 1.f : pow2(best - to);
+      best = to;
+      sum *= keep;
+#pragma unroll
+      for (int t = 0; t < kSteps; ++t) o[t] *= keep;
+    }
+    const float from = best == -INFINITY ? 0.f : best;
+    u32x4 weights[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int e = (i & 1) * 8 + c * 2;
+        const float w0 = pow2(__builtin_fmaf(s[i >> 1][e], to_log2, -from));
+        const float w1 = pow2(__builtin_fmaf(s[i >> 1][e + 1], to_log2, -from));
+        sum += w0 + w1;
+        weights[i][c] = Q::pack(w0, w1);
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < kSteps; ++t) {
+        // sixteen keys' values at elements 32 t + m
+        const uint16_t *at = &values[(i * 16 + g * 4 + ((lane & 15) >> 2)) * kValueRow + t * 32 + (lane & 16) + (lane & 3) * 4];
+        o[t] = Q::mfma32(transposed(at, at + 8 * kValueRow), weights[i], o[t]);
+      }
+    if constexpr (!kWhole) {
+      if (odd) {
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t d = t * 32 + (i >> 2) * 8 + g * 4 + (i & 3);
+            o[t][i] += ((s_odd[0][d] & sees) ? INFINITY : 0.f) + ((s_odd[1][d] & sees) ? -INFINITY : 0.f);
+          }
+      }
+    }
+  };
+
+  for (uint32_t i = threadIdx.x; i < 2 * kDim; i += kManyThreads) (&s_odd[0][0])[i] = 0;
   KeyPlace ahead{-1, 0};
   if (wave == 0) {
     hand_out(look_up(x0), x0);
@@ -158,91 +280,22 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
     }
     const int32_t j0 = range.block(x) * kManyBlock;
     const uint64_t there = s_there[x & 3];
-    const bool seen_any = has_rows && ((j0 <= last && (int64_t)j0 + kManyBlock - 1 > (int64_t)first - p.window) || j0 < w.r.prefix);
-    if (seen_any) {
-      const uint16_t *keys = s_k[x & 1], *values = s_v[x & 1];
-      f32x16 s[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
-#pragma unroll
-      for (int k = 0; k < kSteps * 2; ++k)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-          s[t] = Q::mfma32(*reinterpret_cast<const u32x4 *>(&keys[(t * 32 + m) * kKeyRow + k * 16 + g * 8]), q[k], s[t]);
-      if constexpr (kMore) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float y = s[t][i] * scale;
-            if (cap > 0.f) y = capped(y, cap, cap_by);
-            const int32_t j = j0 + t * 32 + (i >> 2) * 8 + g * 4 + (i & 3);
-            s[t][i] = (y - slope * fabsf((float)(pos - j))) * kLog2e;
-          }
+    const bool odd = !all_see(x) && is_odd(x);  // all waves agree
+    const bool whole = !odd && there == ~0ull &&
+                       ((j0 + kManyBlock - 1 <= first && (int64_t)last - j0 < p.window) || j0 + kManyBlock <= w.r.prefix);
+    const bool any = (j0 <= last && (int64_t)j0 + kManyBlock - 1 > (int64_t)first - p.window) || j0 < w.r.prefix;
+    if (has_rows && any) {
+      if (whole) {
+        block(x, j0, ~0ull, false, std::true_type{});
+      } else {
+        block(x, j0, there & ((low_bits(pos - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(w.r.prefix - j0)),
+              odd, std::false_type{});
       }
-      const float to_log2 = kMore ? 1.f : factor;
-      const bool whole = there == ~0ull && ((j0 + kManyBlock - 1 <= first && (int64_t)last - j0 < p.window) ||
-                                            j0 + kManyBlock <= w.r.prefix);
-      uint64_t sees = ~0ull;
-      if (!whole) {
-        sees = there & ((low_bits(pos - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(w.r.prefix - j0));
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const uint32_t bits = (uint32_t)(sees >> (t * 32)) >> (g * 4);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[t][i] = bits >> ((i >> 2) * 8 + (i & 3)) & 1u ? s[t][i] : -INFINITY;
-        }
-      }
-      float top = s[0][0];
-#pragma unroll
-      for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
-      top = xor32(top, max_of) * to_log2;
-      if (__any(top > best + kSlack) || __any(best == -INFINITY)) {
-        const float to = fmaxf(best, top);
-        const float keep = to == -INFINITY ? 1.f : pow2(best - to);
-        best = to;
-        sum *= keep;
-#pragma unroll
-        for (int t = 0; t < kSteps; ++t) o[t] *= keep;
-      }
-      const float from = best == -INFINITY ? 0.f : best;
-      u32x4 weights[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int e = (i & 1) * 8 + c * 2;
-          const float w0 = pow2(__builtin_fmaf(s[i >> 1][e], to_log2, -from));
-          const float w1 = pow2(__builtin_fmaf(s[i >> 1][e + 1], to_log2, -from));
-          sum += w0 + w1;
-          weights[i][c] = Q::pack(w0, w1);
-        }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        // lane l of 16 gives the address of elements 4 (l % 4) .. + 3 of key l / 4, and gets
-        // element l of four keys
-        const int key = i * 16 + g * 4 + ((lane & 15) >> 2), col = (lane & 16) + (lane & 3) * 4;
-#pragma unroll
-        for (int t = 0; t < kSteps; ++t) {
-          const uint16_t *at = &values[key * kValueRow + t * 32 + col];
-          u32x4 a = transposed(at, at + 8 * kValueRow);
-          if (!whole && __any(any_not_finite4<Q>(a))) {
-            // a weight of 0 keeps a value out of a row, unless it is NaN or inf: those go in apart
-            const uint32_t bits = (uint32_t)(sees >> (i * 16)) >> (g * 4);
-            u32x4 seen;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const int e = (c >> 1) * 8 + (c & 1) * 2;
-              seen[c] = Q::pack((float)(bits >> e & 1u), (float)(bits >> (e + 1) & 1u));
-            }
-            o[t] += not_finite_part32<Q>(a, seen);
-            a = finite_only<Q>(a);
-          }
-          o[t] = Q::mfma32(a, weights[i], o[t]);
-        }
-      }
+    }
+    if (odd) {  // the next such block starts with no keys
+      __syncthreads();
+      for (uint32_t i = threadIdx.x; i < 2 * kDim; i += kManyThreads) (&s_odd[0][0])[i] = 0;
+      __syncthreads();
     }
     if (more) put(x + 1);
     __syncthreads();
