@@ -78,13 +78,19 @@ __device__ __forceinline__ u32x4 widened(u32x2 r) {
                Q::template widen<true>(r.y)};
 }
 
+// LDS by its 32-bit address: what is added to one as a constant goes into the instruction.
+typedef __attribute__((address_space(3))) uint8_t LdsBytes;
+template <typename T>
+__device__ __forceinline__ __attribute__((address_space(3))) T *lds_at(uint32_t address) {
+  return (__attribute__((address_space(3))) T *)(uintptr_t)address;
+}
+
 // Two transposing LDS reads.  In each, lane l of 16 names the 8 bytes that hold
 // elements 4 (l % 4) .. + 3 of row l / 4, and gets element l of the four rows.
-__device__ __forceinline__ u32x4 transposed(const uint16_t *a, const uint16_t *b) {
+__device__ __forceinline__ u32x4 transposed(uint32_t a, uint32_t b) {
   typedef short s16x4 __attribute__((ext_vector_type(4)));
-  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-  const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)a));
-  const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)b));
+  const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(a)));
+  const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(b)));
   return u32x4{x.x, x.y, y.x, y.y};
 }
 
@@ -257,7 +263,18 @@ __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item)
     __syncthreads();
   }
   if (!s_found) return false;
-  item = s_item;
+  // the same for all: into scalar registers
+  auto one = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
+  item.request = one(s_item.request);
+  item.tile = one(s_item.tile);
+  item.part = one(s_item.part);
+  item.parts = one(s_item.parts);
+  item.slot = one(s_item.slot);
+  item.c = one(s_item.c);
+  item.r.start = (int32_t)one((uint32_t)s_item.r.start);
+  item.r.added = (int32_t)one((uint32_t)s_item.r.added);
+  item.r.len = (int32_t)one((uint32_t)s_item.r.len);
+  item.r.prefix = (int32_t)one((uint32_t)s_item.r.prefix);
   return true;
 }
 
@@ -279,26 +296,29 @@ __device__ __forceinline__ Tile tile_of(const AttendParams &p, const WorkItem &w
   return t;
 }
 
-// One lane's view of a key: its row in memory, or none.
-struct KeyPlace {
-  int32_t page;  // -1: not there
+// One lane's look at a key's table entry.  What it loads is judged where it is needed, a block
+// later: a comparison beside the load would wait for it, and for every load issued before.
+struct KeyLook {
+  int32_t page, fill;  // as the tables have them
   uint32_t place;
+  bool seen;  // by some row of the tile: whatever other keys' values hold does not reach them
 };
 
-__device__ __forceinline__ KeyPlace key_place(const AttendParams &p, const WorkItem &w, const Tile &t, int32_t j,
-                                              int32_t end) {
-  KeyPlace k{-1, 0};
-  const uint32_t b = w.request;
-  // a key that no row of the tile sees is not there: whatever its value holds does not reach them
-  if (j < end && ((j <= t.last && (int64_t)t.first - j < p.window) || j < w.r.prefix)) {
-    const uint32_t e = fastdiv((uint32_t)j, p.page_tokens);
-    const uint64_t at = (uint64_t)b * p.width + e;
-    k.place = (uint32_t)j - e * p.page_tokens.d;
-    const int32_t page = p.tables[at];
-    if ((uint32_t)page < p.num_pages) k.page = page;
-    if (p.fills && (int32_t)k.place >= p.fills[at]) k.page = -1;
-  }
+__device__ __forceinline__ KeyLook key_look(const AttendParams &p, const WorkItem &w, const Tile &t, bool in_part,
+                                            int32_t j, int32_t end) {
+  KeyLook k;
+  const bool near = (j <= t.last) & ((int64_t)t.first - j < (int64_t)p.window);
+  k.seen = in_part & (j < end) & (near | (j < w.r.prefix));
+  const uint32_t at = (uint32_t)(k.seen ? j : 0), e = fastdiv(at, p.page_tokens);
+  k.place = at - e * p.page_tokens.d;
+  const uint64_t entry = (uint64_t)w.request * p.width + e;
+  k.page = p.tables[entry];
+  k.fill = p.fills ? p.fills[entry] : 0x7FFFFFFF;
   return k;
+}
+
+__device__ __forceinline__ bool key_there(const AttendParams &p, const KeyLook &k) {
+  return k.seen & ((uint32_t)k.page < p.num_pages) & ((int32_t)k.place < k.fill);
 }
 
 __device__ __forceinline__ float xor32(float x, float (*op)(float, float)) {

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
   if (w.part >= parts) return;
   const int32_t x_end = min((int64_t)range.count, (int64_t)(w.part + 1) * w.c);
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
   const uint64_t zeros = (uint64_t)(uintptr_t)kv_zeros;
   constexpr int kElem = k8 ? 1 : 2;
@@ -82,21 +82,20 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
   for (int t = 0; t < kHalves * 8; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   // Rows of block x into LDS, and its keys' bits: lanes 0..31 a key each.
-  auto place_of = [&](int32_t x) {
-    return key_place(p, w, tile, x < x_end && lane < kFewBlock ? range.block(x) * kFewBlock + lane : range.end,
-                     range.end);
+  auto place_of = [&](int32_t x) __attribute__((always_inline)) {
+    return key_look(p, w, tile, (x < x_end) & (lane < kFewBlock), range.block(x) * kFewBlock + (lane & 31), range.end);
   };
-  auto hand_out = [&](const KeyPlace &k, int turn) -> uint32_t {
-    const bool there = k.page >= 0;
+  auto hand_out = [&](const KeyLook &k, int turn) __attribute__((always_inline)) -> uint32_t {
+    const bool there = key_there(p, k);
     if (lane < kFewBlock) {
       const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
       s_row[wave][turn][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : 0;
       s_row[wave][turn][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : 0;
     }
     wave_lds_order();
-    return (uint32_t)__ballot(there && lane < kFewBlock);
+    return (uint32_t)__ballot(there);
   };
-  auto load_keys = [&](Raw (&k)[2][kSteps], int turn) {
+  auto load_keys = [&](Raw (&k)[2][kSteps], int turn) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint64_t row = s_row[wave][turn][0][i * 16 + m];
@@ -108,7 +107,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
       }
     }
   };
-  auto load_values = [&](Raw (&v)[8], int half, int turn) {
+  auto load_values = [&](Raw (&v)[8], int half, int turn) __attribute__((always_inline)) {
     const uint32_t d = half * 128 + m * 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -122,22 +121,22 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
   Raw k[2][kSteps];
   uint32_t there = hand_out(place_of(x), 0);
   load_keys(k, 0);
-  KeyPlace next = place_of(x + kFewWaves);
+  KeyLook next = place_of(x + kFewWaves);
   for (; x < x_end; x += kFewWaves) {
     const int32_t j0 = range.block(x) * kFewBlock;
+    const uint32_t there_now = there;
+    there = hand_out(next, turn ^ 1);
+    next = place_of(x + 2 * kFewWaves);
     Raw v[kHalves][8];
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) load_values(v[h], h, turn);
-    // the next block's keys and, one further, its places are on their way during this one's products
+    // the next block's keys are on their way during this one's products
     u32x4 kw[2][kSteps];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) kw[i][s] = widened<Q>(k[i][s]);
-    const uint32_t there_now = there;
-    there = hand_out(next, turn ^ 1);
     load_keys(k, turn ^ 1);
-    next = place_of(x + 2 * kFewWaves);
 
     f32x4 s2[2];
 #pragma unroll
@@ -300,7 +299,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
   if (parts <= 1) return;  // written by its one part
   const float *ml0 = p.parts + (uint64_t)p.part_slots * p.kv_heads * kRows * p.D;
   for (uint32_t row = threadIdx.x >> 4; row < tile.rows; row += 16) {
-    auto slot = [&](uint32_t i) { return ((uint64_t)(w.slot + i) * p.kv_heads + head) * kRows + row; };
+    auto slot = [&](uint32_t i) __attribute__((always_inline)) { return ((uint64_t)(w.slot + i) * p.kv_heads + head) * kRows + row; };
     float most = -INFINITY;
     for (uint32_t i = 0; i < parts; ++i) most = fmaxf(most, ml0[slot(i) * 2]);
     const float from = most == -INFINITY ? 0.f : most;

@@ -43,22 +43,24 @@ __device__ __forceinline__ uint64_t low_bits(int32_t n) {
 // kSteps: D <= 32 kSteps.  k8: pages of 8-bit values.  kMore: scores are capped or biased.
 template <typename Q, bool k8, int kSteps, bool kMore>
 __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(AttendParams p) {
-  constexpr int kDim = kSteps * 32, kChunks = kDim / 8;
-  constexpr int kKeyRow = kDim + 8;                                                  // elements
-  constexpr int kValueRow = (kDim * 2) % 256 == 192 ? kDim : kDim + 32;
-  constexpr int kPasses = kManyBlock * kChunks / kManyThreads;                       // 16-byte pieces a thread
+  constexpr int kDim = kSteps * 32, kChunks = kDim / 8;                              // 16-byte pieces of a row
+  constexpr int kPasses = kManyBlock * kChunks / kManyThreads;                       // pieces a thread
   static_assert(kPasses * kManyThreads == kManyBlock * kChunks, "pieces divide");
+  constexpr bool kTurned = (kChunks & (kChunks - 1)) == 0, kDirect = kTurned && !k8;  // see `turned`
+  constexpr int kKeyRow = kTurned ? kDim : kDim + 8;                                 // elements
+  constexpr int kValueRow = kDim;
+  static_assert(kTurned || (kDim * 2) % 256 == 192, "rows of values fall on different banks");
   constexpr int kElem = k8 ? 1 : 2;
   typedef typename std::conditional<k8, u32x2, u32x4>::type Raw;
-  __shared__ __align__(16) uint16_t s_k[2][kManyBlock * kKeyRow];
-  __shared__ __align__(16) uint16_t s_v[2][kManyBlock * kValueRow];
-  __shared__ uint64_t s_row[2][2][kManyBlock];  // turn, keys or values
+  constexpr uint32_t kKeyBytes = kManyBlock * kKeyRow * 2, kValueBytes = kManyBlock * kValueRow * 2;
+  __shared__ __align__(1024) uint8_t s_kv[2 * (kKeyBytes + kValueBytes)];  // keys, keys, values, values
+  __shared__ uint64_t s_row[4][2][kManyBlock];  // block, keys or values
   __shared__ uint64_t s_there[4];
   // Values that are NaN or inf in a block that not all rows see: a weight of 0 would not keep
-  // them out of a row.  They are 0 in s_v; here are the keys that have one at an element,
+  // them out of a row.  They are 0 in s_kv; here are the keys that have one at an element,
   // +inf (or NaN) and -inf (or NaN).
   __shared__ uint64_t s_odd[2][kDim];
-  __shared__ uint32_t s_any_odd[2][kManyWaves];  // turn, wave that found one
+  __shared__ uint32_t s_any_odd[kManyWaves];
 
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
@@ -70,7 +72,7 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
   const int32_t x0 = (int32_t)(w.part * w.c);
   const int32_t x_end = (int32_t)min((int64_t)range.count, (int64_t)x0 + w.c);
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 31, g = lane >> 5;
   const uint64_t zeros = (uint64_t)(uintptr_t)kv_zeros;
 
@@ -102,71 +104,87 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
   }
   const ScoreChange change(scale, p.cap, kMore && p.slopes ? p.slopes[qhead] : 0.f);
 
-  // Where block x's keys lie: threads 0..63 look up a key each ...
-  auto look_up = [&](int32_t x) {
-    const int32_t j = x < x_end ? range.block(x) * kManyBlock + lane : range.end;
-    return key_place(p, w, tile, j, range.end);
+  // Where block x's keys lie: wave 0 looks up a key a lane ...
+  auto look_up = [&](int32_t x) __attribute__((always_inline)) {
+    return key_look(p, w, tile, (x >= x0) & (x < x_end), range.block(x) * kManyBlock + lane, range.end);
   };
-  // ... and hand its rows to all.
-  auto hand_out = [&](const KeyPlace &k, int32_t x) {
-    const bool there = k.page >= 0;
+  // ... and hands its rows to all.
+  auto hand_out = [&](const KeyLook &k, int32_t x) __attribute__((always_inline)) {
+    const bool there = key_there(p, k);
     const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
-    s_row[x & 1][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : 0;
-    s_row[x & 1][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : 0;
+    s_row[x & 3][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : 0;
+    s_row[x & 3][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : 0;
     const uint64_t bits = __ballot(there);
     if (lane == 0) s_there[x & 3] = bits;
   };
-  Raw stage[2][kPasses];
-  auto load = [&](int32_t x) {
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-      for (int i = 0; i < kPasses; ++i) {
-        const uint32_t piece = i * kManyThreads + threadIdx.x, key = piece / kChunks, d = piece % kChunks * 8;
-        const uint64_t at = s_row[x & 1][kv][key];
-        stage[kv][i] = *reinterpret_cast<const Raw *>(at && d < p.D ? at + d * kElem : zeros);
-      }
-  };
-  // every row of the tile sees every key of block x
-  auto all_see = [&](int32_t x) {
+  // Every row of the tile sees every key of block x that is there, by its position.
+  auto all_see = [&](int32_t x) __attribute__((always_inline)) {
     const int32_t j0 = range.block(x) * kManyBlock;
-    return s_there[x & 3] == ~0ull && ((j0 + kManyBlock - 1 <= tile.first && (int64_t)tile.last - j0 < p.window) ||
-                                       j0 + kManyBlock <= w.r.prefix);
+    return (j0 + kManyBlock - 1 <= tile.first && (int64_t)tile.last - j0 < p.window) || j0 + kManyBlock <= w.r.prefix;
   };
-  auto set_apart = [&](u32x4 v, uint32_t key, uint32_t d) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t x = v[i >> 1] >> (i & 1) * 16 & 0xFFFFu, size = x & 0x7FFFu, inf = Q::kF16 ? 0x7C00u : 0x7F80u;
-      if (size > inf || x == inf) atomicOr((unsigned long long *)&s_odd[0][d + i], 1ull << key);
-      if (size > inf || x == (inf | 0x8000u)) atomicOr((unsigned long long *)&s_odd[1][d + i], 1ull << key);
-    }
+
+  // A thread's pieces of a block.  Straight from memory into LDS, a wave's 64 pieces lie one
+  // after the other there, so the banks are spread by which piece a lane asks for: piece c of
+  // key j lies at c ^ turned(j), which sets 16 neighbouring keys' equal pieces, and 4 keys' 64
+  // bytes, on different banks.
+  auto turned = [](uint32_t key) __attribute__((always_inline)) -> uint32_t {
+    return kChunks == 8 ? (key >> 1 & 1u) << 2 | (key >> 2 & 3u) : (key & 3u) << 2 | (key >> 2 & 3u);
   };
-  auto put = [&](int32_t x) {
-    const bool careful = !all_see(x);
-    uint32_t odd = 0;
+  Raw stage[2][kDirect ? 1 : kPasses];
+  const uint32_t lds = (uint32_t)(uintptr_t)(LdsBytes *)s_kv;
+  constexpr uint32_t kKeys[2] = {0, kKeyBytes}, kValues[2] = {2 * kKeyBytes, 2 * kKeyBytes + kValueBytes};
+  // kv: the values of block x, or keys half a block later: 32.. of block x, ..31 of x + 1.
+  auto load = [&](int32_t x, int kv, uint32_t to) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
-      const uint32_t piece = i * kManyThreads + threadIdx.x, key = piece / kChunks, d = piece % kChunks * 8;
-      *reinterpret_cast<u32x4 *>(&s_k[x & 1][key * kKeyRow + d]) = widened<Q>(stage[0][i]);
-      u32x4 v = widened<Q>(stage[1][i]);
-      if (careful && any_not_finite4<Q>(v)) {
-        set_apart(v, key, d);
-        v = finite_only<Q>(v);
-        odd = 1;
+      const uint32_t piece = (i * kManyWaves + wave) * 64 + lane, key = piece / kChunks;
+      const uint32_t c = piece % kChunks, d = (kDirect ? c ^ turned(key) : c) * 8;
+      const uint64_t row = kv ? s_row[x & 3][1][key] : s_row[(x + (key >> 5)) & 3][0][key ^ 32];
+      const uint64_t at = row && d < p.D ? row + d * kElem : zeros;
+      if constexpr (kDirect) {
+        typedef __attribute__((address_space(1))) const uint32_t global_u32;
+        __builtin_amdgcn_global_load_lds((global_u32 *)at, (LdsBytes *)(uintptr_t)(lds + to + (i * kManyWaves + wave) * 1024),
+                                         16, 0, 0);
+      } else {
+        stage[kv][i] = *reinterpret_cast<const Raw *>(at);
       }
-      *reinterpret_cast<u32x4 *>(&s_v[x & 1][key * kValueRow + d]) = v;
-    }
-    if (careful) {
-      odd = __any(odd);
-      if (lane == 0) s_any_odd[x & 1][wave] = odd;
     }
   };
-  // block x, which not all rows see, holds such values
-  auto is_odd = [&](int32_t x) {
-    uint32_t odd = 0;
+  auto put = [&](int kv, uint32_t to) __attribute__((always_inline)) {
+    if constexpr (!kDirect) {
 #pragma unroll
-    for (int i = 0; i < kManyWaves; ++i) odd |= s_any_odd[x & 1][i];
-    return odd != 0;
+      for (int i = 0; i < kPasses; ++i) {
+        const uint32_t piece = (i * kManyWaves + wave) * 64 + lane, key = piece / kChunks, c = piece % kChunks;
+        *lds_at<u32x4>(lds + to + key * (kv ? kValueRow : kKeyRow) * 2 + (kTurned ? c ^ turned(key) : c) * 16) = widened<Q>(stage[kv][i]);
+      }
+    }
+  };
+  // Takes the NaN and inf out of a block of values in LDS; true if there were any.  All threads.
+  auto set_apart = [&](uint32_t values) __attribute__((always_inline)) -> bool {
+    uint32_t odd = 0;
+#pragma unroll 1
+    for (uint32_t piece = threadIdx.x; piece < kManyBlock * kChunks; piece += kManyThreads) {
+      const uint32_t key = piece / kChunks, c = piece % kChunks;
+      auto at = lds_at<u32x4>(lds + values + key * kValueRow * 2 + (kTurned ? c ^ turned(key) : c) * 16);
+      const u32x4 v = *at;
+      if (!any_not_finite4<Q>(v)) continue;
+      odd = 1;
+      *at = finite_only<Q>(v);
+#pragma unroll 1
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t pair = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
+        const uint32_t x = pair >> (i & 1) * 16 & 0xFFFFu, size = x & 0x7FFFu, inf = Q::kF16 ? 0x7C00u : 0x7F80u;
+        if (size > inf || x == inf) atomicOr((unsigned long long *)&s_odd[0][c * 8 + i], 1ull << key);
+        if (size > inf || x == (inf | 0x8000u)) atomicOr((unsigned long long *)&s_odd[1][c * 8 + i], 1ull << key);
+      }
+    }
+    odd = __any(odd);
+    if (lane == 0) s_any_odd[wave] = odd;
+    __syncthreads();
+    odd = 0;
+#pragma unroll
+    for (int i = 0; i < kManyWaves; ++i) odd |= s_any_odd[i];
+    return __builtin_amdgcn_readfirstlane(odd) != 0;
   };
 
   float best = -INFINITY, sum = 0.f;  // best: of scores in log2, as last rescaled to
@@ -176,50 +194,41 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
 
-  // One block's products: `sees` are the keys that this lane's query sees, all of them if kWhole.
-  auto block = [&](int32_t x, int32_t j0, uint64_t sees, bool odd, auto whole) {
-    constexpr bool kWhole = decltype(whole)::value;
-    const uint16_t *keys = s_k[x & 1], *values = s_v[x & 1];
-    f32x16 s[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
-#pragma unroll
-    for (int k = 0; k < kSteps * 2; ++k)
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        s[t] = Q::mfma32(*reinterpret_cast<const u32x4 *>(&keys[(t * 32 + m) * kKeyRow + k * 16 + g * 8]), q[k], s[t]);
+  // Where this lane reads, in block 0 of each buffer's keys and values: a step of 16 elements
+  // (or 32) turns a bit of the address, or adds to it, and all else is a constant offset.
+  auto beside = [](uint32_t at, uint32_t bytes) __attribute__((always_inline)) { return kTurned ? at ^ bytes : at + bytes; };
+  uint32_t key_at = lds + m * kKeyRow * 2 + (kTurned ? g ^ turned(m) : (uint32_t)g) * 16;
+  uint32_t value_at[2];
+  {
+    const uint32_t key = g * 4 + ((lane & 15) >> 2);
+    const uint32_t c = (lane & 16) >> 3 | (lane & 3) >> 1;  // piece of the 64 bytes of 32 elements
+    value_at[0] = lds + key * kValueRow * 2 + (kTurned ? c ^ turned(key) : c) * 16 + (lane & 1) * 8;
+    value_at[1] = lds + (key + 8) * kValueRow * 2 + (kTurned ? c ^ turned(key + 8) : c) * 16 + (lane & 1) * 8;
+  }
+  const float to_log2 = kMore ? 1.f : factor;
+  auto changed = [&](f32x16 &s, int32_t j0) __attribute__((always_inline)) {
     if constexpr (kMore) {
       if (p.cap > 0.f) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = change.capped(s[i >> 4][i & 15]);
+        for (int i = 0; i < 16; ++i) s[i] = change.capped(s[i]);
       } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] *= change.factor;
+        for (int i = 0; i < 16; ++i) s[i] *= change.factor;
       }
       if (p.slopes) {
         const float distance = (float)(pos - j0 - g * 4);
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-          s[i >> 4][i & 15] = change.biased(s[i >> 4][i & 15],
-                                            distance - (float)((i >> 4) * 32 + ((i & 15) >> 2) * 8 + (i & 3)));
+        for (int i = 0; i < 16; ++i) s[i] = change.biased(s[i], distance - (float)((i >> 2) * 8 + (i & 3)));
       }
     }
-    const float to_log2 = kMore ? 1.f : factor;
-    if constexpr (!kWhole) {
+  };
+  // The running maximum takes in 32 keys' scores; the sums are rescaled to it.
+  auto rescale = [&](const f32x16 &s) __attribute__((always_inline)) {
+    float top = s[0];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const uint32_t bits = (uint32_t)(sees >> (t * 32)) >> (g * 4);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[t][i] = bits >> ((i >> 2) * 8 + (i & 3)) & 1u ? s[t][i] : -INFINITY;
-      }
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = xor32(top, max_of) * to_log2;
-    if (__any(top > best + kSlack) || __any(best == -INFINITY)) {
+    if (__any((top > best + kSlack) | (best == -INFINITY))) {
       const float to = fmaxf(best, top);
       const float keep = to == -INFINITY ? 1.f : pow2(best - to);
       best = to;
@@ -227,78 +236,148 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
 #pragma unroll
       for (int t = 0; t < kSteps; ++t) o[t] *= keep;
     }
+  };
+  // 32 keys' scores to weights and O^T of their values, with the scores of the 32 keys after
+  // them computed beside (S^T from `keys`): a matrix instruction takes as long as eight others,
+  // so the exponentials go between those of S^T, and LDS is read a step ahead of its use.
+  auto both = [&](uint32_t keys, f32x16 &next, uint32_t values, const f32x16 &s) __attribute__((always_inline)) {
+    // held as they are: the addresses made of them would cost registers that Q needs
+    asm volatile("" : "+v"(key_at), "+v"(value_at[0]), "+v"(value_at[1]));
     const float from = best == -INFINITY ? 0.f : best;
-    u32x4 weights[4];
+    u32x4 weights[2], kf[2], vf[2][2];
+    auto read_keys = [&](int k) __attribute__((always_inline)) { kf[k & 1] = *lds_at<u32x4>(beside(key_at, k * 32) + keys); };
+    auto read_values = [&](int c) __attribute__((always_inline)) {  // two of sixteen keys' values at elements 32 t + m, keys outside
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int f = 0; f < 2; ++f) {
+        const int i = (c * 2 + f) / kSteps, t = (c * 2 + f) % kSteps;
+        vf[c & 1][f] = transposed(beside(value_at[0], t * 64) + values + i * 16 * kValueRow * 2,
+                                  beside(value_at[1], t * 64) + values + i * 16 * kValueRow * 2);
+      }
+    };
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int e = (i & 1) * 8 + c * 2;
-        const float w0 = pow2(__builtin_fmaf(s[i >> 1][e], to_log2, -from));
-        const float w1 = pow2(__builtin_fmaf(s[i >> 1][e + 1], to_log2, -from));
+    for (int i = 0; i < 16; ++i) next[i] = 0.f;
+    read_keys(0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < kSteps * 2; ++k) {
+      if (k + 1 < kSteps * 2) read_keys(k + 1);
+      else read_values(0);
+      next = Q::mfma32(kf[k & 1], q[k], next);
+#pragma unroll
+      for (int e = 8 * k / (kSteps * 2); e < 8 * (k + 1) / (kSteps * 2); ++e) {  // pairs of scores
+        const float w0 = pow2(__builtin_fmaf(s[e * 2], to_log2, -from));
+        const float w1 = pow2(__builtin_fmaf(s[e * 2 + 1], to_log2, -from));
         sum += w0 + w1;
-        weights[i][c] = Q::pack(w0, w1);
+        weights[e >> 2][e & 3] = Q::pack(w0, w1);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int c = 0; c < kSteps; ++c) {
+      if (c + 1 < kSteps) read_values(c + 1);
 #pragma unroll
-      for (int t = 0; t < kSteps; ++t) {
-        // sixteen keys' values at elements 32 t + m
-        const uint16_t *at = &values[(i * 16 + g * 4 + ((lane & 15) >> 2)) * kValueRow + t * 32 + (lane & 16) + (lane & 3) * 4];
-        o[t] = Q::mfma32(transposed(at, at + 8 * kValueRow), weights[i], o[t]);
+      for (int f = 0; f < 2; ++f) {
+        const int i = (c * 2 + f) / kSteps, t = (c * 2 + f) % kSteps;
+        o[t] = Q::mfma32(vf[c & 1][f], weights[i], o[t]);
       }
-    if constexpr (!kWhole) {
-      if (odd) {
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  // Block x, the scores of whose first 32 keys are in `now`, up to those of block x + 1.  The
+  // buffers alternate, and two steps make a round, so that which one is read is known when this
+  // is compiled.
+  constexpr uint32_t kHalfKeys = 32 * kKeyRow * 2, kHalfValues = 32 * kValueRow * 2;
+  f32x16 now, next;
+  KeyLook ahead{};
+  auto step = [&](int32_t x, uint32_t k_now, uint32_t k_next, uint32_t v_now, uint32_t v_next) __attribute__((always_inline)) {
+    const bool more = x + 1 < x_end;
+    if (wave == 0) {
+      hand_out(ahead, x + 3);
+      ahead = look_up(x + 4);
+    }
+    if (more) {
+      load(x + 1, 0, k_next);
+      load(x + 1, 1, v_next);
+    }
+    const int32_t j0 = range.block(x) * kManyBlock;
+    const uint64_t bits = s_there[x & 3];  // the same for all
+    const uint64_t there = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32 |
+                           (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bits);
+    bool odd = false;
+    if (__builtin_expect(!all_see(x), 0)) odd = set_apart(v_now);
+    const bool near = (j0 + kManyBlock - 1 <= first && (int64_t)last - j0 < p.window) || j0 + kManyBlock <= w.r.prefix;
+    const bool any = (j0 <= last && (int64_t)j0 + kManyBlock - 1 > (int64_t)first - p.window) || j0 < w.r.prefix;
+    const bool masked = !near | odd | (there != ~0ull);
+    uint64_t sees = ~0ull;
+    if (masked)
+      sees = !any ? 0 : there & ((low_bits(pos - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(w.r.prefix - j0));
+    auto mask = [&](f32x16 &s, uint32_t seen) __attribute__((always_inline)) {
+      if (masked) {
+        seen >>= g * 4;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = seen >> ((i >> 2) * 8 + (i & 3)) & 1u ? s[i] : -INFINITY;
+      }
+    };
+    if (has_rows) {
+      changed(now, j0);
+      mask(now, (uint32_t)sees);
+      rescale(now);
+      both(k_now, next, v_now, now);
+      changed(next, j0 + 32);
+      mask(next, (uint32_t)(sees >> 32));
+      rescale(next);
+      both(k_now + kHalfKeys, now, v_now + kHalfValues, next);
+      if (__builtin_expect(odd, 0)) {
 #pragma unroll
         for (int t = 0; t < kSteps; ++t)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const uint32_t d = t * 32 + (i >> 2) * 8 + g * 4 + (i & 3);
             o[t][i] += ((s_odd[0][d] & sees) ? INFINITY : 0.f) + ((s_odd[1][d] & sees) ? -INFINITY : 0.f);
+            __builtin_amdgcn_sched_barrier(0);
           }
-      }
-    }
-  };
-
-  for (uint32_t i = threadIdx.x; i < 2 * kDim; i += kManyThreads) (&s_odd[0][0])[i] = 0;
-  KeyPlace ahead{-1, 0};
-  if (wave == 0) {
-    hand_out(look_up(x0), x0);
-    hand_out(look_up(x0 + 1), x0 + 1);
-    ahead = look_up(x0 + 2);
-  }
-  __syncthreads();
-  load(x0);
-  put(x0);
-  __syncthreads();
-  for (int32_t x = x0; x < x_end; ++x) {
-    const bool more = x + 1 < x_end;
-    if (more) load(x + 1);
-    if (wave == 0) {
-      hand_out(ahead, x + 2);
-      ahead = look_up(x + 3);
-    }
-    const int32_t j0 = range.block(x) * kManyBlock;
-    const uint64_t there = s_there[x & 3];
-    const bool odd = !all_see(x) && is_odd(x);  // all waves agree
-    const bool whole = !odd && there == ~0ull &&
-                       ((j0 + kManyBlock - 1 <= first && (int64_t)last - j0 < p.window) || j0 + kManyBlock <= w.r.prefix);
-    const bool any = (j0 <= last && (int64_t)j0 + kManyBlock - 1 > (int64_t)first - p.window) || j0 < w.r.prefix;
-    if (has_rows && any) {
-      if (whole) {
-        block(x, j0, ~0ull, false, std::true_type{});
-      } else {
-        block(x, j0, there & ((low_bits(pos - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(w.r.prefix - j0)),
-              odd, std::false_type{});
       }
     }
     if (odd) {  // the next such block starts with no keys
       __syncthreads();
       for (uint32_t i = threadIdx.x; i < 2 * kDim; i += kManyThreads) (&s_odd[0][0])[i] = 0;
-      __syncthreads();
     }
-    if (more) put(x + 1);
+    if (more) {
+      put(0, k_next);
+      put(1, v_next);
+    }
     __syncthreads();
+  };
+
+  for (uint32_t i = threadIdx.x; i < 2 * kDim; i += kManyThreads) (&s_odd[0][0])[i] = 0;
+  if (wave == 0) {
+#pragma unroll
+    for (int i = -1; i < 3; ++i) hand_out(look_up(x0 + i), x0 + i);
+    ahead = look_up(x0 + 3);
+  }
+  __syncthreads();
+  if (x0 < x_end) {
+    load(x0 - 1, 0, kKeys[1]);
+    put(0, kKeys[1]);
+    load(x0, 0, kKeys[0]);
+    load(x0, 1, kValues[0]);
+    put(0, kKeys[0]);
+    put(1, kValues[0]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) now[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kSteps * 2; ++k)
+      now = Q::mfma32(*lds_at<u32x4>(beside(key_at, k * 32) + kKeys[1] + kHalfKeys), q[k], now);
+    // the first step loads into the buffer that these products read
+    __syncthreads();
+    for (int32_t x = x0;;) {
+      step(x, kKeys[0], kKeys[1], kValues[0], kValues[1]);
+      if (++x >= x_end) break;
+      step(x, kKeys[1], kKeys[0], kValues[1], kValues[0]);
+      if (++x >= x_end) break;
+    }
   }
 
   sum = xor32(sum, sum_of);
