@@ -42,10 +42,11 @@ constexpr uint32_t kFewUpto = 17;
 // With W the key blocks of all tiles, a part has c >= W heads / most blocks, so
 // there are at most most / heads parts more than tiles; a divided tile has
 // less than 2 blocks / c parts, so divided tiles have at most 2 most / heads.
+// one_tile: no request that it takes has more than one.
 AttendForm divide(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t rows, uint32_t block, uint32_t least,
-                  uint32_t most) {
+                  uint32_t most, bool one_tile) {
   AttendForm f{};
-  const uint64_t tiles = a.tokens * (a.heads / c.heads) / rows + std::min<uint64_t>(a.requests, a.tokens);
+  const uint64_t tiles = (one_tile ? 0 : a.tokens * (a.heads / c.heads) / rows) + std::min<uint64_t>(a.requests, a.tokens);
   const uint64_t blocks = ((uint64_t)a.width * c.page_tokens + block - 1) / block;
   const uint64_t parts = (blocks + least - 1) / least, extra = most / c.heads + 1;
   const uint64_t slots = parts > 1 ? std::min(tiles * parts, 2 * extra) : 0;
@@ -71,8 +72,8 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   const uint64_t others = (a.requests - 1) * most;
   const uint64_t fewest = a.tokens > others ? a.tokens - others : 1;
   const bool few = fewest * group < kFewUpto, many = most * group >= kFewUpto;
-  if (few) l.few = divide(c, a, kFewRows, kFewBlock, 4, 2048);
-  if (many) l.many = divide(c, a, kManyRows, kManyBlock, 4, 1024);
+  if (few) l.few = divide(c, a, kFewRows, kFewBlock, 4, many ? 1024 : 2048, many);
+  if (many) l.many = divide(c, a, kManyRows, kManyBlock, 4, 1024, false);
   if (few && many) l.few.upto = l.many.from = kFewUpto;
   const uint64_t row = (c.D + 2) * sizeof(float) * c.heads;
   *bytes = std::max<uint64_t>(l.few.part_slots * kFewRows, (uint64_t)l.many.part_slots * kManyRows) * row;

@@ -85,13 +85,73 @@ __device__ __forceinline__ __attribute__((address_space(3))) T *lds_at(uint32_t 
   return (__attribute__((address_space(3))) T *)(uintptr_t)address;
 }
 
-// Two transposing LDS reads.  In each, lane l of 16 names the 8 bytes that hold
-// elements 4 (l % 4) .. + 3 of row l / 4, and gets element l of the four rows.
-__device__ __forceinline__ u32x4 transposed(uint32_t a, uint32_t b) {
-  typedef short s16x4 __attribute__((ext_vector_type(4)));
-  const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(a)));
-  const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(b)));
-  return u32x4{x.x, x.y, y.x, y.y};
+// Transposing LDS reads of two times sixteen keys' values at 32 kTiles elements: in each, lane l
+// of 16 names the 8 bytes that hold elements 4 (l % 4) .. + 3 of a key l / 4, and gets element l
+// of the four keys.  at[t][h]: address of elements 32 t.. and of the first (h = 0) or second eight
+// of the sixteen; kFrom: offset of the first sixteen keys; kNext: how much further the others are.
+// Written out, with the wait among them, because the compiler takes this read to depend on the
+// loads into other parts of LDS that are on their way, and would wait for those.
+template <int kTiles, uint32_t kFrom, uint32_t kNext>
+__device__ __forceinline__ void read_transposed(const uint32_t (&at)[kTiles][2], u32x4 (&v)[2][kTiles]) {
+  u32x2 x[2][kTiles][2];
+  if constexpr (kTiles == 2)
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8 offset:%12\n"
+        "ds_read_b64_tr_b16 %1, %9 offset:%12\n"
+        "ds_read_b64_tr_b16 %2, %10 offset:%12\n"
+        "ds_read_b64_tr_b16 %3, %11 offset:%12\n"
+        "ds_read_b64_tr_b16 %4, %8 offset:%13\n"
+        "ds_read_b64_tr_b16 %5, %9 offset:%13\n"
+        "ds_read_b64_tr_b16 %6, %10 offset:%13\n"
+        "ds_read_b64_tr_b16 %7, %11 offset:%13\n"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0][0]), "=&v"(x[0][0][1]), "=&v"(x[0][1][0]), "=&v"(x[0][1][1]), "=&v"(x[1][0][0]), "=&v"(x[1][0][1]), "=&v"(x[1][1][0]), "=&v"(x[1][1][1])
+        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "n"(kFrom), "n"(kFrom + kNext)
+        : "memory");
+  else if constexpr (kTiles == 3)
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %12 offset:%18\n"
+        "ds_read_b64_tr_b16 %1, %13 offset:%18\n"
+        "ds_read_b64_tr_b16 %2, %14 offset:%18\n"
+        "ds_read_b64_tr_b16 %3, %15 offset:%18\n"
+        "ds_read_b64_tr_b16 %4, %16 offset:%18\n"
+        "ds_read_b64_tr_b16 %5, %17 offset:%18\n"
+        "ds_read_b64_tr_b16 %6, %12 offset:%19\n"
+        "ds_read_b64_tr_b16 %7, %13 offset:%19\n"
+        "ds_read_b64_tr_b16 %8, %14 offset:%19\n"
+        "ds_read_b64_tr_b16 %9, %15 offset:%19\n"
+        "ds_read_b64_tr_b16 %10, %16 offset:%19\n"
+        "ds_read_b64_tr_b16 %11, %17 offset:%19\n"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0][0]), "=&v"(x[0][0][1]), "=&v"(x[0][1][0]), "=&v"(x[0][1][1]), "=&v"(x[0][2][0]), "=&v"(x[0][2][1]), "=&v"(x[1][0][0]), "=&v"(x[1][0][1]), "=&v"(x[1][1][0]), "=&v"(x[1][1][1]), "=&v"(x[1][2][0]), "=&v"(x[1][2][1])
+        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "v"(at[2][0]), "v"(at[2][1]), "n"(kFrom), "n"(kFrom + kNext)
+        : "memory");
+  else if constexpr (kTiles == 4)
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %16 offset:%24\n"
+        "ds_read_b64_tr_b16 %1, %17 offset:%24\n"
+        "ds_read_b64_tr_b16 %2, %18 offset:%24\n"
+        "ds_read_b64_tr_b16 %3, %19 offset:%24\n"
+        "ds_read_b64_tr_b16 %4, %20 offset:%24\n"
+        "ds_read_b64_tr_b16 %5, %21 offset:%24\n"
+        "ds_read_b64_tr_b16 %6, %22 offset:%24\n"
+        "ds_read_b64_tr_b16 %7, %23 offset:%24\n"
+        "ds_read_b64_tr_b16 %8, %16 offset:%25\n"
+        "ds_read_b64_tr_b16 %9, %17 offset:%25\n"
+        "ds_read_b64_tr_b16 %10, %18 offset:%25\n"
+        "ds_read_b64_tr_b16 %11, %19 offset:%25\n"
+        "ds_read_b64_tr_b16 %12, %20 offset:%25\n"
+        "ds_read_b64_tr_b16 %13, %21 offset:%25\n"
+        "ds_read_b64_tr_b16 %14, %22 offset:%25\n"
+        "ds_read_b64_tr_b16 %15, %23 offset:%25\n"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0][0]), "=&v"(x[0][0][1]), "=&v"(x[0][1][0]), "=&v"(x[0][1][1]), "=&v"(x[0][2][0]), "=&v"(x[0][2][1]), "=&v"(x[0][3][0]), "=&v"(x[0][3][1]), "=&v"(x[1][0][0]), "=&v"(x[1][0][1]), "=&v"(x[1][1][0]), "=&v"(x[1][1][1]), "=&v"(x[1][2][0]), "=&v"(x[1][2][1]), "=&v"(x[1][3][0]), "=&v"(x[1][3][1])
+        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "v"(at[2][0]), "v"(at[2][1]), "v"(at[3][0]), "v"(at[3][1]), "n"(kFrom), "n"(kFrom + kNext)
+        : "memory");
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) v[i][t] = u32x4{x[i][t][0].x, x[i][t][0].y, x[i][t][1].x, x[i][t][1].y};
 }
 
 struct AttendParams {
@@ -119,9 +179,9 @@ struct AttendParams {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// Zeros that lanes without a key (or past a head's D) read instead of memory
-// that is not theirs: a 0 from here, times any weight, adds nothing.
-__device__ __align__(16) static uint32_t kv_zeros[4];
+// A row of zeros that lanes without a key (or past a head's D) read instead of
+// memory that is not theirs: a 0 from here, times any weight, adds nothing.
+__device__ __align__(16) static uint32_t kv_zeros[128];
 
 // A request as the kernels see it: every value clamped into its range.
 struct Request {
@@ -331,6 +391,14 @@ __device__ __forceinline__ float xor16(float x, float (*op)(float, float)) {
 }
 __device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+
+// The largest of three, NaN passed over.  Written out: fmaxf of values that may be signalling
+// NaN quiets each of them first, an instruction a value.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 // 2^x; -inf gives 0.
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -42,7 +42,7 @@ __device__ __forceinline__ uint64_t low_bits(int32_t n) {
 
 // kSteps: D <= 32 kSteps.  k8: pages of 8-bit values.  kMore: scores are capped or biased.
 template <typename Q, bool k8, int kSteps, bool kMore>
-__global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(AttendParams p) {
+__global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : kSteps > 2 ? 2 : 3) void attend_many(AttendParams p) {
   constexpr int kDim = kSteps * 32, kChunks = kDim / 8;                              // 16-byte pieces of a row
   constexpr int kPasses = kManyBlock * kChunks / kManyThreads;                       // pieces a thread
   static_assert(kPasses * kManyThreads == kManyBlock * kChunks, "pieces divide");
@@ -112,8 +112,8 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
   auto hand_out = [&](const KeyLook &k, int32_t x) __attribute__((always_inline)) {
     const bool there = key_there(p, k);
     const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
-    s_row[x & 3][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : 0;
-    s_row[x & 3][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : 0;
+    s_row[x & 3][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : zeros;
+    s_row[x & 3][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : zeros;
     const uint64_t bits = __ballot(there);
     if (lane == 0) s_there[x & 3] = bits;
   };
@@ -133,21 +133,35 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
   Raw stage[2][kDirect ? 1 : kPasses];
   const uint32_t lds = (uint32_t)(uintptr_t)(LdsBytes *)s_kv;
   constexpr uint32_t kKeys[2] = {0, kKeyBytes}, kValues[2] = {2 * kKeyBytes, 2 * kKeyBytes + kValueBytes};
-  // kv: the values of block x, or keys half a block later: 32.. of block x, ..31 of x + 1.
+  // The values of block x and the keys half a block later: 32.. of block x, ..31 of x + 1.
+  auto row_of = [&](int32_t x, int kv, int i) __attribute__((always_inline)) -> uint64_t {
+    const uint32_t key = ((i * kManyWaves + wave) * 64 + lane) / kChunks;
+    return kv ? s_row[x & 3][1][key] : s_row[(x + (key >> 5)) & 3][0][key ^ 32];
+  };
+  const bool whole_rows = p.D == kDim;
+  auto load_row = [&](uint64_t row, int kv, int i, uint32_t to, bool whole) __attribute__((always_inline)) {
+    const uint32_t piece = (i * kManyWaves + wave) * 64 + lane, c = piece % kChunks;
+    const uint32_t d = (kDirect ? c ^ turned(piece / kChunks) : c) * 8;
+    const uint64_t at = whole || d < p.D ? row + d * kElem : zeros;
+    if constexpr (kDirect) {
+      typedef __attribute__((address_space(1))) const uint32_t global_u32;
+      __builtin_amdgcn_global_load_lds((global_u32 *)at, (LdsBytes *)(uintptr_t)(lds + to + (i * kManyWaves + wave) * 1024),
+                                       16, 0, 0);
+    } else {
+      stage[kv][i] = *reinterpret_cast<const Raw *>(at);
+    }
+  };
   auto load = [&](int32_t x, int kv, uint32_t to) __attribute__((always_inline)) {
+    uint64_t row[kPasses];
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-      const uint32_t piece = (i * kManyWaves + wave) * 64 + lane, key = piece / kChunks;
-      const uint32_t c = piece % kChunks, d = (kDirect ? c ^ turned(key) : c) * 8;
-      const uint64_t row = kv ? s_row[x & 3][1][key] : s_row[(x + (key >> 5)) & 3][0][key ^ 32];
-      const uint64_t at = row && d < p.D ? row + d * kElem : zeros;
-      if constexpr (kDirect) {
-        typedef __attribute__((address_space(1))) const uint32_t global_u32;
-        __builtin_amdgcn_global_load_lds((global_u32 *)at, (LdsBytes *)(uintptr_t)(lds + to + (i * kManyWaves + wave) * 1024),
-                                         16, 0, 0);
-      } else {
-        stage[kv][i] = *reinterpret_cast<const Raw *>(at);
-      }
+    for (int i = 0; i < kPasses; ++i) row[i] = row_of(x, kv, i);
+    __builtin_amdgcn_sched_barrier(0);  // all rows are read before the first is waited for
+    if (whole_rows) {
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i) load_row(row[i], kv, i, to, true);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i) load_row(row[i], kv, i, to, false);
     }
   };
   auto put = [&](int kv, uint32_t to) __attribute__((always_inline)) {
@@ -226,7 +240,8 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
   auto rescale = [&](const f32x16 &s) __attribute__((always_inline)) {
     float top = s[0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    for (int i = 1; i < 15; i += 2) top = max3(top, s[i], s[i + 1]);
+    top = max3(top, s[15], s[15]);
     top = xor32(top, max_of) * to_log2;
     if (__any((top > best + kSlack) | (best == -INFINITY))) {
       const float to = fmaxf(best, top);
@@ -239,47 +254,57 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
   };
   // 32 keys' scores to weights and O^T of their values, with the scores of the 32 keys after
   // them computed beside (S^T from `keys`): a matrix instruction takes as long as eight others,
-  // so the exponentials go between those of S^T, and LDS is read a step ahead of its use.
-  auto both = [&](uint32_t keys, f32x16 &next, uint32_t values, const f32x16 &s) __attribute__((always_inline)) {
-    // held as they are: the addresses made of them would cost registers that Q needs
+  // so the exponentials go between those of S^T.  LDS is read first, all at once, while the
+  // products of the 32 keys before are still under way and the maximum is looked for.
+  auto both = [&](f32x16 &s, f32x16 &next, auto keys, auto values, auto &&prepare) __attribute__((always_inline)) {
+    constexpr int kTiles = kSteps > 4 ? 4 : kSteps, kTurns = kSteps / kTiles;
+    constexpr uint32_t kFrom = decltype(values)::value, kSixteen = 16 * kValueRow * 2;
+    constexpr uint32_t kFar = kFrom + kSixteen > 65535 ? kFrom : 0;  // an instruction's offset has 16 bits
+    // held as they are: the addresses made of them would cost registers
     asm volatile("" : "+v"(key_at), "+v"(value_at[0]), "+v"(value_at[1]));
-    const float from = best == -INFINITY ? 0.f : best;
-    u32x4 weights[2], kf[2], vf[2][2];
-    auto read_keys = [&](int k) __attribute__((always_inline)) { kf[k & 1] = *lds_at<u32x4>(beside(key_at, k * 32) + keys); };
-    auto read_values = [&](int c) __attribute__((always_inline)) {  // two of sixteen keys' values at elements 32 t + m, keys outside
+    u32x4 kf[4], vf[2][kTiles];  // keys: four steps ahead; values: all, or half of 256 elements
+    __builtin_amdgcn_sched_barrier(0);
+    auto read_keys = [&](int k) __attribute__((always_inline)) {
+      kf[k & 3] = *lds_at<u32x4>(beside(key_at, k * 32) + decltype(keys)::value);
+    };
+    auto read_values = [&](int u) __attribute__((always_inline)) {
+      uint32_t at[kTiles][2];
 #pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const int i = (c * 2 + f) / kSteps, t = (c * 2 + f) % kSteps;
-        vf[c & 1][f] = transposed(beside(value_at[0], t * 64) + values + i * 16 * kValueRow * 2,
-                                  beside(value_at[1], t * 64) + values + i * 16 * kValueRow * 2);
-      }
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) at[t][h] = beside(value_at[h], (u * kTiles + t) * 64) + kFar;
+      read_transposed<kTiles, kFrom - kFar, kSixteen>(at, vf);
     };
 #pragma unroll
+    for (int k = 0; k < 4; ++k) read_keys(k);
+    if constexpr (kTurns == 1) read_values(0);
+    __builtin_amdgcn_sched_barrier(0);
+    prepare(s);
+    const float from = best == -INFINITY ? 0.f : best;
+    u32x4 weights[2];
+#pragma unroll
     for (int i = 0; i < 16; ++i) next[i] = 0.f;
-    read_keys(0);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < kSteps * 2; ++k) {
-      if (k + 1 < kSteps * 2) read_keys(k + 1);
-      else read_values(0);
-      next = Q::mfma32(kf[k & 1], q[k], next);
+      next = Q::mfma32(kf[k & 3], q[k], next);
+      if (k + 4 < kSteps * 2) read_keys(k + 4);
 #pragma unroll
       for (int e = 8 * k / (kSteps * 2); e < 8 * (k + 1) / (kSteps * 2); ++e) {  // pairs of scores
         const float w0 = pow2(__builtin_fmaf(s[e * 2], to_log2, -from));
         const float w1 = pow2(__builtin_fmaf(s[e * 2 + 1], to_log2, -from));
-        sum += w0 + w1;
         weights[e >> 2][e & 3] = Q::pack(w0, w1);
+        sum += w0 + w1;
       }
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int c = 0; c < kSteps; ++c) {
-      if (c + 1 < kSteps) read_values(c + 1);
+    for (int u = 0; u < kTurns; ++u) {
+      if constexpr (kTurns > 1) read_values(u);
 #pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const int i = (c * 2 + f) / kSteps, t = (c * 2 + f) % kSteps;
-        o[t] = Q::mfma32(vf[c & 1][f], weights[i], o[t]);
-      }
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) o[u * kTiles + t] = Q::mfma32(vf[i][t], weights[i], o[u * kTiles + t]);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -290,7 +315,9 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
   constexpr uint32_t kHalfKeys = 32 * kKeyRow * 2, kHalfValues = 32 * kValueRow * 2;
   f32x16 now, next;
   KeyLook ahead{};
-  auto step = [&](int32_t x, uint32_t k_now, uint32_t k_next, uint32_t v_now, uint32_t v_next) __attribute__((always_inline)) {
+  auto step = [&](int32_t x, auto turn, auto computes) __attribute__((always_inline)) {
+    constexpr int kNow = decltype(turn)::value, kNext = 1 - kNow;
+    constexpr uint32_t k_now = kKeys[kNow], k_next = kKeys[kNext], v_now = kValues[kNow], v_next = kValues[kNext];
     const bool more = x + 1 < x_end;
     if (wave == 0) {
       hand_out(ahead, x + 3);
@@ -319,15 +346,19 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
         for (int i = 0; i < 16; ++i) s[i] = seen >> ((i >> 2) * 8 + (i & 3)) & 1u ? s[i] : -INFINITY;
       }
     };
-    if (has_rows) {
-      changed(now, j0);
-      mask(now, (uint32_t)sees);
-      rescale(now);
-      both(k_now, next, v_now, now);
-      changed(next, j0 + 32);
-      mask(next, (uint32_t)(sees >> 32));
-      rescale(next);
-      both(k_now + kHalfKeys, now, v_now + kHalfValues, next);
+    if constexpr (decltype(computes)::value) {
+      both(now, next, std::integral_constant<uint32_t, k_now>{}, std::integral_constant<uint32_t, v_now>{},
+           [&](f32x16 &s) __attribute__((always_inline)) {
+             changed(s, j0);
+             mask(s, (uint32_t)sees);
+             rescale(s);
+           });
+      both(next, now, std::integral_constant<uint32_t, k_now + kHalfKeys>{},
+           std::integral_constant<uint32_t, v_now + kHalfValues>{}, [&](f32x16 &s) __attribute__((always_inline)) {
+             changed(s, j0 + 32);
+             mask(s, (uint32_t)(sees >> 32));
+             rescale(s);
+           });
       if (__builtin_expect(odd, 0)) {
 #pragma unroll
         for (int t = 0; t < kSteps; ++t)
@@ -372,12 +403,16 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : 2) void attend_many(
       now = Q::mfma32(*lds_at<u32x4>(beside(key_at, k * 32) + kKeys[1] + kHalfKeys), q[k], now);
     // the first step loads into the buffer that these products read
     __syncthreads();
-    for (int32_t x = x0;;) {
-      step(x, kKeys[0], kKeys[1], kValues[0], kValues[1]);
-      if (++x >= x_end) break;
-      step(x, kKeys[1], kKeys[0], kValues[1], kValues[0]);
-      if (++x >= x_end) break;
-    }
+    auto steps = [&](auto computes) __attribute__((always_inline)) {
+      for (int32_t x = x0;;) {
+        step(x, std::integral_constant<int, 0>{}, computes);
+        if (++x >= x_end) break;
+        step(x, std::integral_constant<int, 1>{}, computes);
+        if (++x >= x_end) break;
+      }
+    };
+    if (has_rows) steps(std::true_type{});
+    else steps(std::false_type{});  // loads for the others
   }
 
   sum = xor32(sum, sum_of);
