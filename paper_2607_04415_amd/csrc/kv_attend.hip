@@ -38,26 +38,20 @@ gorio_status check(const gorio_kv_cache *cache, const gorio_kv_attention *a, gor
 constexpr uint32_t kFewUpto = 17;
 
 // What a call launches and keeps, from the sizes that the host knows: the
-// lengths are on the GPU, so these are bounds, and blocks without work return.
-// With W the key blocks of all tiles, a part has c >= W heads / most blocks, so
-// there are at most most / heads parts more than tiles; a divided tile has
-// less than 2 blocks / c parts, so divided tiles have at most 2 most / heads.
-// one_tile: no request that it takes has more than one.
+// lengths are on the GPU, so these are bounds, and workgroups without work
+// return.  `all`: workgroups that run at once on the GPU.  one_tile: no
+// request that the form takes has more than one tile.
 AttendForm divide(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t rows, uint32_t block, uint32_t least,
-                  uint32_t most, bool one_tile) {
+                  uint32_t all, bool one_tile) {
   AttendForm f{};
   const uint64_t tiles = (one_tile ? 0 : a.tokens * (a.heads / c.heads) / rows) + std::min<uint64_t>(a.requests, a.tokens);
   const uint64_t blocks = ((uint64_t)a.width * c.page_tokens + block - 1) / block;
-  const uint64_t parts = (blocks + least - 1) / least, extra = most / c.heads + 1;
-  const uint64_t slots = parts > 1 ? std::min(tiles * parts, 2 * extra) : 0;
   f.rows = rows;
   f.from = 1;
   f.upto = 0xFFFFFFFFu;
   f.least = least;
-  f.most = most;
-  f.part_slots = (uint32_t)slots;
-  f.grid = (uint32_t)std::min<uint64_t>(std::min(tiles * parts, tiles + extra) * c.heads, kKvMost);
-  f.join = (uint32_t)std::min<uint64_t>(slots / 2 * c.heads, kKvMost);
+  f.shares = (uint32_t)std::min<uint64_t>(std::max(all / c.heads, 1u), (tiles * blocks + least - 1) / least);
+  f.join = f.shares > 1 ? (uint32_t)std::min<uint64_t>(tiles, kKvMost / c.heads) : 0;
   return f;
 }
 
@@ -72,11 +66,13 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   const uint64_t others = (a.requests - 1) * most;
   const uint64_t fewest = a.tokens > others ? a.tokens - others : 1;
   const bool few = fewest * group < kFewUpto, many = most * group >= kFewUpto;
-  if (few) l.few = divide(c, a, kFewRows, kFewBlock, 4, many ? 1024 : 2048, many);
-  if (many) l.many = divide(c, a, kManyRows, kManyBlock, 4, 1024, false);
+  if (few) l.few = divide(c, a, kFewRows, kFewBlock, 4, 512, many);
+  const int steps = steps_of(c.D);
+  if (many) l.many = divide(c, a, many_rows(steps), kManyBlock, 4, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
   if (few && many) l.few.upto = l.many.from = kFewUpto;
-  const uint64_t row = (c.D + 2) * sizeof(float) * c.heads;
-  *bytes = std::max<uint64_t>(l.few.part_slots * kFewRows, (uint64_t)l.many.part_slots * kManyRows) * row;
+  const uint64_t slot = 2 * (c.D + 2) * sizeof(float) * c.heads;  // two parts of a share
+  *bytes = std::max<uint64_t>(l.few.join ? l.few.shares * kFewRows : 0,
+                              l.many.join ? (uint64_t)l.many.shares * many_rows(steps) : 0) * slot;
   return l;
 }
 

@@ -13,6 +13,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "kv.hpp"
 
 namespace gorio {
@@ -85,73 +87,53 @@ __device__ __forceinline__ __attribute__((address_space(3))) T *lds_at(uint32_t 
   return (__attribute__((address_space(3))) T *)(uintptr_t)address;
 }
 
-// Transposing LDS reads of two times sixteen keys' values at 32 kTiles elements: in each, lane l
-// of 16 names the 8 bytes that hold elements 4 (l % 4) .. + 3 of a key l / 4, and gets element l
-// of the four keys.  at[t][h]: address of elements 32 t.. and of the first (h = 0) or second eight
-// of the sixteen; kFrom: offset of the first sixteen keys; kNext: how much further the others are.
+// Transposing LDS reads of sixteen keys' values at 32 kTiles elements: in each, lane l of 16
+// names the 8 bytes that hold elements 4 (l % 4) .. + 3 of a key l / 4, and gets element l of the
+// four keys.  at[t][h]: address of elements 32 t.. of the first (h = 0) or second eight of the
+// sixteen, less kFrom.
 // Written out, with the wait among them, because the compiler takes this read to depend on the
 // loads into other parts of LDS that are on their way, and would wait for those.
-template <int kTiles, uint32_t kFrom, uint32_t kNext>
-__device__ __forceinline__ void read_transposed(const uint32_t (&at)[kTiles][2], u32x4 (&v)[2][kTiles]) {
-  u32x2 x[2][kTiles][2];
+template <int kTiles, uint32_t kFrom>
+__device__ __forceinline__ void read_transposed(const uint32_t (&at)[kTiles][2], u32x4 (&v)[kTiles]) {
+  u32x2 x[kTiles][2];
   if constexpr (kTiles == 2)
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %8 offset:%12\n"
-        "ds_read_b64_tr_b16 %1, %9 offset:%12\n"
-        "ds_read_b64_tr_b16 %2, %10 offset:%12\n"
-        "ds_read_b64_tr_b16 %3, %11 offset:%12\n"
-        "ds_read_b64_tr_b16 %4, %8 offset:%13\n"
-        "ds_read_b64_tr_b16 %5, %9 offset:%13\n"
-        "ds_read_b64_tr_b16 %6, %10 offset:%13\n"
-        "ds_read_b64_tr_b16 %7, %11 offset:%13\n"
+        "ds_read_b64_tr_b16 %0, %4 offset:%8\n"
+        "ds_read_b64_tr_b16 %1, %5 offset:%8\n"
+        "ds_read_b64_tr_b16 %2, %6 offset:%8\n"
+        "ds_read_b64_tr_b16 %3, %7 offset:%8\n"
         "s_waitcnt lgkmcnt(0)"
-        : "=&v"(x[0][0][0]), "=&v"(x[0][0][1]), "=&v"(x[0][1][0]), "=&v"(x[0][1][1]), "=&v"(x[1][0][0]), "=&v"(x[1][0][1]), "=&v"(x[1][1][0]), "=&v"(x[1][1][1])
-        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "n"(kFrom), "n"(kFrom + kNext)
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1])
+        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "n"(kFrom)
         : "memory");
   else if constexpr (kTiles == 3)
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %12 offset:%18\n"
-        "ds_read_b64_tr_b16 %1, %13 offset:%18\n"
-        "ds_read_b64_tr_b16 %2, %14 offset:%18\n"
-        "ds_read_b64_tr_b16 %3, %15 offset:%18\n"
-        "ds_read_b64_tr_b16 %4, %16 offset:%18\n"
-        "ds_read_b64_tr_b16 %5, %17 offset:%18\n"
-        "ds_read_b64_tr_b16 %6, %12 offset:%19\n"
-        "ds_read_b64_tr_b16 %7, %13 offset:%19\n"
-        "ds_read_b64_tr_b16 %8, %14 offset:%19\n"
-        "ds_read_b64_tr_b16 %9, %15 offset:%19\n"
-        "ds_read_b64_tr_b16 %10, %16 offset:%19\n"
-        "ds_read_b64_tr_b16 %11, %17 offset:%19\n"
+        "ds_read_b64_tr_b16 %0, %6 offset:%12\n"
+        "ds_read_b64_tr_b16 %1, %7 offset:%12\n"
+        "ds_read_b64_tr_b16 %2, %8 offset:%12\n"
+        "ds_read_b64_tr_b16 %3, %9 offset:%12\n"
+        "ds_read_b64_tr_b16 %4, %10 offset:%12\n"
+        "ds_read_b64_tr_b16 %5, %11 offset:%12\n"
         "s_waitcnt lgkmcnt(0)"
-        : "=&v"(x[0][0][0]), "=&v"(x[0][0][1]), "=&v"(x[0][1][0]), "=&v"(x[0][1][1]), "=&v"(x[0][2][0]), "=&v"(x[0][2][1]), "=&v"(x[1][0][0]), "=&v"(x[1][0][1]), "=&v"(x[1][1][0]), "=&v"(x[1][1][1]), "=&v"(x[1][2][0]), "=&v"(x[1][2][1])
-        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "v"(at[2][0]), "v"(at[2][1]), "n"(kFrom), "n"(kFrom + kNext)
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1])
+        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "v"(at[2][0]), "v"(at[2][1]), "n"(kFrom)
         : "memory");
   else if constexpr (kTiles == 4)
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %16 offset:%24\n"
-        "ds_read_b64_tr_b16 %1, %17 offset:%24\n"
-        "ds_read_b64_tr_b16 %2, %18 offset:%24\n"
-        "ds_read_b64_tr_b16 %3, %19 offset:%24\n"
-        "ds_read_b64_tr_b16 %4, %20 offset:%24\n"
-        "ds_read_b64_tr_b16 %5, %21 offset:%24\n"
-        "ds_read_b64_tr_b16 %6, %22 offset:%24\n"
-        "ds_read_b64_tr_b16 %7, %23 offset:%24\n"
-        "ds_read_b64_tr_b16 %8, %16 offset:%25\n"
-        "ds_read_b64_tr_b16 %9, %17 offset:%25\n"
-        "ds_read_b64_tr_b16 %10, %18 offset:%25\n"
-        "ds_read_b64_tr_b16 %11, %19 offset:%25\n"
-        "ds_read_b64_tr_b16 %12, %20 offset:%25\n"
-        "ds_read_b64_tr_b16 %13, %21 offset:%25\n"
-        "ds_read_b64_tr_b16 %14, %22 offset:%25\n"
-        "ds_read_b64_tr_b16 %15, %23 offset:%25\n"
+        "ds_read_b64_tr_b16 %0, %8 offset:%16\n"
+        "ds_read_b64_tr_b16 %1, %9 offset:%16\n"
+        "ds_read_b64_tr_b16 %2, %10 offset:%16\n"
+        "ds_read_b64_tr_b16 %3, %11 offset:%16\n"
+        "ds_read_b64_tr_b16 %4, %12 offset:%16\n"
+        "ds_read_b64_tr_b16 %5, %13 offset:%16\n"
+        "ds_read_b64_tr_b16 %6, %14 offset:%16\n"
+        "ds_read_b64_tr_b16 %7, %15 offset:%16\n"
         "s_waitcnt lgkmcnt(0)"
-        : "=&v"(x[0][0][0]), "=&v"(x[0][0][1]), "=&v"(x[0][1][0]), "=&v"(x[0][1][1]), "=&v"(x[0][2][0]), "=&v"(x[0][2][1]), "=&v"(x[0][3][0]), "=&v"(x[0][3][1]), "=&v"(x[1][0][0]), "=&v"(x[1][0][1]), "=&v"(x[1][1][0]), "=&v"(x[1][1][1]), "=&v"(x[1][2][0]), "=&v"(x[1][2][1]), "=&v"(x[1][3][0]), "=&v"(x[1][3][1])
-        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "v"(at[2][0]), "v"(at[2][1]), "v"(at[3][0]), "v"(at[3][1]), "n"(kFrom), "n"(kFrom + kNext)
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]), "=&v"(x[3][0]), "=&v"(x[3][1])
+        : "v"(at[0][0]), "v"(at[0][1]), "v"(at[1][0]), "v"(at[1][1]), "v"(at[2][0]), "v"(at[2][1]), "v"(at[3][0]), "v"(at[3][1]), "n"(kFrom)
         : "memory");
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) v[i][t] = u32x4{x[i][t][0].x, x[i][t][0].y, x[i][t][1].x, x[i][t][1].y};
+  for (int t = 0; t < kTiles; ++t) v[t] = u32x4{x[t][0].x, x[t][0].y, x[t][1].x, x[t][1].y};
 }
 
 struct AttendParams {
@@ -172,8 +154,7 @@ struct AttendParams {
   // division of the work (see WorkItem)
   uint32_t rows;         // query rows of a tile
   uint32_t from, upto;   // requests with this many rows a key head, from <= rows < upto
-  uint32_t least, most;  // key blocks of a part, at least; parts to aim at, all heads together
-  uint32_t part_slots;   // parts that the workspace holds, of one head
+  uint32_t shares, least;  // workgroups of a key head, at most; key blocks of a share, at least
 };
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -221,19 +202,24 @@ __device__ __forceinline__ KeyRange key_range(const AttendParams &p, const Reque
 
 // ---------------------------------------------------------------------------
 // Division of the work.  A tile is `rows` query rows (token x head of the
-// group) of one request and key head; a part is a run of key blocks of a
-// tile.  How long the requests are is known on the GPU only, so every block
-// of threads finds its own part: it sums the key blocks of all tiles, takes
-// from that the length c of a part (so that about `most` parts come out, none
-// shorter than `least`), and walks the requests' numbers of parts up to its
-// own index.  That is two passes over a few lengths in L2; a kernel that did
-// it once before would cost a launch.
+// group) of one request and key head.  Of each key head, the key blocks of all
+// tiles, one tile after the other, make a line of W blocks, and workgroup i of
+// the head takes an equal share of it: blocks i c .. (i + 1) c - 1, whatever
+// tiles they belong to.  So all workgroups run equally long, however ragged the
+// lengths, and a tile is cut only where a share ends in it.  What a workgroup
+// computes of a cut tile is a part: its sums go to the workspace, where it has
+// two slots (a share cuts at most the tile it begins in and the one it ends
+// in), and a second kernel joins them.
+//
+// How long the requests are is known on the GPU only, so every workgroup finds
+// its share by itself: the tiles' blocks are counted and added up, in chunks of
+// as many tiles as there are threads, from a few lengths in L2.  A kernel that
+// did it once before would cost a launch.
 // ---------------------------------------------------------------------------
 struct WorkItem {
-  uint32_t request, tile, part;
-  uint32_t parts;      // of each of the request's tiles, 1: undivided
-  uint32_t slot;       // in the workspace, if divided
-  uint32_t c;          // key blocks of a part
+  uint32_t request, tile, tiles;  // tile of the request's tiles
+  uint64_t begin;                 // of the tile on the line
+  uint64_t share, line;           // c and W
   Request r;
 };
 
@@ -242,12 +228,38 @@ __device__ __forceinline__ uint32_t tiles_of(const AttendParams &p, const Reques
   return (rows >= p.from) & (rows < p.upto) ? (rows + p.rows - 1) / p.rows : 0;
 }
 
-template <int kThreads>
-__device__ __forceinline__ uint32_t scan_threads(uint32_t v, uint32_t *sums) {
+// Rows of a tile: row n is token n / group of the request's new ones, head
+// n % group of the key head's.
+struct Tile {
+  uint32_t row0, rows;  // first row, rows
+  int32_t first, last;  // positions of its first and last token
+};
+
+__device__ __forceinline__ Tile tile_of(const AttendParams &p, const Request &r, uint32_t tile) {
+  Tile t;
+  const uint32_t all = (uint32_t)r.added * p.group.d;
+  t.row0 = tile * p.rows;
+  t.rows = min(p.rows, all - t.row0);
+  const int32_t base = r.len - r.added;
+  t.first = base + (int32_t)fastdiv(t.row0, p.group);
+  t.last = base + (int32_t)fastdiv(t.row0 + t.rows - 1, p.group);
+  return t;
+}
+
+// A tile's blocks on the line: one at least, so that a tile that sees nothing is written by someone.
+template <int kBlock>
+__device__ __forceinline__ uint32_t blocks_of(const AttendParams &p, const Request &r, uint32_t tile) {
+  const Tile t = tile_of(p, r, tile);
+  return (uint32_t)max(key_range<kBlock>(p, r, t.first, t.last).count, 1);
+}
+
+// Inclusive sum over the threads, in thread order.
+template <int kThreads, typename T>
+__device__ __forceinline__ T scan_threads(T v, T *sums) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t up = __shfl_up(v, d);
+    const T up = __shfl_up(v, d);
     if (lane >= d) v += up;
   }
   __syncthreads();
@@ -259,101 +271,105 @@ __device__ __forceinline__ uint32_t scan_threads(uint32_t v, uint32_t *sums) {
   return v;
 }
 
-// Item number `index` of the call, or false if there are not as many.  With
-// kJoin the items are the divided tiles themselves (which a second kernel
-// joins), and part is 0.  Every thread of the block gets the same answer.
+// A value that is the same for all lanes, into scalar registers.
+__device__ __forceinline__ uint64_t one(uint64_t v) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+         (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+}
+__device__ __forceinline__ Request one(const Request &r) {
+  return Request{__builtin_amdgcn_readfirstlane(r.start), __builtin_amdgcn_readfirstlane(r.added),
+                 __builtin_amdgcn_readfirstlane(r.len), __builtin_amdgcn_readfirstlane(r.prefix)};
+}
+
+// The tile in which share number `index` begins (kJoin: tile number `index`), or false if there
+// is none.  Every thread of the workgroup gets the same answer.
 template <int kThreads, int kBlock, bool kJoin>
 __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item) {
-  __shared__ uint32_t s_sums[kThreads / 64];
-  __shared__ uint64_t s_work[kThreads / 64];
-  __shared__ WorkItem s_item;
-  __shared__ int s_found;
-  uint64_t work = 0;
-  for (uint32_t b = threadIdx.x; b < p.requests; b += kThreads) {
-    const Request r = request_of(p, b);
-    const uint32_t tiles = tiles_of(p, r);
-    if (tiles) work += (uint64_t)tiles * key_range<kBlock>(p, r, r.len - r.added, r.len - 1).count;
-  }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d);
-  if ((threadIdx.x & 63) == 0) s_work[threadIdx.x >> 6] = work;
-  if (threadIdx.x == 0) s_found = 0;
-  __syncthreads();
-  work = 0;
-#pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) work += s_work[w];
-  const uint64_t each = (work * p.kv_heads + p.most - 1) / p.most;
-  const uint32_t c = (uint32_t)min(max(each, (uint64_t)p.least), (uint64_t)1 << 30);
-  uint32_t items0 = 0, slots0 = 0;
-  for (uint32_t b0 = 0; b0 < p.requests; b0 += kThreads) {
-    const uint32_t b = b0 + threadIdx.x;
-    WorkItem mine;
-    uint32_t tiles = 0, items = 0, slots = 0;
-    mine.parts = 1;
-    if (b < p.requests) {
-      mine.r = request_of(p, b);
-      tiles = tiles_of(p, mine.r);
-      if (tiles) {
-        const uint32_t blocks = key_range<kBlock>(p, mine.r, mine.r.len - mine.r.added, mine.r.len - 1).count;
-        mine.parts = max((blocks + c - 1) / c, 1u);
-        slots = mine.parts > 1 ? tiles * mine.parts : 0;
-        items = kJoin ? (mine.parts > 1 ? tiles : 0) : tiles * mine.parts;
+  __shared__ uint64_t s_sums[kThreads / 64], s_begin, s_line;
+  __shared__ uint32_t s_tiles[kThreads], s_counts[kThreads / 64], s_found[2];  // request, tile
+  if (threadIdx.x == 0) s_found[0] = ~0u;
+  uint64_t line = 0, share = 0;
+  // twice over the tiles: W is known after the first pass, and the tile after the second
+  for (int pass = 0; pass < 2; ++pass) {
+    uint64_t at = 0;       // on the line, of the next tile
+    uint32_t number = 0;   // of it
+    for (uint32_t b0 = 0; b0 < p.requests; b0 += kThreads) {
+      const uint32_t b = b0 + threadIdx.x;
+      const uint32_t mine = b < p.requests ? tiles_of(p, request_of(p, b)) : 0;
+      const uint32_t upto = scan_threads<kThreads>(mine, s_counts);
+      s_tiles[threadIdx.x] = upto;
+      __syncthreads();
+      const uint32_t tiles = s_tiles[kThreads - 1];
+      for (uint32_t f0 = 0; f0 < tiles; f0 += kThreads) {
+        const uint32_t f = f0 + threadIdx.x;
+        uint32_t blocks = 0, r = 0, tile = 0;
+        if (f < tiles) {
+          uint32_t hi = kThreads - 1;  // the first request whose tiles reach past f
+          while (r < hi) {
+            const uint32_t mid = (r + hi) / 2;
+            if (s_tiles[mid] > f) hi = mid;
+            else r = mid + 1;
+          }
+          tile = f - (r ? s_tiles[r - 1] : 0);
+          blocks = blocks_of<kBlock>(p, request_of(p, b0 + r), tile);
+        }
+        const uint64_t end = at + scan_threads<kThreads>((uint64_t)blocks, s_sums), begin = end - blocks;
+        if (pass) {
+          const bool here = kJoin ? number + f == index : (uint64_t)index * share >= begin && (uint64_t)index * share < end;
+          if (f < tiles && here) s_found[0] = b0 + r, s_found[1] = tile, s_begin = begin;
+        }
+        if (threadIdx.x == kThreads - 1) s_line = end;
+        __syncthreads();
+        at = s_line;
       }
+      number += tiles;
+      __syncthreads();
+      if (pass && s_found[0] != ~0u) break;
     }
-    const uint32_t items1 = items0 + scan_threads<kThreads>(items, s_sums);
-    const uint32_t slots1 = slots0 + scan_threads<kThreads>(slots, s_sums);
-    if (index < items1 && index >= items1 - items) {
-      const uint32_t at = index - (items1 - items), per = kJoin ? 1 : mine.parts;
-      mine.request = b;
-      // the last tiles of a chunk see the most keys: they begin first
-      const uint32_t from_end = at / per;
-      mine.tile = tiles - 1 - from_end;
-      mine.part = at - from_end * per;
-      mine.slot = slots1 - slots + from_end * mine.parts + mine.part;
-      mine.c = c;
-      s_item = mine;
-      s_found = 1;
+    if (pass == 0) {
+      line = at;
+      share = max((line + p.shares - 1) / p.shares, (uint64_t)p.least);
     }
-    __syncthreads();
-    if (s_found) break;
-    if (threadIdx.x == kThreads - 1) s_sums[0] = items1, s_work[0] = slots1;
-    __syncthreads();
-    items0 = s_sums[0];
-    slots0 = (uint32_t)s_work[0];
-    __syncthreads();
   }
-  if (!s_found) return false;
-  // the same for all: into scalar registers
-  auto one = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
-  item.request = one(s_item.request);
-  item.tile = one(s_item.tile);
-  item.part = one(s_item.part);
-  item.parts = one(s_item.parts);
-  item.slot = one(s_item.slot);
-  item.c = one(s_item.c);
-  item.r.start = (int32_t)one((uint32_t)s_item.r.start);
-  item.r.added = (int32_t)one((uint32_t)s_item.r.added);
-  item.r.len = (int32_t)one((uint32_t)s_item.r.len);
-  item.r.prefix = (int32_t)one((uint32_t)s_item.r.prefix);
+  if (s_found[0] == ~0u) return false;
+  item.request = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_found[0]);
+  item.tile = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_found[1]);
+  item.begin = one(s_begin);
+  item.line = one(line);
+  item.share = one(share);
+  item.r = one(request_of(p, item.request));
+  item.tiles = tiles_of(p, item.r);
   return true;
 }
 
-// Rows of a tile: row n is token n / group of the request's new ones, head
-// n % group of the key head's.
-struct Tile {
-  uint32_t row0, rows;    // first row, rows
-  int32_t first, last;    // positions of its first and last token
+// The tile after w's on the line, if the line goes on.
+__device__ __forceinline__ bool next_item(const AttendParams &p, WorkItem &w, uint64_t begin) {
+  w.begin = begin;
+  if (++w.tile < w.tiles) return true;
+  w.tile = 0;
+  do {
+    if (++w.request >= p.requests) return false;
+    w.r = one(request_of(p, w.request));
+    w.tiles = tiles_of(p, w.r);
+  } while (w.tiles == 0);
+  return true;
+}
+
+// What a workgroup computes of a tile: blocks from..upto - 1 of the tile.
+struct Part {
+  uint32_t from, upto;
+  uint32_t slot;
+  bool divided;
 };
 
-__device__ __forceinline__ Tile tile_of(const AttendParams &p, const WorkItem &w) {
-  Tile t;
-  const uint32_t all = (uint32_t)w.r.added * p.group.d;
-  t.row0 = w.tile * p.rows;
-  t.rows = min(p.rows, all - t.row0);
-  const int32_t base = w.r.len - w.r.added;
-  t.first = base + (int32_t)fastdiv(t.row0, p.group);
-  t.last = base + (int32_t)fastdiv(t.row0 + t.rows - 1, p.group);
-  return t;
+__device__ __forceinline__ Part part_of(const WorkItem &w, uint32_t blocks, uint32_t index) {
+  const uint64_t begin = index * w.share, end = min(begin + w.share, w.line);
+  Part a;
+  a.from = (uint32_t)(max(begin, w.begin) - w.begin);
+  a.upto = (uint32_t)(min(end, w.begin + blocks) - w.begin);
+  a.divided = a.from > 0 || a.upto < blocks;
+  a.slot = index * 2 + (w.begin > begin ? 1 : 0);
+  return a;
 }
 
 // One lane's look at a key's table entry.  What it loads is judged where it is needed, a block
@@ -472,6 +488,15 @@ __device__ __forceinline__ f32x4 not_finite_part(u32x4 a, u32x4 seen) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = not_finite_sum(up[i], down[i]);
   return r;
+}
+
+// f(0), f(1), .. f(n - 1) with numbers that are constants.
+template <int n, int i = 0, typename F>
+__device__ __forceinline__ void each(F &&f) {
+  if constexpr (i < n) {
+    f(std::integral_constant<int, i>{});
+    each<n, i + 1>(static_cast<F &&>(f));
+  }
 }
 
 // LDS written by some lanes of a wave and read by others of the same wave:

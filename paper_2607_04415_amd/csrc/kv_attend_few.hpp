@@ -32,7 +32,8 @@ constexpr int kFewBlock = 32;  // keys
 // kSteps: 32-element steps of a head, D <= 32 kSteps.  k8: pages of 8-bit values.
 // kMore: scores are capped or biased.
 template <typename Q, bool k8, int kSteps, bool kMore>
-__global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
+__device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
+                                         const KeyRange &range, const Part &part, uint32_t head) {
   constexpr int kHalves = (kSteps + 3) / 4;  // 128 elements of a value
   constexpr int kDim = kHalves * 128;
   constexpr int kPad = kDim + 4;
@@ -41,16 +42,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
   __shared__ float s_o[kFewWaves][kFewRows][kPad];
   __shared__ float s_m[kFewWaves][kFewRows], s_l[kFewWaves][kFewRows];
 
-  uint32_t head, index;
-  index = fastdiv(blockIdx.x, p.by_kv);
-  head = blockIdx.x - index * p.kv_heads;
-  WorkItem w;
-  if (!find_item<kFewThreads, kFewBlock, false>(p, index, w)) return;
-  const Tile tile = tile_of(p, w);
-  const KeyRange range = key_range<kFewBlock>(p, w.r, tile.first, tile.last);
-  const uint32_t parts = max(((uint32_t)range.count + w.c - 1) / w.c, 1u);  // of this tile
-  if (w.part >= parts) return;
-  const int32_t x_end = min((int64_t)range.count, (int64_t)(w.part + 1) * w.c);
+  const int32_t x_end = min(range.count, (int32_t)part.upto);
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
@@ -116,7 +108,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
       v[i] = *reinterpret_cast<const Raw *>(at);
     }
   };
-  int32_t x = (int32_t)(w.part * w.c) + wave;
+  int32_t x = (int32_t)part.from + wave;
   int turn = 0;
   Raw k[2][kSteps];
   uint32_t there = hand_out(place_of(x), 0);
@@ -252,9 +244,9 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
   const uint32_t tk = fastdiv(tile.row0 + row, p.group), hq = head * p.group.d + (tile.row0 + row - tk * p.group.d);
   const uint64_t t_out = (uint64_t)(w.r.start + tk);
   const float vs = p.value_scale ? p.value_scale[head] : 1.f;
-  const bool divided = parts > 1;
+  const bool divided = part.divided;
   const float norm = divided ? 1.f : all != 0.f ? vs / all : 0.f;
-  const uint64_t slot = ((uint64_t)w.slot * p.kv_heads + head) * kFewRows + row;
+  const uint64_t slot = ((uint64_t)part.slot * p.kv_heads + head) * kFewRows + row;
 #pragma unroll
   for (int h = 0; h < kHalves; ++h) {
     const uint32_t d = h * 128 + (threadIdx.x & 15) * 8;
@@ -278,7 +270,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
   }
   if ((threadIdx.x & 15) == 0) {
     if (divided) {
-      float *ml = p.parts + (uint64_t)p.part_slots * p.kv_heads * kFewRows * p.D + slot * 2;
+      float *ml = p.parts + (uint64_t)p.shares * 2 * p.kv_heads * kFewRows * p.D + slot * 2;
       ml[0] = most;
       ml[1] = all;
     } else if (p.lse) {
@@ -287,43 +279,86 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
   }
 }
 
-// Joins the parts of divided tiles: a block a tile and head, 16 threads a row.
+template <typename Q, bool k8, int kSteps, bool kMore>
+__global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
+  const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
+  WorkItem w;
+  if (!find_item<kFewThreads, kFewBlock, false>(p, index, w)) return;
+  for (;;) {
+    const Tile tile = tile_of(p, w.r, w.tile);
+    const KeyRange range = key_range<kFewBlock>(p, w.r, tile.first, tile.last);
+    const uint32_t blocks = (uint32_t)max(range.count, 1);
+    few_part<Q, k8, kSteps, kMore>(p, w, tile, range, part_of(w, blocks, index), head);
+    const uint64_t end = w.begin + blocks;
+    if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end)) return;
+    __syncthreads();  // the next tile's sums go where this one's are read
+  }
+}
+
+// Joins the parts of divided tiles: a workgroup a tile and head, 16 threads a row.
 template <typename Q, int kRows, int kBlock>
 __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
   if (!find_item<256, kBlock, true>(p, index, w)) return;
-  const Tile tile = tile_of(p, w);
-  const KeyRange range = key_range<kBlock>(p, w.r, tile.first, tile.last);
-  const uint32_t parts = ((uint32_t)range.count + w.c - 1) / w.c;
-  if (parts <= 1) return;  // written by its one part
-  const float *ml0 = p.parts + (uint64_t)p.part_slots * p.kv_heads * kRows * p.D;
+  const uint64_t end = w.begin + blocks_of<kBlock>(p, w.r, w.tile);
+  const uint32_t s0 = (uint32_t)(w.begin / w.share), s1 = (uint32_t)((end - 1) / w.share);
+  if (s0 == s1) return;  // written by its one part
+  const Tile tile = tile_of(p, w.r, w.tile);
+  const uint32_t parts = s1 - s0 + 1, lane = threadIdx.x & 15;
+  const uint32_t slot0 = s0 * 2 + (w.begin > s0 * w.share ? 1 : 0);  // of the first part; the others begin their shares
+  const float *ml = p.parts + (uint64_t)p.shares * 2 * p.kv_heads * kRows * p.D;
+  const float vs = p.value_scale ? p.value_scale[head] : 1.f;
   for (uint32_t row = threadIdx.x >> 4; row < tile.rows; row += 16) {
-    auto slot = [&](uint32_t i) __attribute__((always_inline)) { return ((uint64_t)(w.slot + i) * p.kv_heads + head) * kRows + row; };
+    auto slot = [&](uint32_t i) {
+      return ((uint64_t)(i ? (s0 + i) * 2 : slot0) * p.kv_heads + head) * kRows + row;
+    };
     float most = -INFINITY;
-    for (uint32_t i = 0; i < parts; ++i) most = fmaxf(most, ml0[slot(i) * 2]);
+    for (uint32_t i = lane; i < parts; i += 16) most = fmaxf(most, ml[slot(i) * 2]);
+#pragma unroll
+    for (int d = 8; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
     const float from = most == -INFINITY ? 0.f : most;
+    f32x4 y[4];  // 8 elements, and 8 more of a head past 128
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float all = 0.f;
-    for (uint32_t i = 0; i < parts; ++i) all += ml0[slot(i) * 2 + 1] * pow2(ml0[slot(i) * 2] - from);
-    const float vs = p.value_scale ? p.value_scale[head] : 1.f;
+    const uint32_t d0 = lane * 8, d1 = d0 + 128;
+    for (uint32_t i0 = 0; i0 < parts; i0 += 16) {
+      float by = 0.f;  // of part i0 + lane
+      if (i0 + lane < parts) {
+        const uint64_t at = slot(i0 + lane) * 2;
+        by = pow2(ml[at] - from);
+        all = fmaf(ml[at + 1], by, all);
+      }
+      const uint32_t upto = min(parts - i0, 16u);
+#pragma unroll 4
+      for (uint32_t i = 0; i < upto; ++i) {
+        const float one = __shfl(by, (int)i, 16);
+        const float *o = p.parts + slot(i0 + i) * p.D;
+        if (d0 < p.D) {
+          y[0] += *reinterpret_cast<const f32x4 *>(o + d0) * one;
+          y[1] += *reinterpret_cast<const f32x4 *>(o + d0 + 4) * one;
+        }
+        if (d1 < p.D) {
+          y[2] += *reinterpret_cast<const f32x4 *>(o + d1) * one;
+          y[3] += *reinterpret_cast<const f32x4 *>(o + d1 + 4) * one;
+        }
+      }
+    }
+#pragma unroll
+    for (int d = 8; d; d >>= 1) all += __shfl_xor(all, d);
     const float norm = all != 0.f ? vs / all : 0.f;
     const uint32_t tk = fastdiv(tile.row0 + row, p.group), hq = head * p.group.d + (tile.row0 + row - tk * p.group.d);
     const uint64_t t_out = (uint64_t)(w.r.start + tk);
-    for (uint32_t d = (threadIdx.x & 15) * 8; d < p.D; d += 128) {
-      f32x4 y[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-      for (uint32_t i = 0; i < parts; ++i) {
-        const float by = pow2(ml0[slot(i) * 2] - from);
-        const f32x4 *o = reinterpret_cast<const f32x4 *>(p.parts + slot(i) * p.D + d);
-        y[0] += o[0] * by;
-        y[1] += o[1] * by;
-      }
-      y[0] *= norm;
-      y[1] *= norm;
-      *reinterpret_cast<u32x4 *>(p.out + t_out * p.out_stride + (uint64_t)hq * p.D + d) =
-          u32x4{Q::pack(y[0].x, y[0].y), Q::pack(y[0].z, y[0].w), Q::pack(y[1].x, y[1].y), Q::pack(y[1].z, y[1].w)};
+    uint16_t *out = p.out + t_out * p.out_stride + (uint64_t)hq * p.D;
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      const uint32_t d = i ? d1 : d0;
+      if (d >= p.D) continue;
+      const f32x4 a = y[i] * norm, b = y[i + 1] * norm;
+      *reinterpret_cast<u32x4 *>(out + d) = u32x4{Q::pack(a.x, a.y), Q::pack(a.z, a.w), Q::pack(b.x, b.y), Q::pack(b.z, b.w)};
     }
-    if (p.lse && (threadIdx.x & 15) == 0)
-      p.lse[t_out * p.heads + hq] = all != 0.f ? (from + __log2f(all)) * kLn2 : -INFINITY;
+    if (p.lse && lane == 0) p.lse[t_out * p.heads + hq] = all != 0.f ? (from + __log2f(all)) * kLn2 : -INFINITY;
   }
 }
 

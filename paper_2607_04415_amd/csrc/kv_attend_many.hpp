@@ -25,9 +25,9 @@
 
 namespace gorio {
 
-constexpr int kManyWaves = 4;
-constexpr int kManyThreads = kManyWaves * 64;
-constexpr int kManyRows = kManyWaves * 32;
+// Waves of a workgroup, 32 rows each.
+__host__ __device__ constexpr int many_waves(int steps) { return steps == 4 ? 8 : 4; }
+__host__ __device__ constexpr int many_rows(int steps) { return many_waves(steps) * 32; }
 constexpr int kManyBlock = 64;  // keys
 
 // A maximum is kept until a score passes it by 2^8 (weights stay far inside
@@ -42,7 +42,9 @@ __device__ __forceinline__ uint64_t low_bits(int32_t n) {
 
 // kSteps: D <= 32 kSteps.  k8: pages of 8-bit values.  kMore: scores are capped or biased.
 template <typename Q, bool k8, int kSteps, bool kMore>
-__global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : kSteps > 2 ? 2 : 3) void attend_many(AttendParams p) {
+__device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
+                                          const KeyRange &range, const Part &part, uint32_t head) {
+  constexpr int kManyWaves = many_waves(kSteps), kManyThreads = kManyWaves * 64, kManyRows = kManyWaves * 32;
   constexpr int kDim = kSteps * 32, kChunks = kDim / 8;                              // 16-byte pieces of a row
   constexpr int kPasses = kManyBlock * kChunks / kManyThreads;                       // pieces a thread
   static_assert(kPasses * kManyThreads == kManyBlock * kChunks, "pieces divide");
@@ -54,23 +56,16 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : kSteps > 2 ? 2 : 3) 
   typedef typename std::conditional<k8, u32x2, u32x4>::type Raw;
   constexpr uint32_t kKeyBytes = kManyBlock * kKeyRow * 2, kValueBytes = kManyBlock * kValueRow * 2;
   __shared__ __align__(1024) uint8_t s_kv[2 * (kKeyBytes + kValueBytes)];  // keys, keys, values, values
-  __shared__ uint64_t s_row[4][2][kManyBlock];  // block, keys or values
-  __shared__ uint64_t s_there[4];
+  constexpr int kRing = kManyWaves * 2;                 // blocks
+  __shared__ uint64_t s_row[kRing][2][kManyBlock];      // block, keys or values
+  __shared__ uint64_t s_there[kRing];
   // Values that are NaN or inf in a block that not all rows see: a weight of 0 would not keep
   // them out of a row.  They are 0 in s_kv; here are the keys that have one at an element,
   // +inf (or NaN) and -inf (or NaN).
   __shared__ uint64_t s_odd[2][kDim];
   __shared__ uint32_t s_any_odd[kManyWaves];
 
-  const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
-  WorkItem w;
-  if (!find_item<kManyThreads, kManyBlock, false>(p, index, w)) return;
-  const Tile tile = tile_of(p, w);
-  const KeyRange range = key_range<kManyBlock>(p, w.r, tile.first, tile.last);
-  const uint32_t parts = max(((uint32_t)range.count + w.c - 1) / w.c, 1u);
-  if (w.part >= parts) return;
-  const int32_t x0 = (int32_t)(w.part * w.c);
-  const int32_t x_end = (int32_t)min((int64_t)range.count, (int64_t)x0 + w.c);
+  const int32_t x0 = (int32_t)part.from, x_end = min(range.count, (int32_t)part.upto);
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 31, g = lane >> 5;
@@ -112,10 +107,10 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : kSteps > 2 ? 2 : 3) 
   auto hand_out = [&](const KeyLook &k, int32_t x) __attribute__((always_inline)) {
     const bool there = key_there(p, k);
     const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
-    s_row[x & 3][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : zeros;
-    s_row[x & 3][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : zeros;
+    s_row[x & (kRing - 1)][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : zeros;
+    s_row[x & (kRing - 1)][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : zeros;
     const uint64_t bits = __ballot(there);
-    if (lane == 0) s_there[x & 3] = bits;
+    if (lane == 0) s_there[x & (kRing - 1)] = bits;
   };
   // Every row of the tile sees every key of block x that is there, by its position.
   auto all_see = [&](int32_t x) __attribute__((always_inline)) {
@@ -136,7 +131,7 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : kSteps > 2 ? 2 : 3) 
   // The values of block x and the keys half a block later: 32.. of block x, ..31 of x + 1.
   auto row_of = [&](int32_t x, int kv, int i) __attribute__((always_inline)) -> uint64_t {
     const uint32_t key = ((i * kManyWaves + wave) * 64 + lane) / kChunks;
-    return kv ? s_row[x & 3][1][key] : s_row[(x + (key >> 5)) & 3][0][key ^ 32];
+    return kv ? s_row[x & (kRing - 1)][1][key] : s_row[(x + (key >> 5)) & (kRing - 1)][0][key ^ 32];
   };
   const bool whole_rows = p.D == kDim;
   auto load_row = [&](uint64_t row, int kv, int i, uint32_t to, bool whole) __attribute__((always_inline)) {
@@ -262,22 +257,23 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : kSteps > 2 ? 2 : 3) 
     constexpr uint32_t kFar = kFrom + kSixteen > 65535 ? kFrom : 0;  // an instruction's offset has 16 bits
     // held as they are: the addresses made of them would cost registers
     asm volatile("" : "+v"(key_at), "+v"(value_at[0]), "+v"(value_at[1]));
-    u32x4 kf[4], vf[2][kTiles];  // keys: four steps ahead; values: all, or half of 256 elements
+    u32x4 kf[4], vf[2][kTiles];  // keys: four steps ahead; values: sixteen keys ahead
     __builtin_amdgcn_sched_barrier(0);
     auto read_keys = [&](int k) __attribute__((always_inline)) {
       kf[k & 3] = *lds_at<u32x4>(beside(key_at, k * 32) + decltype(keys)::value);
     };
-    auto read_values = [&](int u) __attribute__((always_inline)) {
+    auto read_values = [&](auto turn) __attribute__((always_inline)) {  // elements outside, keys inside
+      constexpr int u = decltype(turn)::value / 2, i = decltype(turn)::value % 2;
       uint32_t at[kTiles][2];
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
 #pragma unroll
         for (int h = 0; h < 2; ++h) at[t][h] = beside(value_at[h], (u * kTiles + t) * 64) + kFar;
-      read_transposed<kTiles, kFrom - kFar, kSixteen>(at, vf);
+      read_transposed<kTiles, kFrom - kFar + i * kSixteen>(at, vf[i]);
     };
 #pragma unroll
     for (int k = 0; k < 4; ++k) read_keys(k);
-    if constexpr (kTurns == 1) read_values(0);
+    read_values(std::integral_constant<int, 0>{});
     __builtin_amdgcn_sched_barrier(0);
     prepare(s);
     const float from = best == -INFINITY ? 0.f : best;
@@ -298,15 +294,21 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : kSteps > 2 ? 2 : 3) 
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    auto values_turn = [&](auto turn) __attribute__((always_inline)) {
+      constexpr int u = decltype(turn)::value / 2, i = decltype(turn)::value % 2;
 #pragma unroll
-    for (int u = 0; u < kTurns; ++u) {
-      if constexpr (kTurns > 1) read_values(u);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) o[u * kTiles + t] = Q::mfma32(vf[i][t], weights[i], o[u * kTiles + t]);
+      for (int t = 0; t < kTiles; ++t) o[u * kTiles + t] = Q::mfma32(vf[i][t], weights[i], o[u * kTiles + t]);
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (decltype(turn)::value + 1 < 2 * kTurns)
+        read_values(std::integral_constant<int, decltype(turn)::value + 1>{});
+    };
+    values_turn(std::integral_constant<int, 0>{});
+    values_turn(std::integral_constant<int, 1>{});
+    if constexpr (kTurns > 1) {
+      values_turn(std::integral_constant<int, 2>{});
+      values_turn(std::integral_constant<int, 3>{});
     }
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   // Block x, the scores of whose first 32 keys are in `now`, up to those of block x + 1.  The
@@ -319,16 +321,16 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : kSteps > 2 ? 2 : 3) 
     constexpr int kNow = decltype(turn)::value, kNext = 1 - kNow;
     constexpr uint32_t k_now = kKeys[kNow], k_next = kKeys[kNext], v_now = kValues[kNow], v_next = kValues[kNext];
     const bool more = x + 1 < x_end;
-    if (wave == 0) {
-      hand_out(ahead, x + 3);
-      ahead = look_up(x + 4);
+    if (((x - x0) & (kManyWaves - 1)) == 0) {  // a block a wave, for the steps up to the next such
+      hand_out(ahead, x + 3 + wave);
+      ahead = look_up(x + 3 + kManyWaves + wave);
     }
     if (more) {
       load(x + 1, 0, k_next);
       load(x + 1, 1, v_next);
     }
     const int32_t j0 = range.block(x) * kManyBlock;
-    const uint64_t bits = s_there[x & 3];  // the same for all
+    const uint64_t bits = s_there[x & (kRing - 1)];  // the same for all
     const uint64_t there = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32 |
                            (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bits);
     bool odd = false;
@@ -382,11 +384,8 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : kSteps > 2 ? 2 : 3) 
   };
 
   for (uint32_t i = threadIdx.x; i < 2 * kDim; i += kManyThreads) (&s_odd[0][0])[i] = 0;
-  if (wave == 0) {
-#pragma unroll
-    for (int i = -1; i < 3; ++i) hand_out(look_up(x0 + i), x0 + i);
-    ahead = look_up(x0 + 3);
-  }
+  for (int i = wave; i < 4; i += kManyWaves) hand_out(look_up(x0 - 1 + i), x0 - 1 + i);
+  ahead = look_up(x0 + 3 + wave);
   __syncthreads();
   if (x0 < x_end) {
     load(x0 - 1, 0, kKeys[1]);
@@ -417,11 +416,11 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : kSteps > 2 ? 2 : 3) 
 
   sum = xor32(sum, sum_of);
   if ((uint32_t)wave * 32 + m >= tile.rows) return;
-  const bool divided = parts > 1;
+  const bool divided = part.divided;
   const uint64_t t_out = (uint64_t)(w.r.start + token);
   const float vs = p.value_scale ? p.value_scale[head] : 1.f;
   const float norm = divided ? 1.f : sum != 0.f ? vs / sum : 0.f;
-  const uint64_t slot = ((uint64_t)w.slot * p.kv_heads + head) * kManyRows + wave * 32 + m;
+  const uint64_t slot = ((uint64_t)part.slot * p.kv_heads + head) * kManyRows + wave * 32 + m;
 #pragma unroll
   for (int t = 0; t < kSteps; ++t)
 #pragma unroll
@@ -437,12 +436,28 @@ __global__ __launch_bounds__(kManyThreads, kSteps > 4 ? 1 : kSteps > 2 ? 2 : 3) 
     }
   if (g == 0) {
     if (divided) {
-      float *ml = p.parts + (uint64_t)p.part_slots * p.kv_heads * kManyRows * p.D + slot * 2;
+      float *ml = p.parts + (uint64_t)p.shares * 2 * p.kv_heads * kManyRows * p.D + slot * 2;
       ml[0] = best;
       ml[1] = sum;
     } else if (p.lse) {
       p.lse[t_out * p.heads + qhead] = sum != 0.f ? (best + __log2f(sum)) * kLn2 : -INFINITY;
     }
+  }
+}
+
+template <typename Q, bool k8, int kSteps, bool kMore>
+__global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps > 2 ? 2 : 3) void attend_many(AttendParams p) {
+  const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
+  WorkItem w;
+  if (!find_item<many_waves(kSteps) * 64, kManyBlock, false>(p, index, w)) return;
+  for (;;) {
+    const Tile tile = tile_of(p, w.r, w.tile);
+    const KeyRange range = key_range<kManyBlock>(p, w.r, tile.first, tile.last);
+    const uint32_t blocks = (uint32_t)max(range.count, 1);
+    many_part<Q, k8, kSteps, kMore>(p, w, tile, range, part_of(w, blocks, index), head);
+    const uint64_t end = w.begin + blocks;
+    if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end)) return;
+    __syncthreads();
   }
 }
 

@@ -7,11 +7,11 @@
 
 namespace gorio {
 
-// One form's launch: AttendParams' fields for the division of its work, blocks, and blocks
-// that join divided tiles (0: none are).
+// One form's launch: AttendParams' fields for the division of its work, and workgroups that
+// join divided tiles, a head (0: none are).
 struct AttendForm {
-  uint32_t rows, from, upto, least, most, part_slots;
-  uint32_t grid, join;
+  uint32_t rows, from, upto, shares, least;
+  uint32_t join;
 };
 
 struct AttendLaunch {
@@ -25,19 +25,18 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
     p.rows = f.rows;
     p.from = f.from;
     p.upto = f.upto;
+    p.shares = f.shares;
     p.least = f.least;
-    p.most = f.most;
-    p.part_slots = f.part_slots;
   };
-  if (l.few.grid) {
+  if (l.few.shares) {
     divide(l.few);
-    attend_few<Q, k8, kSteps, kMore><<<l.few.grid, kFewThreads, 0, s>>>(p);
-    if (l.few.join) attend_join<Q, kFewRows, kFewBlock><<<l.few.join, 256, 0, s>>>(p);
+    attend_few<Q, k8, kSteps, kMore><<<l.few.shares * p.kv_heads, kFewThreads, 0, s>>>(p);
+    if (l.few.join) attend_join<Q, kFewRows, kFewBlock><<<l.few.join * p.kv_heads, 256, 0, s>>>(p);
   }
-  if (l.many.grid) {
+  if (l.many.shares) {
     divide(l.many);
-    attend_many<Q, k8, kSteps, kMore><<<l.many.grid, kManyThreads, 0, s>>>(p);
-    if (l.many.join) attend_join<Q, kManyRows, kManyBlock><<<l.many.join, 256, 0, s>>>(p);
+    attend_many<Q, k8, kSteps, kMore><<<l.many.shares * p.kv_heads, many_waves(kSteps) * 64, 0, s>>>(p);
+    if (l.many.join) attend_join<Q, many_rows(kSteps), kManyBlock><<<l.many.join * p.kv_heads, 256, 0, s>>>(p);
   }
   return hipGetLastError();
 }
@@ -47,12 +46,17 @@ hipError_t launch_steps(const AttendParams &p, const AttendLaunch &l, hipStream_
   return l.more ? launch_forms<Q, k8, kSteps, true>(p, l, s) : launch_forms<Q, k8, kSteps, false>(p, l, s);
 }
 
+// 32-element steps of the kernels for a head of D elements.
+inline int steps_of(uint32_t D) { return D <= 64 ? 2 : D <= 96 ? 3 : D <= 128 ? 4 : 8; }
+
 template <typename Q, bool k8>
 hipError_t launch_pages(const AttendParams &p, const AttendLaunch &l, hipStream_t s) {
-  if (p.D <= 64) return launch_steps<Q, k8, 2>(p, l, s);
-  if (p.D <= 96) return launch_steps<Q, k8, 3>(p, l, s);
-  if (p.D <= 128) return launch_steps<Q, k8, 4>(p, l, s);
-  return launch_steps<Q, k8, 8>(p, l, s);
+  switch (steps_of(p.D)) {
+    case 2: return launch_steps<Q, k8, 2>(p, l, s);
+    case 3: return launch_steps<Q, k8, 3>(p, l, s);
+    case 4: return launch_steps<Q, k8, 4>(p, l, s);
+    default: return launch_steps<Q, k8, 8>(p, l, s);
+  }
 }
 
 hipError_t launch_attend_bf16(const AttendParams &p, const AttendLaunch &l, hipStream_t s);
