@@ -51,7 +51,6 @@ AttendForm divide(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t
   f.upto = 0xFFFFFFFFu;
   f.least = least;
   f.shares = (uint32_t)std::min<uint64_t>(std::max(all / c.heads, 1u), (tiles * blocks + least - 1) / least);
-  f.join = f.shares > 1 ? (uint32_t)std::min<uint64_t>(tiles, kKvMost / c.heads) : 0;
   return f;
 }
 
@@ -66,13 +65,13 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   const uint64_t others = (a.requests - 1) * most;
   const uint64_t fewest = a.tokens > others ? a.tokens - others : 1;
   const bool few = fewest * group < kFewUpto, many = most * group >= kFewUpto;
-  if (few) l.few = divide(c, a, kFewRows, kFewBlock, 4, 512, many);
   const int steps = steps_of(c.D);
+  if (few) l.few = divide(c, a, kFewRows, kFewBlock, 32, 256, many);
   if (many) l.many = divide(c, a, many_rows(steps), kManyBlock, 4, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
   if (few && many) l.few.upto = l.many.from = kFewUpto;
   const uint64_t slot = 2 * (c.D + 2) * sizeof(float) * c.heads;  // two parts of a share
-  *bytes = std::max<uint64_t>(l.few.join ? l.few.shares * kFewRows : 0,
-                              l.many.join ? (uint64_t)l.many.shares * many_rows(steps) : 0) * slot;
+  *bytes = std::max<uint64_t>(l.few.shares > 1 ? l.few.shares * kFewRows : 0,
+                              l.many.shares > 1 ? (uint64_t)l.many.shares * many_rows(steps) : 0) * slot;
   return l;
 }
 

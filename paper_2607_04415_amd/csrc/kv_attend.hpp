@@ -281,18 +281,25 @@ __device__ __forceinline__ Request one(const Request &r) {
                  __builtin_amdgcn_readfirstlane(r.len), __builtin_amdgcn_readfirstlane(r.prefix)};
 }
 
-// The tile in which share number `index` begins (kJoin: tile number `index`), or false if there
-// is none.  Every thread of the workgroup gets the same answer.
-template <int kThreads, int kBlock, bool kJoin>
+// The tile of the block that share number `index` begins with, or false if the line ends before.
+// Every thread of the workgroup gets the same answer.
+template <int kThreads, int kBlock>
 __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item) {
   __shared__ uint64_t s_sums[kThreads / 64], s_begin, s_line;
   __shared__ uint32_t s_tiles[kThreads], s_counts[kThreads / 64], s_found[2];  // request, tile
   if (threadIdx.x == 0) s_found[0] = ~0u;
   uint64_t line = 0, share = 0;
-  // twice over the tiles: W is known after the first pass, and the tile after the second
+  // this thread's tile, of the chunk last counted
+  uint64_t begin = 0, end = 0;
+  uint32_t request = 0, tile = 0;
+  bool once = true;  // there is one chunk only
+  auto take = [&]() {
+    const uint64_t at = (uint64_t)index * share;
+    if (at >= begin && at < end) s_found[0] = request, s_found[1] = tile, s_begin = begin;
+  };
+  // twice over the tiles, unless they are few: W is known after the first pass
   for (int pass = 0; pass < 2; ++pass) {
-    uint64_t at = 0;       // on the line, of the next tile
-    uint32_t number = 0;   // of it
+    uint64_t at = 0;  // on the line, of the next tile
     for (uint32_t b0 = 0; b0 < p.requests; b0 += kThreads) {
       const uint32_t b = b0 + threadIdx.x;
       const uint32_t mine = b < p.requests ? tiles_of(p, request_of(p, b)) : 0;
@@ -300,9 +307,10 @@ __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item)
       s_tiles[threadIdx.x] = upto;
       __syncthreads();
       const uint32_t tiles = s_tiles[kThreads - 1];
+      once &= p.requests <= kThreads && tiles <= kThreads;
       for (uint32_t f0 = 0; f0 < tiles; f0 += kThreads) {
         const uint32_t f = f0 + threadIdx.x;
-        uint32_t blocks = 0, r = 0, tile = 0;
+        uint32_t blocks = 0, r = 0;
         if (f < tiles) {
           uint32_t hi = kThreads - 1;  // the first request whose tiles reach past f
           while (r < hi) {
@@ -311,24 +319,27 @@ __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item)
             else r = mid + 1;
           }
           tile = f - (r ? s_tiles[r - 1] : 0);
-          blocks = blocks_of<kBlock>(p, request_of(p, b0 + r), tile);
+          request = b0 + r;
+          blocks = blocks_of<kBlock>(p, request_of(p, request), tile);
         }
-        const uint64_t end = at + scan_threads<kThreads>((uint64_t)blocks, s_sums), begin = end - blocks;
-        if (pass) {
-          const bool here = kJoin ? number + f == index : (uint64_t)index * share >= begin && (uint64_t)index * share < end;
-          if (f < tiles && here) s_found[0] = b0 + r, s_found[1] = tile, s_begin = begin;
-        }
+        end = at + scan_threads<kThreads>((uint64_t)blocks, s_sums);
+        begin = end - blocks;
+        if (pass) take();
         if (threadIdx.x == kThreads - 1) s_line = end;
         __syncthreads();
         at = s_line;
       }
-      number += tiles;
       __syncthreads();
       if (pass && s_found[0] != ~0u) break;
     }
     if (pass == 0) {
       line = at;
       share = max((line + p.shares - 1) / p.shares, (uint64_t)p.least);
+      if (once) {
+        take();
+        __syncthreads();
+        break;
+      }
     }
   }
   if (s_found[0] == ~0u) return false;

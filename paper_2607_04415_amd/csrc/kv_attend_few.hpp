@@ -3,7 +3,7 @@
 //
 // Every key and value is read once for 16 rows or fewer, far below what the
 // matrix units could do with it, so the rate at which HBM gives them is the
-// bound.  Four waves share a part of the keys, 32 at a time each; a wave keeps
+// bound.  Eight waves share a part of the keys, 32 at a time each; a wave keeps
 // its own running maximum, sum and output, joined in LDS at the end, so no
 // wave waits for another in between.  Keys and values go from memory straight
 // into the operands of the matrix instructions (16x16x32):
@@ -24,8 +24,8 @@
 
 namespace gorio {
 
-constexpr int kFewThreads = 256;
-constexpr int kFewWaves = kFewThreads / 64;
+// Waves of a workgroup; 256 elements take the registers of twice as many.
+__host__ __device__ constexpr int few_waves(int steps) { return steps > 4 ? 4 : 8; }
 constexpr int kFewRows = 16;
 constexpr int kFewBlock = 32;  // keys
 
@@ -34,6 +34,7 @@ constexpr int kFewBlock = 32;  // keys
 template <typename Q, bool k8, int kSteps, bool kMore>
 __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
                                          const KeyRange &range, const Part &part, uint32_t head) {
+  constexpr int kFewWaves = few_waves(kSteps), kFewThreads = kFewWaves * 64;
   constexpr int kHalves = (kSteps + 3) / 4;  // 128 elements of a value
   constexpr int kDim = kHalves * 128;
   constexpr int kPad = kDim + 4;
@@ -108,34 +109,30 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
       v[i] = *reinterpret_cast<const Raw *>(at);
     }
   };
-  int32_t x = (int32_t)part.from + wave;
-  int turn = 0;
-  Raw k[2][kSteps];
-  uint32_t there = hand_out(place_of(x), 0);
-  load_keys(k, 0);
-  KeyLook next = place_of(x + kFewWaves);
-  for (; x < x_end; x += kFewWaves) {
+  // Block x, with the next one's keys and values on their way; the registers alternate.
+  Raw k[2][2][kSteps], v[2][kHalves][8];
+  uint32_t there[2];
+  KeyLook next;
+  auto load = [&](auto turn) __attribute__((always_inline)) {
+    constexpr int t = decltype(turn)::value;
+    load_keys(k[t], t);
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) load_values(v[t][h], h, t);
+  };
+  auto step = [&](int32_t x, auto turn) __attribute__((always_inline)) {
+    constexpr int t0 = decltype(turn)::value, t1 = 1 - t0;
     const int32_t j0 = range.block(x) * kFewBlock;
-    const uint32_t there_now = there;
-    there = hand_out(next, turn ^ 1);
+    const uint32_t there_now = there[t0];
+    there[t1] = hand_out(next, t1);
     next = place_of(x + 2 * kFewWaves);
-    Raw v[kHalves][8];
-#pragma unroll
-    for (int h = 0; h < kHalves; ++h) load_values(v[h], h, turn);
-    // the next block's keys are on their way during this one's products
-    u32x4 kw[2][kSteps];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) kw[i][s] = widened<Q>(k[i][s]);
-    load_keys(k, turn ^ 1);
+    load(std::integral_constant<int, t1>{});
 
     f32x4 s2[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       s2[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) s2[i] = Q::mfma16(kw[i][s], q[s], s2[i]);
+      for (int s = 0; s < kSteps; ++s) s2[i] = Q::mfma16(widened<Q>(k[t0][i][s]), q[s], s2[i]);
     }
     float e[8];
 #pragma unroll
@@ -190,7 +187,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     for (int h = 0; h < kHalves; ++h) {
       u32x4 vw[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) vw[i] = widened<Q>(v[h][i]);
+      for (int i = 0; i < 8; ++i) vw[i] = widened<Q>(v[t0][h][i]);
       // A weight of 0 keeps a value out of a row, unless the value is NaN or inf.  Such
       // values in a block that some rows see only in part go in apart from the others.
       bool odd = false;
@@ -212,10 +209,19 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
         o[h * 8 + t] = Q::mfma16(a, weights, o[h * 8 + t]);
       }
     }
-    turn ^= 1;
+  };
+  int32_t x = (int32_t)part.from + wave;
+  there[0] = hand_out(place_of(x), 0);
+  next = place_of(x + kFewWaves);
+  load(std::integral_constant<int, 0>{});
+  while (x < x_end) {
+    step(x, std::integral_constant<int, 0>{});
+    if ((x += kFewWaves) >= x_end) break;
+    step(x, std::integral_constant<int, 1>{});
+    x += kFewWaves;
   }
 
-  // the four waves' results, joined
+  // the waves' results, joined
   sum = xor16(xor32(sum, sum_of), sum_of);
   if (g == 0) s_m[wave][m] = best, s_l[wave][m] = sum;
 #pragma unroll
@@ -229,16 +235,17 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
             f32x4{o[h * 8 + t][r], o[h * 8 + t + 1][r], o[h * 8 + t + 2][r], o[h * 8 + t + 3][r]};
     }
   __syncthreads();
-  const uint32_t row = threadIdx.x >> 4;
+  constexpr int kRowThreads = kFewThreads / kFewRows, kOwn = 128 / kRowThreads;  // elements of each 128
+  const uint32_t row = threadIdx.x / kRowThreads, at = threadIdx.x % kRowThreads;
   if (row >= tile.rows) return;
   float most = s_m[0][row];
 #pragma unroll
   for (int i = 1; i < kFewWaves; ++i) most = fmaxf(most, s_m[i][row]);
-  const float from = most == -INFINITY ? 0.f : most;
+  const float base = most == -INFINITY ? 0.f : most;
   float by[kFewWaves], all = 0.f;
 #pragma unroll
   for (int i = 0; i < kFewWaves; ++i) {
-    by[i] = pow2(s_m[i][row] - from);
+    by[i] = pow2(s_m[i][row] - base);
     all += s_l[i][row] * by[i];
   }
   const uint32_t tk = fastdiv(tile.row0 + row, p.group), hq = head * p.group.d + (tile.row0 + row - tk * p.group.d);
@@ -249,41 +256,41 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   const uint64_t slot = ((uint64_t)part.slot * p.kv_heads + head) * kFewRows + row;
 #pragma unroll
   for (int h = 0; h < kHalves; ++h) {
-    const uint32_t d = h * 128 + (threadIdx.x & 15) * 8;
+    const uint32_t d = h * 128 + at * kOwn;
     if (d >= p.D) break;
-    float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      y[i] = 0.f;
+    for (int i = 0; i < kOwn; i += 4) {
+      f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < kFewWaves; ++j) y[i] = fmaf(s_o[j][row][d + i], by[j], y[i]);
-      y[i] *= norm;
-    }
-    if (divided) {
-      float *to = p.parts + slot * p.D + d;
-      *reinterpret_cast<f32x4 *>(to) = f32x4{y[0], y[1], y[2], y[3]};
-      *reinterpret_cast<f32x4 *>(to + 4) = f32x4{y[4], y[5], y[6], y[7]};
-    } else {
-      *reinterpret_cast<u32x4 *>(p.out + t_out * p.out_stride + (uint64_t)hq * p.D + d) =
-          u32x4{Q::pack(y[0], y[1]), Q::pack(y[2], y[3]), Q::pack(y[4], y[5]), Q::pack(y[6], y[7])};
+      for (int j = 0; j < kFewWaves; ++j) {
+        const f32x4 o4 = *reinterpret_cast<const f32x4 *>(&s_o[j][row][d + i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = fmaf(o4[e], by[j], y[e]);
+      }
+      y *= norm;
+      if (divided)
+        *reinterpret_cast<f32x4 *>(p.parts + slot * p.D + d + i) = y;
+      else
+        *reinterpret_cast<u32x2 *>(p.out + t_out * p.out_stride + (uint64_t)hq * p.D + d + i) =
+            u32x2{Q::pack(y.x, y.y), Q::pack(y.z, y.w)};
     }
   }
-  if ((threadIdx.x & 15) == 0) {
+  if (at == 0) {
     if (divided) {
       float *ml = p.parts + (uint64_t)p.shares * 2 * p.kv_heads * kFewRows * p.D + slot * 2;
       ml[0] = most;
       ml[1] = all;
     } else if (p.lse) {
-      p.lse[t_out * p.heads + hq] = all != 0.f ? (from + __log2f(all)) * kLn2 : -INFINITY;
+      p.lse[t_out * p.heads + hq] = all != 0.f ? (base + __log2f(all)) * kLn2 : -INFINITY;
     }
   }
 }
 
 template <typename Q, bool k8, int kSteps, bool kMore>
-__global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
+__global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
-  if (!find_item<kFewThreads, kFewBlock, false>(p, index, w)) return;
+  if (!find_item<few_waves(kSteps) * 64, kFewBlock>(p, index, w)) return;
   for (;;) {
     const Tile tile = tile_of(p, w.r, w.tile);
     const KeyRange range = key_range<kFewBlock>(p, w.r, tile.first, tile.last);
@@ -295,21 +302,23 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(AttendParams p) {
   }
 }
 
-// Joins the parts of divided tiles: a workgroup a tile and head, 16 threads a row.
+// Joins the parts of divided tiles: a workgroup a share (but the first) and head.  It joins the
+// tile that the share begins in, if the tile begins in the share before; 64 rows, 16 threads a row.
 template <typename Q, int kRows, int kBlock>
 __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
-  const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
+  const uint32_t before = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - before * p.kv_heads, index = before + 1;
   WorkItem w;
-  if (!find_item<256, kBlock, true>(p, index, w)) return;
+  if (!find_item<256, kBlock>(p, index, w)) return;
+  if (w.begin == index * w.share || w.begin < before * w.share) return;  // not cut here, or not first here
   const uint64_t end = w.begin + blocks_of<kBlock>(p, w.r, w.tile);
-  const uint32_t s0 = (uint32_t)(w.begin / w.share), s1 = (uint32_t)((end - 1) / w.share);
-  if (s0 == s1) return;  // written by its one part
+  const uint32_t s0 = before, s1 = (uint32_t)((end - 1) / w.share);
   const Tile tile = tile_of(p, w.r, w.tile);
   const uint32_t parts = s1 - s0 + 1, lane = threadIdx.x & 15;
   const uint32_t slot0 = s0 * 2 + (w.begin > s0 * w.share ? 1 : 0);  // of the first part; the others begin their shares
   const float *ml = p.parts + (uint64_t)p.shares * 2 * p.kv_heads * kRows * p.D;
   const float vs = p.value_scale ? p.value_scale[head] : 1.f;
-  for (uint32_t row = threadIdx.x >> 4; row < tile.rows; row += 16) {
+  const uint32_t upto = min(tile.rows, blockIdx.y * 64 + 64);
+  for (uint32_t row = blockIdx.y * 64 + (threadIdx.x >> 4); row < upto; row += 16) {
     auto slot = [&](uint32_t i) {
       return ((uint64_t)(i ? (s0 + i) * 2 : slot0) * p.kv_heads + head) * kRows + row;
     };
@@ -330,9 +339,9 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
         by = pow2(ml[at] - from);
         all = fmaf(ml[at + 1], by, all);
       }
-      const uint32_t upto = min(parts - i0, 16u);
+      const uint32_t some = min(parts - i0, 16u);
 #pragma unroll 4
-      for (uint32_t i = 0; i < upto; ++i) {
+      for (uint32_t i = 0; i < some; ++i) {
         const float one = __shfl(by, (int)i, 16);
         const float *o = p.parts + slot(i0 + i) * p.D;
         if (d0 < p.D) {

@@ -449,7 +449,7 @@ template <typename Q, bool k8, int kSteps, bool kMore>
 __global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps > 2 ? 2 : 3) void attend_many(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
-  if (!find_item<many_waves(kSteps) * 64, kManyBlock, false>(p, index, w)) return;
+  if (!find_item<many_waves(kSteps) * 64, kManyBlock>(p, index, w)) return;
   for (;;) {
     const Tile tile = tile_of(p, w.r, w.tile);
     const KeyRange range = key_range<kManyBlock>(p, w.r, tile.first, tile.last);
