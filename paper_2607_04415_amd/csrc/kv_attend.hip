@@ -42,7 +42,7 @@ constexpr uint32_t kFewUpto = 17;
 // return.  `all`: workgroups that run at once on the GPU.  one_tile: no
 // request that the form takes has more than one tile.
 AttendForm divide(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t rows, uint32_t block, uint32_t least,
-                  uint32_t all, bool one_tile) {
+                  uint32_t whole, uint32_t all, bool one_tile) {
   AttendForm f{};
   const uint64_t tiles = (one_tile ? 0 : a.tokens * (a.heads / c.heads) / rows) + std::min<uint64_t>(a.requests, a.tokens);
   const uint64_t blocks = ((uint64_t)a.width * c.page_tokens + block - 1) / block;
@@ -50,7 +50,9 @@ AttendForm divide(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t
   f.from = 1;
   f.upto = 0xFFFFFFFFu;
   f.least = least;
+  f.whole = whole;
   f.shares = (uint32_t)std::min<uint64_t>(std::max(all / c.heads, 1u), (tiles * blocks + least - 1) / least);
+  f.cuts = f.shares > 1 && blocks > whole;
   return f;
 }
 
@@ -66,12 +68,12 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   const uint64_t fewest = a.tokens > others ? a.tokens - others : 1;
   const bool few = fewest * group < kFewUpto, many = most * group >= kFewUpto;
   const int steps = steps_of(c.D);
-  if (few) l.few = divide(c, a, kFewRows, kFewBlock, 32, 256, many);
-  if (many) l.many = divide(c, a, many_rows(steps), kManyBlock, 4, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
+  if (few) l.few = divide(c, a, kFewRows, kFewBlock, 8, 16, 256, many);
+  if (many) l.many = divide(c, a, many_rows(steps), kManyBlock, 4, 8, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
   if (few && many) l.few.upto = l.many.from = kFewUpto;
   const uint64_t slot = 2 * (c.D + 2) * sizeof(float) * c.heads;  // two parts of a share
-  *bytes = std::max<uint64_t>(l.few.shares > 1 ? l.few.shares * kFewRows : 0,
-                              l.many.shares > 1 ? (uint64_t)l.many.shares * many_rows(steps) : 0) * slot;
+  *bytes = std::max<uint64_t>(l.few.cuts ? l.few.shares * kFewRows : 0,
+                              l.many.cuts ? (uint64_t)l.many.shares * many_rows(steps) : 0) * slot;
   return l;
 }
 

@@ -155,6 +155,7 @@ struct AttendParams {
   uint32_t rows;         // query rows of a tile
   uint32_t from, upto;   // requests with this many rows a key head, from <= rows < upto
   uint32_t shares, least;  // workgroups of a key head, at most; key blocks of a share, at least
+  uint32_t whole;          // key blocks of a tile that is not cut, at most
 };
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -206,10 +207,12 @@ __device__ __forceinline__ KeyRange key_range(const AttendParams &p, const Reque
 // tiles, one tile after the other, make a line of W blocks, and workgroup i of
 // the head takes an equal share of it: blocks i c .. (i + 1) c - 1, whatever
 // tiles they belong to.  So all workgroups run equally long, however ragged the
-// lengths, and a tile is cut only where a share ends in it.  What a workgroup
-// computes of a cut tile is a part: its sums go to the workspace, where it has
-// two slots (a share cuts at most the tile it begins in and the one it ends
-// in), and a second kernel joins them.
+// lengths, and a tile is cut only where a share ends in it.  A tile of up to
+// `whole` blocks is not cut but goes to the share it begins in: parts of so few
+// blocks would cost more than they save.  What a workgroup computes of a cut
+// tile is a part: its sums go to the workspace, where it has two slots (a share
+// cuts at most the tile it begins in and the one it ends in), and a second
+// kernel joins them.
 //
 // How long the requests are is known on the GPU only, so every workgroup finds
 // its share by itself: the tiles' blocks are counted and added up, in chunks of
@@ -287,22 +290,42 @@ template <int kThreads, int kBlock>
 __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item) {
   __shared__ uint64_t s_sums[kThreads / 64], s_begin, s_line;
   __shared__ uint32_t s_tiles[kThreads], s_counts[kThreads / 64], s_found[2];  // request, tile
+  __shared__ Request s_request;
   if (threadIdx.x == 0) s_found[0] = ~0u;
   uint64_t line = 0, share = 0;
   // this thread's tile, of the chunk last counted
   uint64_t begin = 0, end = 0;
   uint32_t request = 0, tile = 0;
+  Request its{};
   bool once = true;  // there is one chunk only
   auto take = [&]() {
     const uint64_t at = (uint64_t)index * share;
-    if (at >= begin && at < end) s_found[0] = request, s_found[1] = tile, s_begin = begin;
+    if (at >= begin && at < end) s_found[0] = request, s_found[1] = tile, s_begin = begin, s_request = its;
   };
   // twice over the tiles, unless they are few: W is known after the first pass
   for (int pass = 0; pass < 2; ++pass) {
     uint64_t at = 0;  // on the line, of the next tile
     for (uint32_t b0 = 0; b0 < p.requests; b0 += kThreads) {
       const uint32_t b = b0 + threadIdx.x;
-      const uint32_t mine = b < p.requests ? tiles_of(p, request_of(p, b)) : 0;
+      Request own{};
+      if (b < p.requests) own = request_of(p, b);
+      const uint32_t mine = b < p.requests ? tiles_of(p, own) : 0;
+      if (!__syncthreads_or(mine > 1)) {  // single tokens: a thread's request is its tile
+        request = b;
+        tile = 0;
+        its = own;
+        const uint32_t blocks = mine ? blocks_of<kBlock>(p, own, 0) : 0;
+        end = at + scan_threads<kThreads>((uint64_t)blocks, s_sums);
+        begin = end - blocks;
+        if (pass) take();
+        if (threadIdx.x == kThreads - 1) s_line = end;
+        __syncthreads();
+        at = s_line;
+        once &= p.requests <= kThreads;
+        __syncthreads();
+        if (pass && s_found[0] != ~0u) break;
+        continue;
+      }
       const uint32_t upto = scan_threads<kThreads>(mine, s_counts);
       s_tiles[threadIdx.x] = upto;
       __syncthreads();
@@ -320,7 +343,8 @@ __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item)
           }
           tile = f - (r ? s_tiles[r - 1] : 0);
           request = b0 + r;
-          blocks = blocks_of<kBlock>(p, request_of(p, request), tile);
+          its = request_of(p, request);
+          blocks = blocks_of<kBlock>(p, its, tile);
         }
         end = at + scan_threads<kThreads>((uint64_t)blocks, s_sums);
         begin = end - blocks;
@@ -348,7 +372,7 @@ __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item)
   item.begin = one(s_begin);
   item.line = one(line);
   item.share = one(share);
-  item.r = one(request_of(p, item.request));
+  item.r = one(s_request);
   item.tiles = tiles_of(p, item.r);
   return true;
 }
@@ -366,20 +390,24 @@ __device__ __forceinline__ bool next_item(const AttendParams &p, WorkItem &w, ui
   return true;
 }
 
-// What a workgroup computes of a tile: blocks from..upto - 1 of the tile.
+// What share number `index` computes of tile w: blocks from..upto - 1 of the tile, none if the
+// tile begins in the share before and is not cut.
 struct Part {
   uint32_t from, upto;
   uint32_t slot;
-  bool divided;
+  bool divided, none;
 };
 
-__device__ __forceinline__ Part part_of(const WorkItem &w, uint32_t blocks, uint32_t index) {
+__device__ __forceinline__ Part part_of(const AttendParams &p, const WorkItem &w, uint32_t blocks, uint32_t index) {
   const uint64_t begin = index * w.share, end = min(begin + w.share, w.line);
-  Part a;
-  a.from = (uint32_t)(max(begin, w.begin) - w.begin);
-  a.upto = (uint32_t)(min(end, w.begin + blocks) - w.begin);
-  a.divided = a.from > 0 || a.upto < blocks;
-  a.slot = index * 2 + (w.begin > begin ? 1 : 0);
+  Part a{0, blocks, index * 2 + (w.begin > begin ? 1 : 0), false, false};
+  if (blocks <= p.whole) {
+    a.none = w.begin < begin;
+  } else {
+    a.from = (uint32_t)(max(begin, w.begin) - w.begin);
+    a.upto = (uint32_t)(min(end, w.begin + blocks) - w.begin);
+    a.divided = a.from > 0 || a.upto < blocks;
+  }
   return a;
 }
 
@@ -508,6 +536,12 @@ __device__ __forceinline__ void each(F &&f) {
     f(std::integral_constant<int, i>{});
     each<n, i + 1>(static_cast<F &&>(f));
   }
+}
+
+// The low n bits, n of any size.
+__device__ __forceinline__ uint64_t low_bits(int32_t n) {
+  const uint64_t some = (1ull << (n & 63)) - 1;
+  return n <= 0 ? 0 : n >= 64 ? ~0ull : some;
 }
 
 // LDS written by some lanes of a wave and read by others of the same wave:

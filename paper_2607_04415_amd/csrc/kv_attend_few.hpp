@@ -150,16 +150,12 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     const bool whole = there_now == 0xFFFFFFFFu &&
                        ((j0 + kFewBlock - 1 <= tile.first && tile.last - j0 < (int64_t)p.window) ||
                         j0 + kFewBlock <= w.r.prefix);
-    uint32_t sees = 0xFF;  // this lane's eight keys
+    uint32_t sees = ~0u;  // this lane's keys: bits 0..3 and 16..19
     if (!whole) {
+      const uint64_t seen = (low_bits(pos - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(w.r.prefix - j0);
+      sees = (there_now & (uint32_t)seen) >> (g * 4);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int at = (i >> 2) * 16 + g * 4 + (i & 3);
-        const int32_t j = j0 + at;
-        const uint32_t seen = (there_now >> at & 1u) & (((uint32_t)(j <= pos) & (uint32_t)(j >= oldest)) | (uint32_t)(j < w.r.prefix));
-        e[i] = seen ? e[i] : -INFINITY;
-        sees &= ~((seen ^ 1u) << i);
-      }
+      for (int i = 0; i < 8; ++i) e[i] = sees >> ((i >> 2) * 16 + (i & 3)) & 1u ? e[i] : -INFINITY;
     }
     float top = fmaxf(fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])), fmaxf(fmaxf(e[4], e[5]), fmaxf(e[6], e[7])));
     top = xor16(xor32(top, max_of), max_of);
@@ -180,9 +176,6 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     }
     sum += part;
     const u32x4 weights = {Q::pack(e[0], e[1]), Q::pack(e[2], e[3]), Q::pack(e[4], e[5]), Q::pack(e[6], e[7])};
-    u32x4 seen_weights;  // 1 where the row sees the key
-#pragma unroll
-    for (int i = 0; i < 4; ++i) seen_weights[i] = Q::pack(sees >> (2 * i) & 1, sees >> (2 * i + 1) & 1);
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
       u32x4 vw[8];
@@ -204,8 +197,16 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
         u32x4 a;
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(vw[2 * i + 1][t >> 1], vw[2 * i][t >> 1], sel);
-        if (odd) o[h * 8 + t] += not_finite_part<Q>(a, seen_weights);
-        if (odd) a = finite_only<Q>(a);
+        if (__builtin_expect(odd, 0)) {
+          u32x4 seen;  // 1 where the row sees the key
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int at = (i >> 1) * 16 + (i & 1) * 2;
+            seen[i] = Q::pack((float)(sees >> at & 1u), (float)(sees >> (at + 1) & 1u));
+          }
+          o[h * 8 + t] += not_finite_part<Q>(a, seen);
+          a = finite_only<Q>(a);
+        }
         o[h * 8 + t] = Q::mfma16(a, weights, o[h * 8 + t]);
       }
     }
@@ -295,7 +296,8 @@ __global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParam
     const Tile tile = tile_of(p, w.r, w.tile);
     const KeyRange range = key_range<kFewBlock>(p, w.r, tile.first, tile.last);
     const uint32_t blocks = (uint32_t)max(range.count, 1);
-    few_part<Q, k8, kSteps, kMore>(p, w, tile, range, part_of(w, blocks, index), head);
+    const Part part = part_of(p, w, blocks, index);
+    if (!part.none) few_part<Q, k8, kSteps, kMore>(p, w, tile, range, part, head);
     const uint64_t end = w.begin + blocks;
     if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end)) return;
     __syncthreads();  // the next tile's sums go where this one's are read
@@ -310,7 +312,9 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
   WorkItem w;
   if (!find_item<256, kBlock>(p, index, w)) return;
   if (w.begin == index * w.share || w.begin < before * w.share) return;  // not cut here, or not first here
-  const uint64_t end = w.begin + blocks_of<kBlock>(p, w.r, w.tile);
+  const uint32_t blocks = blocks_of<kBlock>(p, w.r, w.tile);
+  if (blocks <= p.whole) return;
+  const uint64_t end = w.begin + blocks;
   const uint32_t s0 = before, s1 = (uint32_t)((end - 1) / w.share);
   const Tile tile = tile_of(p, w.r, w.tile);
   const uint32_t parts = s1 - s0 + 1, lane = threadIdx.x & 15;

@@ -34,12 +34,6 @@ constexpr int kManyBlock = 64;  // keys
 // f16's range, and a sum of them loses nothing): most blocks then rescale nothing.
 constexpr float kSlack = 8.f;
 
-// The low n bits, n of any size.
-__device__ __forceinline__ uint64_t low_bits(int32_t n) {
-  const uint64_t some = (1ull << (n & 63)) - 1;
-  return n <= 0 ? 0 : n >= 64 ? ~0ull : some;
-}
-
 // kSteps: D <= 32 kSteps.  k8: pages of 8-bit values.  kMore: scores are capped or biased.
 template <typename Q, bool k8, int kSteps, bool kMore>
 __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
@@ -454,7 +448,8 @@ __global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps >
     const Tile tile = tile_of(p, w.r, w.tile);
     const KeyRange range = key_range<kManyBlock>(p, w.r, tile.first, tile.last);
     const uint32_t blocks = (uint32_t)max(range.count, 1);
-    many_part<Q, k8, kSteps, kMore>(p, w, tile, range, part_of(w, blocks, index), head);
+    const Part part = part_of(p, w, blocks, index);
+    if (!part.none) many_part<Q, k8, kSteps, kMore>(p, w, tile, range, part, head);
     const uint64_t end = w.begin + blocks;
     if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end)) return;
     __syncthreads();

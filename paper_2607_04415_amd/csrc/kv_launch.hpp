@@ -9,7 +9,8 @@ namespace gorio {
 
 // One form's launch: AttendParams' fields for the division of its work.
 struct AttendForm {
-  uint32_t rows, from, upto, shares, least;
+  uint32_t rows, from, upto, shares, least, whole;
+  bool cuts;  // a tile may be cut
 };
 
 struct AttendLaunch {
@@ -25,16 +26,17 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
     p.upto = f.upto;
     p.shares = f.shares;
     p.least = f.least;
+    p.whole = f.whole;
   };
   if (l.few.shares) {
     divide(l.few);
     attend_few<Q, k8, kSteps, kMore><<<l.few.shares * p.kv_heads, few_waves(kSteps) * 64, 0, s>>>(p);
-    if (l.few.shares > 1) attend_join<Q, kFewRows, kFewBlock><<<(l.few.shares - 1) * p.kv_heads, 256, 0, s>>>(p);
+    if (l.few.cuts) attend_join<Q, kFewRows, kFewBlock><<<(l.few.shares - 1) * p.kv_heads, 256, 0, s>>>(p);
   }
   if (l.many.shares) {
     divide(l.many);
     attend_many<Q, k8, kSteps, kMore><<<l.many.shares * p.kv_heads, many_waves(kSteps) * 64, 0, s>>>(p);
-    if (l.many.shares > 1)
+    if (l.many.cuts)
       attend_join<Q, many_rows(kSteps), kManyBlock><<<dim3((l.many.shares - 1) * p.kv_heads, many_rows(kSteps) / 64), 256, 0, s>>>(p);
   }
   return hipGetLastError();

@@ -15,6 +15,7 @@ torch's current stream of the tensors' device.  Nothing waits for the GPU.
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import NamedTuple
 
 BF16, F16, E4M3 = 0, 1, 2
@@ -38,6 +39,10 @@ class AttentionDesc(ctypes.Structure):
         ("max_new", ctypes.c_uint32)]
 
 
+_ATTENTION = struct.Struct("4IQ2P2Q7P2f2I")   # AttentionDesc's fields, packed at once
+assert _ATTENTION.size == ctypes.sizeof(AttentionDesc)
+
+
 def declare(L):
     """Argument types of the gorio_kv_* symbols of the loaded library."""
     v, u32, u64, i32 = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int
@@ -53,26 +58,42 @@ def declare(L):
     L.gorio_kv_workspace.argtypes = [v, v, v]
 
 
-def _call(fn: str, *args):
-    from . import _check, lib
-    _check(getattr(lib(), fn)(*args))
+_torch = _L = None
 
 
-def _stream(device):
-    import torch
-    return torch.cuda.current_stream(device).cuda_stream
+def _bind():
+    """torch and the loaded library, once: a step of a decoding loop is a few of these calls."""
+    global _torch, _L
+    if _L is None:
+        import torch
+
+        from . import lib
+        _torch, _L = torch, lib()
+    return _torch, _L
+
+
+def _done(status: int):
+    if status:
+        from . import _check
+        _check(status)
+
+
+def _stream(device) -> int:
+    """torch's current stream of the device, as a handle."""
+    return _torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _need(name: str, a, dtype, shape, device):
     """Plain pointers cross the C ABI: what they point to is checked here."""
+    if a.dtype is dtype and a.shape == shape and a.device == device and a.is_contiguous():
+        return
     if a.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, not {a.dtype}")
     if a.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(a.shape)}")
-    if not a.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
     if a.device != device:
         raise ValueError(f"{name} must be on {device}, not {a.device}")
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _on_gpu(name: str, a):
@@ -93,7 +114,7 @@ def kv_attach(nodes, first_page, tokens, page_tokens: int, width: int, limit: in
     returned (gorio_kv_attach).  nodes: requests x k int32 or uint32 ids, as
     Index.search returns them; first_page, tokens: int32 per node; limit: table
     entries that passages may take of the `width` (default: all)."""
-    import torch
+    torch, L = _bind()
     dev = _on_gpu("nodes", nodes)
     if nodes.dim() != 2:
         raise ValueError(f"nodes must be (requests, k), not {tuple(nodes.shape)}")
@@ -107,10 +128,11 @@ def kv_attach(nodes, first_page, tokens, page_tokens: int, width: int, limit: in
     limit = width if limit is None else _count("limit", limit)
     tables = torch.empty((B, width), dtype=torch.int32, device=dev)
     fills = torch.empty_like(tables)
-    lens, attached = torch.empty((2, B), dtype=torch.int32, device=dev).unbind(0)
-    _call("gorio_kv_attach", nodes.data_ptr(), B, k, first_page.data_ptr(), tokens.data_ptr(), tokens.numel(),
-          _count("page_tokens", page_tokens), width, limit, tables.data_ptr(), fills.data_ptr(), lens.data_ptr(),
-          attached.data_ptr(), _stream(dev))
+    lens = torch.empty(B, dtype=torch.int32, device=dev)
+    attached = torch.empty_like(lens)
+    _done(L.gorio_kv_attach(nodes.data_ptr(), B, k, first_page.data_ptr(), tokens.data_ptr(), tokens.numel(),
+                            _count("page_tokens", page_tokens), width, limit, tables.data_ptr(), fills.data_ptr(),
+                            lens.data_ptr(), attached.data_ptr(), _stream(dev)))
     return tables, fills, lens, attached
 
 
@@ -128,7 +150,7 @@ class KVPlan(NamedTuple):
 def kv_plan(before, added, free_pages, tables, page_tokens: int, tokens: int) -> KVPlan:
     """A step's plan from request lengths (gorio_kv_plan): `tokens` new ones in
     all, or at most; the tables' new entries are written in place."""
-    import torch
+    torch, L = _bind()
     dev = _on_gpu("before", before)
     B, width = tables.shape
     _need("before", before, torch.int32, (B,), dev)
@@ -137,16 +159,17 @@ def kv_plan(before, added, free_pages, tables, page_tokens: int, tokens: int) ->
     _need("tables", tables, torch.int32, tables.shape, dev)
     T = _count("tokens", tokens)
     starts = torch.empty(B + 1, dtype=torch.int32, device=dev)
-    lens = torch.empty(B, dtype=torch.int32, device=dev)
+    lens = torch.empty_like(before)
     positions = torch.empty(T, dtype=torch.int32, device=dev)
     slots = torch.empty(T, dtype=torch.int64, device=dev)
     taken = torch.empty(1, dtype=torch.int32, device=dev)
     if B == 0:
         starts.zero_(), taken.zero_(), positions.fill_(-1), slots.fill_(-1)
         return KVPlan(starts, lens, positions, slots, taken)
-    _call("gorio_kv_plan", before.data_ptr(), added.data_ptr(), B, _count("page_tokens", page_tokens),
-          free_pages.data_ptr(), free_pages.numel(), tables.data_ptr(), width, T, lens.data_ptr(), starts.data_ptr(),
-          positions.data_ptr() if T else None, slots.data_ptr() if T else None, taken.data_ptr(), _stream(dev))
+    _done(L.gorio_kv_plan(before.data_ptr(), added.data_ptr(), B, _count("page_tokens", page_tokens),
+                          free_pages.data_ptr(), free_pages.numel(), tables.data_ptr(), width, T, lens.data_ptr(),
+                          starts.data_ptr(), positions.data_ptr() if T else None, slots.data_ptr() if T else None,
+                          taken.data_ptr(), _stream(dev)))
     return KVPlan(starts, lens, positions, slots, taken)
 
 
@@ -186,9 +209,16 @@ class KVCache:
                                None if key_scale is None else key_scale.data_ptr(),
                                None if value_scale is None else value_scale.data_ptr())
         self._ref = ctypes.addressof(self._desc)
+        self._layouts, self._spaces = {}, {}    # what _rows found of a layout; workspace bytes of a call's sizes
 
     def _rows(self, name: str, x, heads: int | None = None):
-        """Checks rows of a projection, tokens x heads x D; returns its type and row stride."""
+        """Checks rows of a projection, tokens x heads x D; returns their type and row stride."""
+        if x.device != self.device:
+            raise ValueError(f"{name} must be on {self.device}, not {x.device}")
+        key = (x.dtype, x.shape, x.stride(), heads)
+        known = self._layouts.get(key)
+        if known is not None:
+            return known
         if x.dim() != 3 or x.shape[2] != self.D or (heads is not None and x.shape[1] != heads):
             raise ValueError(f"{name} must be (tokens, {heads or 'heads'}, {self.D}), not {tuple(x.shape)}")
         code = self._codes.get(x.dtype, E4M3)
@@ -197,14 +227,15 @@ class KVCache:
         T, H, D = x.shape
         if (D > 1 and x.stride(2) != 1) or (H > 1 and x.stride(1) != D):
             raise ValueError(f"each token's heads in {name} must be contiguous")
-        if x.device != self.device:
-            raise ValueError(f"{name} must be on {self.device}, not {x.device}")
-        return code, (x.stride(0) if T > 1 else H * D)
+        if len(self._layouts) > 4096:
+            self._layouts.clear()
+        self._layouts[key] = known = code, (x.stride(0) if T > 1 else H * D)
+        return known
 
     def store(self, keys, values, slots):
         """Keys and values of new tokens (tokens x heads x D each; rows may be
         parts of wider ones) into their slots (int64; below 0: not stored)."""
-        import torch
+        torch, L = _bind()
         code, key_stride = self._rows("keys", keys, self.heads)
         code2, value_stride = self._rows("values", values, self.heads)
         if code != code2 or keys.shape != values.shape:
@@ -212,8 +243,8 @@ class KVCache:
         T = keys.shape[0]
         _need("slots", slots, torch.int64, (T,), self.device)
         if T:
-            _call("gorio_kv_store", self._ref, code, keys.data_ptr(), values.data_ptr(), T, key_stride, value_stride,
-                  slots.data_ptr(), _stream(self.device))
+            _done(L.gorio_kv_store(self._ref, code, keys.data_ptr(), values.data_ptr(), T, key_stride, value_stride,
+                                   slots.data_ptr(), _stream(self.device)))
 
     def attend(self, q, starts, lens, tables, *, fills=None, prefix=None, slopes=None, scale: float | None = None,
                cap: float = 0.0, window: int = 0, max_new: int = 0, out=None, with_lse: bool = False):
@@ -228,35 +259,41 @@ class KVCache:
         default.  cap: scores become cap * tanh(score / cap).  window: the
         distance from which a key outside the prefix is not seen (0: none).
         max_new: the most new tokens of a request, where the program knows it."""
-        import torch
-        dev = self.device
+        torch, L = _bind()
+        dev, i32 = self.device, torch.int32
         code, q_stride = self._rows("q", q)
         T, H, D = q.shape
         B, width = tables.shape
-        _need("tables", tables, torch.int32, (B, width), dev)
-        _need("starts", starts, torch.int32, (B + 1,), dev)
-        _need("lens", lens, torch.int32, (B,), dev)
+        _need("tables", tables, i32, (B, width), dev)
+        _need("starts", starts, i32, (B + 1,), dev)
+        _need("lens", lens, i32, (B,), dev)
         if fills is not None:
-            _need("fills", fills, torch.int32, (B, width), dev)
+            _need("fills", fills, i32, (B, width), dev)
         if prefix is not None:
-            _need("prefix", prefix, torch.int32, (B,), dev)
+            _need("prefix", prefix, i32, (B,), dev)
         if slopes is not None:
             _need("slopes", slopes, torch.float32, (H,), dev)
         if out is None:
-            out = torch.empty((T, H, D), dtype=q.dtype, device=dev)
-        out_code, out_stride = self._rows("out", out, H)
-        if out_code != code or out.shape[0] != T:
-            raise ValueError("out must be of q's type and shape")
+            out, out_stride = torch.empty((T, H, D), dtype=q.dtype, device=dev), H * D
+        else:
+            out_code, out_stride = self._rows("out", out, H)
+            if out_code != code or out.shape[0] != T:
+                raise ValueError("out must be of q's type and shape")
         lse = torch.empty((T, H), dtype=torch.float32, device=dev) if with_lse else None
-        a = AttentionDesc(code, H, B, width, T, q.data_ptr(), out.data_ptr(), q_stride, out_stride,
-                          None if lse is None else lse.data_ptr(), starts.data_ptr(), lens.data_ptr(),
-                          tables.data_ptr(), None if fills is None else fills.data_ptr(),
-                          None if prefix is None else prefix.data_ptr(), None if slopes is None else slopes.data_ptr(),
-                          D ** -0.5 if scale is None else scale, cap, _count("window", window),
-                          _count("max_new", max_new))
-        ref = ctypes.addressof(a)
-        need = ctypes.c_uint64()
-        _call("gorio_kv_workspace", self._ref, ref, ctypes.addressof(need))
-        space = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
-        _call("gorio_kv_attend", self._ref, ref, None if space is None else space.data_ptr(), need.value, _stream(dev))
+        window, max_new = _count("window", window), _count("max_new", max_new)
+        a = _ATTENTION.pack(code, H, B, width, T, q.data_ptr(), out.data_ptr(), q_stride, out_stride,
+                            0 if lse is None else lse.data_ptr(), starts.data_ptr(), lens.data_ptr(),
+                            tables.data_ptr(), 0 if fills is None else fills.data_ptr(),
+                            0 if prefix is None else prefix.data_ptr(), 0 if slopes is None else slopes.data_ptr(),
+                            D ** -0.5 if scale is None else scale, cap, window, max_new)
+        sizes = (code, T, H, B, width, max_new)
+        need = self._spaces.get(sizes)
+        if need is None:
+            got = ctypes.c_uint64()
+            _done(L.gorio_kv_workspace(self._ref, a, ctypes.addressof(got)))
+            if len(self._spaces) > 4096:
+                self._spaces.clear()
+            need = self._spaces[sizes] = got.value
+        space = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        _done(L.gorio_kv_attend(self._ref, a, None if space is None else space.data_ptr(), need, _stream(dev)))
         return (out, lse) if with_lse else out
