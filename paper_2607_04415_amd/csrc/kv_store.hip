@@ -1,7 +1,9 @@
 // gorio_kv_store: rows of new keys and values into their slots.
 //
 // A copy whose destination rows are scattered: a thread moves 8 elements (16
-// bytes), neighbouring threads neighbouring parts of a row.
+// bytes) of a key and of its value, neighbouring threads neighbouring parts of
+// a row.  A block's first token is divided out once, so that the threads' own
+// divisions are multiplications of 32 bits.
 #include "kv.hpp"
 
 using namespace gorio;
@@ -16,7 +18,7 @@ struct StoreParams {
   uint64_t key_stride, value_stride;  // elements
   uint64_t page_stride, head_stride, token_stride;
   uint64_t num_pages;
-  uint64_t parts;  // 8-element parts of the keys: tokens * heads * D / 8
+  uint64_t parts;  // 8-element parts of the keys: tokens * heads * D / 8, of which a block takes kParts
   FastDiv per_row, per_token;  // parts of a head's row, and of a token
   FastDiv page_tokens;
 };
@@ -28,30 +30,14 @@ __device__ __forceinline__ float to_float(uint16_t bits, bool f16) {
 // +-448 is the largest value of the 8-bit type; a NaN stays one.
 __device__ __forceinline__ float clamp_e4m3(float x) { return x > 448.f ? 448.f : x < -448.f ? -448.f : x; }
 
-template <int kTo>  // 0: as it is; 1: bf16 to e4m3; 2: f16 to e4m3
-__global__ __launch_bounds__(256) void store_kernel(StoreParams p) {
-  const uint64_t part = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  if (part >= p.parts) return;
-  const bool value = blockIdx.y != 0;
-  // parts stay below 2^31 * 1024 * 32: the token by 64-bit division once per
-  // thread, the rest by multiplication
-  const uint64_t token = part / p.per_token.d;
-  const uint32_t in = (uint32_t)(part - token * p.per_token.d);
-  const uint32_t head = fastdiv(in, p.per_row), at = (in - head * p.per_row.d) * 8;
-  const int64_t slot = p.slots[token];
-  if (slot < 0) return;
-  const uint64_t page = (uint64_t)slot / p.page_tokens.d;
-  if (page >= p.num_pages) return;
-  const uint32_t place = (uint32_t)((uint64_t)slot - page * p.page_tokens.d);
-  const uint16_t *from = value ? p.values + token * p.value_stride : p.keys + token * p.key_stride;
-  const uint4 x = *reinterpret_cast<const uint4 *>(from + (uint64_t)head * p.per_row.d * 8 + at);
-  const uint64_t to = page * p.page_stride + head * p.head_stride + place * p.token_stride + at;
-  uint8_t *pages = value ? p.to_values : p.to_keys;
+constexpr uint32_t kParts = 1024;
+
+// Eight elements as they are (kTo 0), or bf16 (1) or f16 (2) to e4m3.
+template <int kTo>
+__device__ __forceinline__ void put(uint8_t *pages, uint64_t to, const uint4 &x, float scale) {
   if constexpr (kTo == 0) {
     *reinterpret_cast<uint4 *>(pages + to * 2) = x;
   } else {
-    const float *scales = value ? p.value_scale : p.key_scale;
-    const float scale = scales ? scales[head] : 1.f;
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     int packed[2];
 #pragma unroll
@@ -64,6 +50,31 @@ __global__ __launch_bounds__(256) void store_kernel(StoreParams p) {
       packed[i] = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], packed[i], true);
     }
     *reinterpret_cast<int2 *>(pages + to) = make_int2(packed[0], packed[1]);
+  }
+}
+
+template <int kTo>
+__global__ __launch_bounds__(256) void store_kernel(StoreParams p) {
+  const uint64_t part0 = (uint64_t)blockIdx.x * kParts, token0 = part0 / p.per_token.d;
+  const uint32_t in0 = (uint32_t)(part0 - token0 * p.per_token.d);
+#pragma unroll
+  for (uint32_t i = 0; i < kParts / 256; ++i) {
+    const uint32_t at = i * 256 + threadIdx.x;
+    if (part0 + at >= p.parts) return;
+    const uint32_t n = fastdiv(in0 + at, p.per_token), in = in0 + at - n * p.per_token.d;
+    const uint64_t token = token0 + n;
+    const uint32_t head = fastdiv(in, p.per_row), d = (in - head * p.per_row.d) * 8;
+    const int64_t slot = p.slots[token];
+    if (slot < 0) continue;
+    const uint64_t page = slot < (1ll << 31) ? fastdiv((uint32_t)slot, p.page_tokens) : (uint64_t)slot / p.page_tokens.d;
+    if (page >= p.num_pages) continue;
+    const uint32_t place = (uint32_t)((uint64_t)slot - page * p.page_tokens.d);
+    const uint32_t from = head * p.per_row.d * 8 + d;
+    const uint4 k = *reinterpret_cast<const uint4 *>(p.keys + token * p.key_stride + from);
+    const uint4 v = *reinterpret_cast<const uint4 *>(p.values + token * p.value_stride + from);
+    const uint64_t to = page * p.page_stride + head * p.head_stride + place * p.token_stride + d;
+    put<kTo>(p.to_keys, to, k, kTo && p.key_scale ? p.key_scale[head] : 1.f);
+    put<kTo>(p.to_values, to, v, kTo && p.value_scale ? p.value_scale[head] : 1.f);
   }
 }
 
@@ -112,12 +123,12 @@ extern "C" gorio_status gorio_kv_store(const gorio_kv_cache *cache, gorio_kv_dty
   p.per_token = make_fastdiv(c.heads * (c.D / 8));
   p.page_tokens = make_fastdiv(c.page_tokens);
   p.parts = tokens * p.per_token.d;
-  const uint64_t blocks = (p.parts + 255) / 256;
-  if (blocks > 0x7FFFFFFFull) return fail(GORIO_EINVAL, "tokens=%llu too large", (unsigned long long)tokens);
-  const dim3 grid((uint32_t)blocks, 2);
+  // at most 2^31 tokens of 2^15 parts; a launch has less than 2^32 threads
+  const uint64_t grid = (p.parts + kParts - 1) / kParts;
+  if (grid >= 1ull << 24) return fail(GORIO_EINVAL, "tokens=%llu too large", (unsigned long long)tokens);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (c.dtype != GORIO_KV_E4M3) store_kernel<0><<<grid, 256, 0, s>>>(p);
-  else if (dtype == GORIO_KV_BF16) store_kernel<1><<<grid, 256, 0, s>>>(p);
-  else store_kernel<2><<<grid, 256, 0, s>>>(p);
+  if (c.dtype != GORIO_KV_E4M3) store_kernel<0><<<(uint32_t)grid, 256, 0, s>>>(p);
+  else if (dtype == GORIO_KV_BF16) store_kernel<1><<<(uint32_t)grid, 256, 0, s>>>(p);
+  else store_kernel<2><<<(uint32_t)grid, 256, 0, s>>>(p);
   return kv_launched("gorio_kv_store");
 }
