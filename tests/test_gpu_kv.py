@@ -280,6 +280,31 @@ def test_attend_long(torch, type, cache, news, lens, H, KV):
     holds(torch, a, call(torch, a, max_new=max(news)))
 
 
+@pytest.mark.parametrize("B,most,longest", [(1300, 1, 60), (700, 1, 900), (600, 3, 100), (300, 90, 130)])
+def test_attend_many_requests(torch, B, most, longest):
+    """More requests, and more tiles, than a workgroup has threads; some with nothing new or nothing at all."""
+    rng = np.random.default_rng([B, most])
+    news = rng.integers(0, most + 1, B) if most > 1 else np.ones(B, int)
+    if most > 50:
+        news[rng.random(B) < 0.9] = 1
+    lens = np.maximum(news, rng.integers(0, longest, B))
+    lens[5] = longest + 700
+    a = setup(torch, B, "bf16", "bf16", 2, 1, 64, 16, news, lens, poison=False)
+    holds(torch, a, call(torch, a, max_new=int(news.max())))
+
+
+def test_attend_more_key_heads_than_workgroups(torch):
+    a = setup(torch, 18, "f16", "f16", 300, 300, 8, 16, [1, 70], [600, 90], poison=False)
+    holds(torch, a, call(torch, a))
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 200])
+def test_attend_cut_tiles(torch, D):
+    """Chunks over texts long enough that their tiles are divided among workgroups."""
+    a = setup(torch, D, "bf16", "bf16", 2, 1, D, 16, [9, 40], [2600, 1500], fills=True, slopes=True)
+    holds(torch, a, call(torch, a))
+
+
 @pytest.mark.parametrize("news", [[1, 3], [64, 40]])
 def test_attend_peaked(torch, news):
     """Scores of several hundred, of both signs: the running maximum moves by a lot."""
