@@ -468,9 +468,9 @@ struct ScoreChange {
   __device__ __forceinline__ ScoreChange(float scale, float cap_, float slope_)
       : factor(scale * kLog2e), cap(cap_ * kLog2e), twice(-2.f * cap_ * kLog2e),
         by(cap_ > 0.f ? 2.f * kLog2e * scale / cap_ : 0.f), slope(-slope_ * kLog2e) {}
-  __device__ __forceinline__ float capped(float x) const {
-    return __builtin_fmaf(twice, __builtin_amdgcn_rcpf(1.f + pow2(x * by)), cap);
-  }
+  // -1 / (1 + E): grows with the score, which is cap - twice * this
+  __device__ __forceinline__ float quotient(float x) const { return __builtin_amdgcn_rcpf(-1.f - pow2(x * by)); }
+  __device__ __forceinline__ float capped(float x) const { return __builtin_fmaf(quotient(x), -twice, cap); }
   // y less the bias at this distance
   __device__ __forceinline__ float biased(float y, float distance) const {
     return __builtin_fmaf(slope, fabsf(distance), y);

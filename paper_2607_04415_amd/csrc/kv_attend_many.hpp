@@ -79,7 +79,8 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   const float scale = p.scale * (p.key_scale ? p.key_scale[head] : 1.f);
   // the running maximum is taken of the products as they are, so the factor has to be positive:
   // a negative one turns the queries' signs around
-  const uint32_t flip = !kMore && scale < 0.f ? 0x80008000u : 0u;
+  const bool capped = kMore && p.cap > 0.f, biased = kMore && p.slopes;
+  const uint32_t flip = !capped && scale < 0.f ? 0x80008000u : 0u;
   const float factor = scale == 0.f ? 1e-30f : fabsf(scale) * kLog2e;  // 0 times a masked score's -inf would be NaN
   u32x4 q[kSteps * 2];
   {
@@ -91,7 +92,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       q[s] ^= flip;
     }
   }
-  const ScoreChange change(scale, p.cap, kMore && p.slopes ? p.slopes[qhead] : 0.f);
+  const ScoreChange change(scale, p.cap, biased ? p.slopes[qhead] : 0.f);
 
   // Where block x's keys lie: wave 0 looks up a key a lane ...
   auto look_up = [&](int32_t x) __attribute__((always_inline)) {
@@ -208,20 +209,33 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
     value_at[0] = lds + key * kValueRow * 2 + (kTurned ? c ^ turned(key) : c) * 16 + (lane & 1) * 8;
     value_at[1] = lds + (key + 8) * kValueRow * 2 + (kTurned ? c ^ turned(key + 8) : c) * 16 + (lane & 1) * 8;
   }
-  const float to_log2 = kMore ? 1.f : factor;
+  // A score in log2 is s * mul + add.  Without a cap s is the product, to which the bias is
+  // added as what the product starts from.  With a cap s is -1 / (1 + E) (see ScoreChange), or,
+  // if there is a bias as well, the score itself.
+  const float mul = !capped ? factor : biased ? 1.f : -change.twice;
+  const float add = capped && !biased ? change.cap : 0.f;
+  const float start_slope = biased && !capped ? change.slope / factor : 0.f;
+  auto start = [&](f32x16 &s, int32_t j) __attribute__((always_inline)) {
+    if (kMore && biased && !capped) {
+      const float distance = (float)(pos - j - g * 4);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = start_slope * fabsf(distance - (float)((i >> 2) * 8 + (i & 3)));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    }
+  };
   auto changed = [&](f32x16 &s, int32_t j0) __attribute__((always_inline)) {
     if constexpr (kMore) {
-      if (p.cap > 0.f) {
+      if (capped) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = change.capped(s[i]);
-      } else {
+        for (int i = 0; i < 16; ++i) s[i] = change.quotient(s[i]);
+        if (biased) {
+          const float distance = (float)(pos - j0 - g * 4);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] *= change.factor;
-      }
-      if (p.slopes) {
-        const float distance = (float)(pos - j0 - g * 4);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = change.biased(s[i], distance - (float)((i >> 2) * 8 + (i & 3)));
+          for (int i = 0; i < 16; ++i)
+            s[i] = change.biased(__builtin_fmaf(s[i], -change.twice, change.cap), distance - (float)((i >> 2) * 8 + (i & 3)));
+        }
       }
     }
   };
@@ -231,7 +245,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
 #pragma unroll
     for (int i = 1; i < 15; i += 2) top = max3(top, s[i], s[i + 1]);
     top = max3(top, s[15], s[15]);
-    top = xor32(top, max_of) * to_log2;
+    top = __builtin_fmaf(xor32(top, max_of), mul, add);
     if (__any((top > best + kSlack) | (best == -INFINITY))) {
       const float to = fmaxf(best, top);
       const float keep = to == -INFINITY ? 1.f : pow2(best - to);
@@ -245,7 +259,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   // them computed beside (S^T from `keys`): a matrix instruction takes as long as eight others,
   // so the exponentials go between those of S^T.  LDS is read first, all at once, while the
   // products of the 32 keys before are still under way and the maximum is looked for.
-  auto both = [&](f32x16 &s, f32x16 &next, auto keys, auto values, auto &&prepare) __attribute__((always_inline)) {
+  auto both = [&](f32x16 &s, f32x16 &next, int32_t j_next, auto keys, auto values, auto &&prepare) __attribute__((always_inline)) {
     constexpr int kTiles = kSteps > 4 ? 4 : kSteps, kTurns = kSteps / kTiles;
     constexpr uint32_t kFrom = decltype(values)::value, kSixteen = 16 * kValueRow * 2;
     constexpr uint32_t kFar = kFrom + kSixteen > 65535 ? kFrom : 0;  // an instruction's offset has 16 bits
@@ -270,10 +284,9 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
     read_values(std::integral_constant<int, 0>{});
     __builtin_amdgcn_sched_barrier(0);
     prepare(s);
-    const float from = best == -INFINITY ? 0.f : best;
+    const float less = add - (best == -INFINITY ? 0.f : best);
     u32x4 weights[2];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) next[i] = 0.f;
+    start(next, j_next);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < kSteps * 2; ++k) {
@@ -281,8 +294,8 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       if (k + 4 < kSteps * 2) read_keys(k + 4);
 #pragma unroll
       for (int e = 8 * k / (kSteps * 2); e < 8 * (k + 1) / (kSteps * 2); ++e) {  // pairs of scores
-        const float w0 = pow2(__builtin_fmaf(s[e * 2], to_log2, -from));
-        const float w1 = pow2(__builtin_fmaf(s[e * 2 + 1], to_log2, -from));
+        const float w0 = pow2(__builtin_fmaf(s[e * 2], mul, less));
+        const float w1 = pow2(__builtin_fmaf(s[e * 2 + 1], mul, less));
         weights[e >> 2][e & 3] = Q::pack(w0, w1);
         sum += w0 + w1;
       }
@@ -343,13 +356,13 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       }
     };
     if constexpr (decltype(computes)::value) {
-      both(now, next, std::integral_constant<uint32_t, k_now>{}, std::integral_constant<uint32_t, v_now>{},
+      both(now, next, j0 + 32, std::integral_constant<uint32_t, k_now>{}, std::integral_constant<uint32_t, v_now>{},
            [&](f32x16 &s) __attribute__((always_inline)) {
              changed(s, j0);
              mask(s, (uint32_t)sees);
              rescale(s);
            });
-      both(next, now, std::integral_constant<uint32_t, k_now + kHalfKeys>{},
+      both(next, now, range.block(x + 1) * kManyBlock, std::integral_constant<uint32_t, k_now + kHalfKeys>{},
            std::integral_constant<uint32_t, v_now + kHalfValues>{}, [&](f32x16 &s) __attribute__((always_inline)) {
              changed(s, j0 + 32);
              mask(s, (uint32_t)(sees >> 32));
@@ -389,8 +402,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
     put(0, kKeys[0]);
     put(1, kValues[0]);
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) now[i] = 0.f;
+    start(now, range.block(x0) * kManyBlock);
 #pragma unroll
     for (int k = 0; k < kSteps * 2; ++k)
       now = Q::mfma32(*lds_at<u32x4>(beside(key_at, k * 32) + kKeys[1] + kHalfKeys), q[k], now);
