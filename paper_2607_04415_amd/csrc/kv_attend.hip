@@ -60,7 +60,7 @@ AttendForm divide(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t
 AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint64_t *bytes) {
   AttendLaunch l{};
   l.e4m3 = c.dtype == GORIO_KV_E4M3;
-  l.more = a.cap > 0.f || a.slopes;
+  l.more = a.cap > 0.f ? 2 : a.slopes ? 1 : 0;
   const uint64_t group = a.heads / c.heads;
   // the most and the fewest new tokens of a request that has any; exact for one request
   const uint64_t most = a.max_new ? std::min<uint64_t>(a.max_new, a.tokens) : a.tokens;
@@ -71,9 +71,10 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   if (few) l.few = divide(c, a, kFewRows, kFewBlock, 8, 16, 256, many);
   if (many) l.many = divide(c, a, many_rows(steps), kManyBlock, 4, 8, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
   if (few && many) l.few.upto = l.many.from = kFewUpto;
-  const uint64_t slot = 2 * (c.D + 2) * sizeof(float) * c.heads;  // two parts of a share
-  *bytes = std::max<uint64_t>(l.few.cuts ? l.few.shares * kFewRows : 0,
-                              l.many.cuts ? (uint64_t)l.many.shares * many_rows(steps) : 0) * slot;
+  auto room = [&](const AttendForm &f) -> uint64_t {  // of a share and key head: two parts, and which tile is cut
+    return f.cuts ? (uint64_t)f.shares * c.heads * (2 * (c.D + 2) * sizeof(float) * f.rows + sizeof(Cut)) : 0;
+  };
+  *bytes = std::max(room(l.few), room(l.many));
   return l;
 }
 

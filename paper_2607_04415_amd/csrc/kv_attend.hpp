@@ -156,6 +156,7 @@ struct AttendParams {
   uint32_t from, upto;   // requests with this many rows a key head, from <= rows < upto
   uint32_t shares, least;  // workgroups of a key head, at most; key blocks of a share, at least
   uint32_t whole;          // key blocks of a tile that is not cut, at most
+  bool cuts;               // a tile may be cut
 };
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -409,6 +410,34 @@ __device__ __forceinline__ Part part_of(const AttendParams &p, const WorkItem &w
     a.divided = a.from > 0 || a.upto < blocks;
   }
   return a;
+}
+
+// What the joining kernel needs of the tile that begins in a share and is cut at its end; parts
+// is 0 if there is none.  Written by the share's workgroup behind the parts' sums: to find the
+// tile again from the lengths took the joining kernel 12 us for 264 tiles.
+struct Cut {
+  int32_t start;         // of the request's tokens
+  uint32_t row0, rows;   // of the tile
+  uint32_t slot, parts;  // of its first part, and how many; the others begin their shares
+};
+
+template <int kRows>
+__device__ __forceinline__ Cut *cuts_of(const AttendParams &p) {
+  return reinterpret_cast<Cut *>(p.parts + (uint64_t)p.shares * 2 * p.kv_heads * kRows * (p.D + 2));
+}
+
+// At a workgroup's end: `part` of tile w is its last.  A call of which no tile is cut has no room for it.
+template <int kRows>
+__device__ __forceinline__ void note_cut(const AttendParams &p, uint32_t index, uint32_t head, const WorkItem &w,
+                                         const Tile &tile, const Part &part, uint32_t blocks) {
+  if (threadIdx.x != 0 || !p.cuts) return;
+  const bool here = part.divided && part.from == 0;
+  const uint32_t last = (uint32_t)((w.begin + blocks - 1) / w.share);
+  cuts_of<kRows>(p)[index * p.kv_heads + head] = Cut{w.r.start, tile.row0, tile.rows, part.slot, here ? last - index + 1 : 0};
+}
+template <int kRows>
+__device__ __forceinline__ void note_cut(const AttendParams &p, uint32_t index, uint32_t head) {
+  if (threadIdx.x == 0 && p.cuts) cuts_of<kRows>(p)[index * p.kv_heads + head] = Cut{0, 0, 0, 0, 0};
 }
 
 // One lane's look at a key's table entry.  What it loads is judged where it is needed, a block

@@ -291,7 +291,7 @@ template <typename Q, bool k8, int kSteps, bool kMore>
 __global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
-  if (!find_item<few_waves(kSteps) * 64, kFewBlock>(p, index, w)) return;
+  if (!find_item<few_waves(kSteps) * 64, kFewBlock>(p, index, w)) return note_cut<kFewRows>(p, index, head);
   for (;;) {
     const Tile tile = tile_of(p, w.r, w.tile);
     const KeyRange range = key_range<kFewBlock>(p, w.r, tile.first, tile.last);
@@ -299,30 +299,23 @@ __global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParam
     const Part part = part_of(p, w, blocks, index);
     if (!part.none) few_part<Q, k8, kSteps, kMore>(p, w, tile, range, part, head);
     const uint64_t end = w.begin + blocks;
-    if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end)) return;
+    if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end))
+      return note_cut<kFewRows>(p, index, head, w, tile, part, blocks);
     __syncthreads();  // the next tile's sums go where this one's are read
   }
 }
 
-// Joins the parts of divided tiles: a workgroup a share (but the first) and head.  It joins the
-// tile that the share begins in, if the tile begins in the share before; 64 rows, 16 threads a row.
-template <typename Q, int kRows, int kBlock>
+// Joins the parts of divided tiles: a workgroup a share and head, for the tile that begins in the
+// share and is cut at its end; 16 rows, 16 threads a row.
+template <typename Q, int kRows>
 __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
-  const uint32_t before = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - before * p.kv_heads, index = before + 1;
-  WorkItem w;
-  if (!find_item<256, kBlock>(p, index, w)) return;
-  if (w.begin == index * w.share || w.begin < before * w.share) return;  // not cut here, or not first here
-  const uint32_t blocks = blocks_of<kBlock>(p, w.r, w.tile);
-  if (blocks <= p.whole) return;
-  const uint64_t end = w.begin + blocks;
-  const uint32_t s0 = before, s1 = (uint32_t)((end - 1) / w.share);
-  const Tile tile = tile_of(p, w.r, w.tile);
-  const uint32_t parts = s1 - s0 + 1, lane = threadIdx.x & 15;
-  const uint32_t slot0 = s0 * 2 + (w.begin > s0 * w.share ? 1 : 0);  // of the first part; the others begin their shares
+  const uint32_t s0 = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - s0 * p.kv_heads;
+  const Cut cut = cuts_of<kRows>(p)[blockIdx.x];
+  const uint32_t parts = cut.parts, slot0 = cut.slot, lane = threadIdx.x & 15;  // slot0: of the first part
   const float *ml = p.parts + (uint64_t)p.shares * 2 * p.kv_heads * kRows * p.D;
   const float vs = p.value_scale ? p.value_scale[head] : 1.f;
-  const uint32_t upto = min(tile.rows, blockIdx.y * 64 + 64);
-  for (uint32_t row = blockIdx.y * 64 + (threadIdx.x >> 4); row < upto; row += 16) {
+  const uint32_t row = blockIdx.y * 16 + (threadIdx.x >> 4);
+  if (parts && row < cut.rows) {
     auto slot = [&](uint32_t i) {
       return ((uint64_t)(i ? (s0 + i) * 2 : slot0) * p.kv_heads + head) * kRows + row;
     };
@@ -361,8 +354,8 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
 #pragma unroll
     for (int d = 8; d; d >>= 1) all += __shfl_xor(all, d);
     const float norm = all != 0.f ? vs / all : 0.f;
-    const uint32_t tk = fastdiv(tile.row0 + row, p.group), hq = head * p.group.d + (tile.row0 + row - tk * p.group.d);
-    const uint64_t t_out = (uint64_t)(w.r.start + tk);
+    const uint32_t tk = fastdiv(cut.row0 + row, p.group), hq = head * p.group.d + (cut.row0 + row - tk * p.group.d);
+    const uint64_t t_out = (uint64_t)(cut.start + tk);
     uint16_t *out = p.out + t_out * p.out_stride + (uint64_t)hq * p.D;
 #pragma unroll
     for (int i = 0; i < 4; i += 2) {

@@ -34,8 +34,9 @@ constexpr int kManyBlock = 64;  // keys
 // f16's range, and a sum of them loses nothing): most blocks then rescale nothing.
 constexpr float kSlack = 8.f;
 
-// kSteps: D <= 32 kSteps.  k8: pages of 8-bit values.  kMore: scores are capped or biased.
-template <typename Q, bool k8, int kSteps, bool kMore>
+// kSteps: D <= 32 kSteps.  k8: pages of 8-bit values.  kMore: 1 if scores are biased, 2 if they
+// are capped, and biased if there are slopes.
+template <typename Q, bool k8, int kSteps, int kMore>
 __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
                                           const KeyRange &range, const Part &part, uint32_t head) {
   constexpr int kManyWaves = many_waves(kSteps), kManyThreads = kManyWaves * 64, kManyRows = kManyWaves * 32;
@@ -79,9 +80,11 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   const float scale = p.scale * (p.key_scale ? p.key_scale[head] : 1.f);
   // the running maximum is taken of the products as they are, so the factor has to be positive:
   // a negative one turns the queries' signs around
-  const bool capped = kMore && p.cap > 0.f, biased = kMore && p.slopes;
+  constexpr bool capped = kMore == 2;
+  const bool biased = kMore == 1 || (kMore == 2 && p.slopes);
   const uint32_t flip = !capped && scale < 0.f ? 0x80008000u : 0u;
-  const float factor = scale == 0.f ? 1e-30f : fabsf(scale) * kLog2e;  // 0 times a masked score's -inf would be NaN
+  // 0 times a masked score's -inf would be NaN, and a bias is divided by it
+  const float factor = scale == 0.f || (biased && fabsf(scale) < 1e-30f) ? 1e-30f : fabsf(scale) * kLog2e;
   u32x4 q[kSteps * 2];
   {
     const uint16_t *at = p.q + (uint64_t)(w.r.start + token) * p.q_stride + (uint64_t)qhead * p.D;
@@ -216,26 +219,30 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   const float add = capped && !biased ? change.cap : 0.f;
   const float start_slope = biased && !capped ? change.slope / factor : 0.f;
   auto start = [&](f32x16 &s, int32_t j) __attribute__((always_inline)) {
-    if (kMore && biased && !capped) {
+    if constexpr (kMore == 1) {
       const float distance = (float)(pos - j - g * 4);
+      if (j < w.r.prefix && j + 31 > first) {  // keys after a row's position that it sees
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = start_slope * fabsf(distance - (float)((i >> 2) * 8 + (i & 3)));
+        for (int i = 0; i < 16; ++i) s[i] = start_slope * fabsf(distance - (float)((i >> 2) * 8 + (i & 3)));
+      } else {
+        const float here = start_slope * distance;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(-start_slope, (float)((i >> 2) * 8 + (i & 3)), here);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.f;
     }
   };
   auto changed = [&](f32x16 &s, int32_t j0) __attribute__((always_inline)) {
-    if constexpr (kMore) {
-      if (capped) {
+    if constexpr (capped) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = change.quotient(s[i]);
-        if (biased) {
-          const float distance = (float)(pos - j0 - g * 4);
+      for (int i = 0; i < 16; ++i) s[i] = change.quotient(s[i]);
+      if (biased) {
+        const float distance = (float)(pos - j0 - g * 4);
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            s[i] = change.biased(__builtin_fmaf(s[i], -change.twice, change.cap), distance - (float)((i >> 2) * 8 + (i & 3)));
-        }
+        for (int i = 0; i < 16; ++i)
+          s[i] = change.biased(__builtin_fmaf(s[i], -change.twice, change.cap), distance - (float)((i >> 2) * 8 + (i & 3)));
       }
     }
   };
@@ -451,11 +458,11 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   }
 }
 
-template <typename Q, bool k8, int kSteps, bool kMore>
+template <typename Q, bool k8, int kSteps, int kMore>
 __global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps > 2 ? 2 : 3) void attend_many(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
-  if (!find_item<many_waves(kSteps) * 64, kManyBlock>(p, index, w)) return;
+  if (!find_item<many_waves(kSteps) * 64, kManyBlock>(p, index, w)) return note_cut<many_rows(kSteps)>(p, index, head);
   for (;;) {
     const Tile tile = tile_of(p, w.r, w.tile);
     const KeyRange range = key_range<kManyBlock>(p, w.r, tile.first, tile.last);
@@ -463,7 +470,8 @@ __global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps >
     const Part part = part_of(p, w, blocks, index);
     if (!part.none) many_part<Q, k8, kSteps, kMore>(p, w, tile, range, part, head);
     const uint64_t end = w.begin + blocks;
-    if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end)) return;
+    if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end))
+      return note_cut<many_rows(kSteps)>(p, index, head, w, tile, part, blocks);
     __syncthreads();
   }
 }

@@ -14,11 +14,12 @@ struct AttendForm {
 };
 
 struct AttendLaunch {
-  bool e4m3, more;  // 8-bit pages; scores capped or biased
+  bool e4m3;  // 8-bit pages
+  int more;   // 1 if scores are biased, 2 if they are capped
   AttendForm few, many;
 };
 
-template <typename Q, bool k8, int kSteps, bool kMore>
+template <typename Q, bool k8, int kSteps, int kMore>
 hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
   auto divide = [&](const AttendForm &f) {
     p.rows = f.rows;
@@ -27,24 +28,29 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
     p.shares = f.shares;
     p.least = f.least;
     p.whole = f.whole;
+    p.cuts = f.cuts;
   };
   if (l.few.shares) {
     divide(l.few);
-    attend_few<Q, k8, kSteps, kMore><<<l.few.shares * p.kv_heads, few_waves(kSteps) * 64, 0, s>>>(p);
-    if (l.few.cuts) attend_join<Q, kFewRows, kFewBlock><<<(l.few.shares - 1) * p.kv_heads, 256, 0, s>>>(p);
+    attend_few<Q, k8, kSteps, (kMore > 0)><<<l.few.shares * p.kv_heads, few_waves(kSteps) * 64, 0, s>>>(p);
+    if (l.few.cuts) attend_join<Q, kFewRows><<<(l.few.shares - 1) * p.kv_heads, 256, 0, s>>>(p);
   }
   if (l.many.shares) {
     divide(l.many);
     attend_many<Q, k8, kSteps, kMore><<<l.many.shares * p.kv_heads, many_waves(kSteps) * 64, 0, s>>>(p);
     if (l.many.cuts)
-      attend_join<Q, many_rows(kSteps), kManyBlock><<<dim3((l.many.shares - 1) * p.kv_heads, many_rows(kSteps) / 64), 256, 0, s>>>(p);
+      attend_join<Q, many_rows(kSteps)><<<dim3((l.many.shares - 1) * p.kv_heads, many_rows(kSteps) / 16), 256, 0, s>>>(p);
   }
   return hipGetLastError();
 }
 
 template <typename Q, bool k8, int kSteps>
 hipError_t launch_steps(const AttendParams &p, const AttendLaunch &l, hipStream_t s) {
-  return l.more ? launch_forms<Q, k8, kSteps, true>(p, l, s) : launch_forms<Q, k8, kSteps, false>(p, l, s);
+  switch (l.more) {
+    case 0: return launch_forms<Q, k8, kSteps, 0>(p, l, s);
+    case 1: return launch_forms<Q, k8, kSteps, 1>(p, l, s);
+    default: return launch_forms<Q, k8, kSteps, 2>(p, l, s);
+  }
 }
 
 // 32-element steps of the kernels for a head of D elements.
