@@ -573,6 +573,12 @@ __device__ __forceinline__ uint64_t low_bits(int32_t n) {
   return n <= 0 ? 0 : n >= 64 ? ~0ull : some;
 }
 
+// x if the bit is set, or -inf.  On the bits: compares would hold a scalar pair for every score.
+__device__ __forceinline__ float kept(float x, uint32_t bits, int bit) {
+  const uint32_t mask = (uint32_t)((int32_t)(bits << (31 - bit)) >> 31);
+  return __uint_as_float((__float_as_uint(x) & mask) | (0xFF800000u & ~mask));
+}
+
 // LDS written by some lanes of a wave and read by others of the same wave:
 // the hardware keeps their order, the compiler has to.
 __device__ __forceinline__ void wave_lds_order() {

@@ -155,7 +155,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
       const uint64_t seen = (low_bits(pos - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(w.r.prefix - j0);
       sees = (there_now & (uint32_t)seen) >> (g * 4);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = sees >> ((i >> 2) * 16 + (i & 3)) & 1u ? e[i] : -INFINITY;
+      for (int i = 0; i < 8; ++i) e[i] = kept(e[i], sees, (i >> 2) * 16 + (i & 3));
     }
     float top = fmaxf(fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])), fmaxf(fmaxf(e[4], e[5]), fmaxf(e[6], e[7])));
     top = xor16(xor32(top, max_of), max_of);

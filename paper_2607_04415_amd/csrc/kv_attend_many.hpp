@@ -359,7 +359,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       if (masked) {
         seen >>= g * 4;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = seen >> ((i >> 2) * 8 + (i & 3)) & 1u ? s[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) s[i] = kept(s[i], seen, (i >> 2) * 8 + (i & 3));
       }
     };
     if constexpr (decltype(computes)::value) {
