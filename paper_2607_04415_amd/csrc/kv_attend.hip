@@ -34,7 +34,10 @@ gorio_status check(const gorio_kv_cache *cache, const gorio_kv_attention *a, gor
   return GORIO_OK;
 }
 
-// Rows of a request and key head up to which the form for few rows takes it.
+// Rows of a request and key head from which the form for many rows takes it.  The other form
+// reads every key once per 16 rows.  16 requests of 12 rows over 4000 tokens: 56 us, by the form
+// for many rows 70; of 20 rows 58 (its second reading is cached) and 72; but 64 requests over
+// 16000 tokens, which no cache holds: of 16 rows 702 and 764 us, of 20 rows 1385 and 764.
 constexpr uint32_t kFewUpto = 17;
 
 // What a call launches and keeps, from the sizes that the host knows: the
@@ -68,6 +71,16 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   const uint64_t fewest = a.tokens > others ? a.tokens - others : 1;
   const bool few = fewest * group < kFewUpto, many = most * group >= kFewUpto;
   const int steps = steps_of(c.D);
+  // The least share and the largest tile that is not cut, in blocks.  Few rows: 8 blocks are one
+  // a wave; 8 requests of 250 tokens take 13 us, with shares of 16 blocks 19, of 32 31 us.  Tiles
+  // of up to 16 are not cut: 8 requests of 500 tokens take 16 us, cut from 8 on 19; one of 1000
+  // takes the same 20 us either way.  Many rows: 128 new tokens over 500 take 33 us, with shares
+  // of 8 blocks 54 us, 64 over 250 in 8 requests 23 and 40; of 2 blocks, over 2000, 68 instead of
+  // 50 us.  Tiles of up to 8 are not cut: one of 500 keys takes 33 us, cut from 4 on 43; up to 16,
+  // 8 requests of 64 over 1000 tokens take 47 instead of 42 us.
+  // Workgroups: as many as run at once, a CU each for few rows, which has 128 KB of loads under way
+  // then (64 requests of 16384 tokens take 451 us, and 454 with twice as many workgroups); for many
+  // rows see attend_many.
   if (few) l.few = divide(c, a, kFewRows, kFewBlock, 8, 16, 256, many);
   if (many) l.many = divide(c, a, many_rows(steps), kManyBlock, 4, 8, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
   if (few && many) l.few.upto = l.many.from = kFewUpto;

