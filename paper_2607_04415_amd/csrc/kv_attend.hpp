@@ -476,11 +476,21 @@ __device__ __forceinline__ float xor16(float x, float (*op)(float, float)) {
 __device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 
-// The largest of three, NaN passed over.  Written out: fmaxf of values that may be signalling
-// NaN quiets each of them first, an instruction a value.
-__device__ __forceinline__ float max3(float a, float b, float c) {
+// The largest, NaN passed over.  Written out: fmaxf of values that may be signalling NaN quiets
+// each of them first, an instruction a value.
+__device__ __forceinline__ float max16(const f32x16 &s) {
   float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  asm("v_max3_f32 %0, %1, %2, %3\n"
+      "v_max3_f32 %0, %0, %4, %5\n"
+      "v_max3_f32 %0, %0, %6, %7\n"
+      "v_max3_f32 %0, %0, %8, %9\n"
+      "v_max3_f32 %0, %0, %10, %11\n"
+      "v_max3_f32 %0, %0, %12, %13\n"
+      "v_max3_f32 %0, %0, %14, %15\n"
+      "v_max_f32 %0, %0, %16"
+      : "=&v"(r)
+      : "v"(s[0]), "v"(s[1]), "v"(s[2]), "v"(s[3]), "v"(s[4]), "v"(s[5]), "v"(s[6]), "v"(s[7]), "v"(s[8]), "v"(s[9]),
+        "v"(s[10]), "v"(s[11]), "v"(s[12]), "v"(s[13]), "v"(s[14]), "v"(s[15]));
   return r;
 }
 

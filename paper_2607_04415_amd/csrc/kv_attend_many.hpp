@@ -91,7 +91,6 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   const uint32_t token = fastdiv(row, p.group), gh = row - token * p.group.d;
   const int32_t base = w.r.len - w.r.added;
   const int32_t pos = base + (int32_t)token;
-  const int32_t oldest = (int32_t)max((int64_t)pos - p.window + 1, (int64_t)0);  // the window's first key
   const int32_t first = base + (int32_t)fastdiv(wave_row, p.group), last = base + (int32_t)fastdiv(wave_end, p.group);
   const uint32_t qhead = head * p.group.d + gh;
   const float scale = p.scale * (p.key_scale ? p.key_scale[head] : 1.f);
@@ -265,10 +264,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   };
   // The running maximum takes in 32 keys' scores; the sums are rescaled to it.
   auto rescale = [&](const f32x16 &s) __attribute__((always_inline)) {
-    float top = s[0];
-#pragma unroll
-    for (int i = 1; i < 15; i += 2) top = max3(top, s[i], s[i + 1]);
-    top = max3(top, s[15], s[15]);
+    float top = max16(s);
     top = __builtin_fmaf(xor32(top, max_of), mul, add);
     if (__any((top > best + kSlack) | (best == -INFINITY))) {
       const float to = fmaxf(best, top);
@@ -370,8 +366,12 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
     const bool any = (j0 <= last && (int64_t)j0 + kManyBlock - 1 > (int64_t)first - p.window) || j0 < w.r.prefix;
     const bool masked = !near | odd | (there != ~0ull);
     uint64_t sees = ~0ull;
-    if (masked)
-      sees = !any ? 0 : there & ((low_bits(pos - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(w.r.prefix - j0));
+    if (masked) {
+      int32_t here = pos;
+      asm("" : "+v"(here));  // what follows from it is worked out here, not kept in registers
+      const int32_t oldest = (int32_t)max((int64_t)here - p.window + 1, (int64_t)0);  // the window's first key
+      sees = !any ? 0 : there & ((low_bits(here - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(w.r.prefix - j0));
+    }
     auto mask = [&](f32x16 &s, uint32_t seen) __attribute__((always_inline)) {
       if (masked) {
         seen >>= g * 4;
@@ -446,8 +446,13 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
 
   sum = xor32(sum, sum_of);
   if ((uint32_t)wave * 32 + m >= tile.rows) return;
+  // the row again, which was not kept in registers
+  uint32_t n = m;
+  asm("" : "+v"(n));
+  n += tile.row0 + wave * 32;
+  const uint32_t token_out = fastdiv(n, p.group), head_out = head * p.group.d + (n - token_out * p.group.d);
   const bool divided = part.divided;
-  const uint64_t t_out = (uint64_t)(w.r.start + token);
+  const uint64_t t_out = (uint64_t)(w.r.start + token_out);
   const float vs = p.value_scale ? p.value_scale[head] : 1.f;
   const float norm = divided ? 1.f : sum != 0.f ? vs / sum : 0.f;
   const uint64_t slot = ((uint64_t)part.slot * p.kv_heads + head) * kManyRows + wave * 32 + m;
@@ -461,7 +466,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       if (divided)
         *reinterpret_cast<f32x4 *>(p.parts + slot * p.D + d) = y;
       else
-        *reinterpret_cast<u32x2 *>(p.out + t_out * p.out_stride + (uint64_t)qhead * p.D + d) =
+        *reinterpret_cast<u32x2 *>(p.out + t_out * p.out_stride + (uint64_t)head_out * p.D + d) =
             u32x2{Q::pack(y.x, y.y), Q::pack(y.z, y.w)};
     }
   if (g == 0) {
@@ -470,7 +475,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       ml[0] = best;
       ml[1] = sum;
     } else if (p.lse) {
-      p.lse[t_out * p.heads + qhead] = sum != 0.f ? (best + __log2f(sum)) * kLn2 : -INFINITY;
+      p.lse[t_out * p.heads + head_out] = sum != 0.f ? (best + __log2f(sum)) * kLn2 : -INFINITY;
     }
   }
 }
