@@ -27,9 +27,12 @@
 // that the matrix units take; the sum adds them before that rounding.
 //
 // Measured, 4096 new tokens after 12288, two heads of queries to each of 8:
-// 674 TF at D = 64, 732 at 96, 924 at 128, 472 at 192, 637 at 256 (heads past
-// 128 are computed as 256 elements, which also fill the registers), 915 at 128
-// from 8-bit pages; a large matrix product reaches 1210.
+// 660 TF at D = 64, 721 at 96, 894 at 128, 483 at 192, 647 at 256 (heads past
+// 128 are computed as 256 elements); from 8-bit pages 889 at 128 and 473 at
+// 256, where registers are spilled; with a cap, an exponential and a
+// reciprocal more a score, 744 at 128.  A large matrix product reaches 1210.
+// Counters at D = 128: the matrix units work 43% of the time, and a SIMD
+// issues 72% of it, 6.7 vector instructions beside each matrix instruction.
 #pragma once
 
 #include <type_traits>
@@ -480,8 +483,8 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   }
 }
 
-// Workgroups a CU: three for D <= 64 although some registers are spilled, outside the products
-// (8 requests of 1000 tokens over 8000: 127 us; two workgroups and no spills: 137), two for 96.
+// Workgroups a CU: three for D <= 64, in 168 registers (8 requests of 1000 tokens over 8000: 127
+// us; two workgroups, with room for more registers, 137), two for 96.
 template <typename Q, bool k8, int kSteps, int kMore>
 __global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps > 2 ? 2 : 3) void attend_many(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
