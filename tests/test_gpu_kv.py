@@ -252,6 +252,25 @@ def test_attend_scales(torch, news, scale):
     holds(torch, a, call(torch, a))
 
 
+@pytest.mark.parametrize("scale,cap", [(0.0, 0.0), (1e-36, 0.0), (-0.3, 0.0), (-0.3, 20.0), (0.0, 5.0), (0.7, 300.0)])
+@pytest.mark.parametrize("news", [[1, 4], [50, 30]])
+def test_attend_biased_scales(torch, news, scale, cap):
+    """Biases beside scores of no size, of both signs, capped and not, before and behind the tokens."""
+    a = setup(torch, 23, "f16", "f16", 4, 2, 64, 16, news, [150, 130], scale=scale, cap=cap, slopes=True,
+              prefix=[150, 20])
+    holds(torch, a, call(torch, a))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("news", [[1, 3], [40, 20]])
+def test_attend_biased_from_afar(torch, news, D):
+    """All pages near the tokens are missing: the distances are thousands, and so are the biases."""
+    a = setup(torch, D + 1, "f16", "f16", 2, 1, D, 16, news, [6000, 3001], slopes=True, poison=False)
+    a["tables"][:, 6:] = -1
+    a["slopes"] = [0.0, 0.5]
+    holds(torch, a, call(torch, a))
+
+
 @pytest.mark.parametrize("news", [[1, 1], [50, 3]])
 def test_attend_table_narrower_than_the_length(torch, news):
     a = setup(torch, 5, "bf16", "bf16", 4, 2, 64, 16, news, [150, 130], width=3)
