@@ -131,6 +131,25 @@ def test_store(torch, type, cache, T, H, D, page, scaled):
         assert np.array_equal(pool.float().cpu().numpy().reshape(-1, H, D), want, equal_nan=True)
 
 
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+def test_store_every_value_in_8_bits(torch, type):
+    """All 16-bit values by factors of all sizes: every quotient rounded to 32 bits, then to 8."""
+    factors = np.array([1.0, 0.013, 0.7 + 2**-24, 1 - 2**-24, 1 + 2**-23, 3.0, 1 / 448, -0.02, 2.0**-60, 2.0**-61,
+                        1.5e-39, 2.0**61, 3e38, 0.0, 7e-7, 1.0625 - 2**-23], np.float32)
+    H, D = len(factors), 64
+    rows = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(types(torch)[type]).reshape(-1, 1, D)
+    T = rows.shape[0]
+    k, v = (torch.zeros(T, H, 1, D).to(torch.float8_e4m3fn).cuda() for _ in range(2))
+    kv = g.KVCache(k, v, torch.from_numpy(factors).cuda(), torch.from_numpy(factors[::-1].copy()).cuda())
+    wide = rows.expand(T, H, D).contiguous().cuda()
+    kv.store(wide, wide, torch.arange(T, device="cuda"))
+    x = rows.float().numpy()
+    with np.errstate(all="ignore"):
+        for pool, by in ((k, factors), (v, factors[::-1])):
+            want = e4m3((x / by[:, None]).astype(np.float32).astype(np.float64))
+            assert np.array_equal(pool.float().cpu().numpy()[:, :, 0], want, equal_nan=True)
+
+
 # --------------------------------------------------------------------------- #
 # attend
 # --------------------------------------------------------------------------- #
