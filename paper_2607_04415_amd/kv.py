@@ -187,6 +187,8 @@ class KVCache:
             raise TypeError(f"keys must be bfloat16, float16 or float8_e4m3fn, not {keys.dtype}")
         if keys.dim() != 4:
             raise ValueError(f"keys must be (pages, heads, page_tokens, D), not {tuple(keys.shape)}")
+        if any(n > 1 and step == 0 for n, step in zip(keys.shape, keys.stride())):
+            raise ValueError(f"elements of keys must not share memory, its strides are {keys.stride()}")
         dev = _on_gpu("keys", keys)
         if (values.dtype, values.shape, values.stride(), values.device) != (
                 keys.dtype, keys.shape, keys.stride(), keys.device):
@@ -227,6 +229,8 @@ class KVCache:
         T, H, D = x.shape
         if (D > 1 and x.stride(2) != 1) or (H > 1 and x.stride(1) != D):
             raise ValueError(f"each token's heads in {name} must be contiguous")
+        if T > 1 and x.stride(0) < H * D:    # a stride of 0 would mean packed rows to the library
+            raise ValueError(f"rows of {name} must not share memory, its strides are {x.stride()}")
         if len(self._layouts) > 4096:
             self._layouts.clear()
         self._layouts[key] = known = code, (x.stride(0) if T > 1 else H * D)

@@ -82,3 +82,23 @@ def test_attach_and_plan_refusals(lib):
     assert lib.gorio_kv_attach(None, 1, 1, None, None, 1, 16, 4, 5, None, None, None, None, None) == g.EINVAL
     assert lib.gorio_kv_plan(None, None, 1, 16, None, 0, None, 0, 1, None, None, None, None, None, None) == g.EINVAL
     assert lib.gorio_kv_plan(None, None, 1 << 31, 16, None, 0, None, 1, 1, None, None, None, None, None, None) == g.EINVAL
+
+
+def test_rows_that_share_memory_are_refused():
+    """Strides of 0 mean packed rows to the library, which would read past an expanded tensor."""
+    torch = pytest.importorskip("torch")
+    one = torch.zeros(64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="share memory"):
+        g.KVCache(one.expand(10, 2, 16, 64), one.expand(10, 2, 16, 64))
+    with pytest.raises(ValueError, match="share memory"):
+        g.KVCache(torch.zeros(10, 1, 16, 64).bfloat16().expand(10, 2, 16, 64), None)
+    c = object.__new__(g.KVCache)               # what _rows needs of a cache, without a device
+    c.device, c.D, c._layouts, c._codes = one.device, 64, {}, {torch.bfloat16: kv.BF16}
+    with pytest.raises(ValueError, match="share memory"):
+        c._rows("q", torch.zeros(1, 4, 64).bfloat16().expand(3, 4, 64))
+    with pytest.raises(ValueError, match="share memory"):
+        c._rows("out", torch.zeros(1024).bfloat16().as_strided((3, 4, 64), (128, 64, 1)))
+    wide = torch.zeros(3, 6, 64).bfloat16()
+    assert c._rows("q", wide[:, :4]) == (kv.BF16, 6 * 64)
+    assert c._rows("q", wide[:1, :4]) == (kv.BF16, 4 * 64)
+    assert c._rows("q", wide[:1].expand(1, 6, 64)) == (kv.BF16, 6 * 64)
