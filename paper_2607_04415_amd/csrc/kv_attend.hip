@@ -29,8 +29,11 @@ gorio_status check(const gorio_kv_cache *cache, const gorio_kv_attention *a, gor
   if (a->out_stride == 0) out->out_stride = (uint64_t)a->heads * c->D;
   if (out->q_stride % 8 || out->out_stride % 8)
     return fail(GORIO_EINVAL, "q_stride and out_stride must be multiples of 8 elements");
-  if (!(a->cap >= 0.f) || !(a->cap <= 3e38f)) return fail(GORIO_EINVAL, "cap=%g, need a number >= 0", (double)a->cap);
-  if (!(a->scale <= 3e38f && a->scale >= -3e38f)) return fail(GORIO_EINVAL, "scale=%g", (double)a->scale);
+  // twice the cap, and the scale, are kept in log2: up to 1e38 neither overflows
+  if (!(a->cap >= 0.f) || !(a->cap <= 1e38f))
+    return fail(GORIO_EINVAL, "cap=%g, need a number in 0..1e38", (double)a->cap);
+  if (!(a->scale <= 1e38f && a->scale >= -1e38f))
+    return fail(GORIO_EINVAL, "scale=%g, need a number in -1e38..1e38", (double)a->scale);
   return GORIO_OK;
 }
 

@@ -211,8 +211,8 @@ extern "C" gorio_status gorio_kv_attach(const uint32_t *nodes, uint64_t requests
   if (requests == 0) return GORIO_OK;
   KvDevice dev;
   const gorio_status st = dev.use({{"nodes", nodes, 4, false},
-                                   {"first_page", first_page, 4, false},
-                                   {"tokens", tokens, 4, false},
+                                   {"first_page", first_page, 4, n == 0},
+                                   {"tokens", tokens, 4, n == 0},
                                    {"tables", tables, 4, false},
                                    {"fills", fills, 4, false},
                                    {"lens", lens, 4, false},

@@ -522,3 +522,9 @@ def test_refusals(torch):
     assert g.lib().gorio_kv_plan(host, lens.data_ptr(), 1, 16, None, 0, tables.data_ptr(), 1, 0, starts.data_ptr(),
                                  starts.data_ptr(), None, None, None, None) == g.EINVAL
     assert b"device pointer" in g.lib().gorio_last_error()
+
+
+def test_attach_without_passages(torch):
+    none = ints(torch, [])
+    tables, fills, lens, attached = g.kv_attach(ints(torch, [[-1, 3], [0, -1]]), none, none, 16, 4)
+    assert (tables == -1).all() and (fills == 16).all() and not lens.any() and not attached.any()

@@ -84,6 +84,12 @@ def test_attach_and_plan_refusals(lib):
     assert lib.gorio_kv_plan(None, None, 1 << 31, 16, None, 0, None, 1, 1, None, None, None, None, None, None) == g.EINVAL
 
 
+@pytest.mark.parametrize("more,text", [(dict(cap=2e38), "cap"), (dict(scale=2e38), "scale"), (dict(scale=-2e38), "scale")])
+def test_sizes_past_float32_in_log2_are_refused(lib, more, text):
+    assert workspace(lib, cache(), attention(**more))[0] == g.EINVAL
+    assert text in lib.gorio_last_error().decode()
+
+
 def test_rows_that_share_memory_are_refused():
     """Strides of 0 mean packed rows to the library, which would read past an expanded tensor."""
     torch = pytest.importorskip("torch")
