@@ -434,7 +434,7 @@ typedef struct {
                                (NULL: page_tokens) */
     const int32_t *prefix;  /* requests: its first positions, which every new token sees (NULL: 0) */
     const float *slopes;    /* heads: see below (NULL: 0) */
-    float scale, cap;       /* cap 0 = none */
+    float scale, cap;       /* cap 0 = none; cap and |scale| at most 1e38 */
     uint32_t window;        /* 0 = none */
     uint32_t max_new;       /* the most new tokens of a request, if the caller knows it (0: not);
                                chooses a kernel, and changes no result beyond rounding */
