@@ -68,10 +68,13 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   l.e4m3 = c.dtype == GORIO_KV_E4M3;
   l.more = a.cap > 0.f ? 2 : a.slopes ? 1 : 0;
   const uint64_t group = a.heads / c.heads;
-  // the most and the fewest new tokens of a request that has any; exact for one request
+  // The most new tokens of a request, and the fewest of one that has any, as far as the host can
+  // tell: rows of q may be padding, which counts as new tokens here, and max_new may be too small.
+  // So they decide only which form is the faster one.  `fewest` is at most `most`, so that one form
+  // is launched always, and a form launched alone takes requests of any number of rows.
   const uint64_t most = a.max_new ? std::min<uint64_t>(a.max_new, a.tokens) : a.tokens;
   const uint64_t others = (a.requests - 1) * most;
-  const uint64_t fewest = a.tokens > others ? a.tokens - others : 1;
+  const uint64_t fewest = a.tokens > others ? std::min(a.tokens - others, most) : 1;
   const bool few = fewest * group < kFewUpto, many = most * group >= kFewUpto;
   const int steps = steps_of(c.D);
   // The least share and the largest tile that is not cut, in blocks.  Few rows: 8 blocks are one

@@ -528,3 +528,19 @@ def test_attach_without_passages(torch):
     none = ints(torch, [])
     tables, fills, lens, attached = g.kv_attach(ints(torch, [[-1, 3], [0, -1]]), none, none, 16, 4)
     assert (tables == -1).all() and (fills == 16).all() and not lens.any() and not attached.any()
+
+
+@pytest.mark.parametrize("H,KV", [(2, 2), (8, 2), (17, 1)])
+@pytest.mark.parametrize("news,rows,max_new", [
+    ([1], 8, 1), ([1, 1, 0, 1], 64, 1), ([2, 1], 30, 2), ([1, 4], 40, 4),       # rows past the last start
+    ([1, 40], 41, 1), ([30], 30, 2), ([3, 1, 25], 60, 3)])                      # a hint that is too small
+def test_attend_rows_beyond_the_hint(torch, H, KV, news, rows, max_new):
+    """A batch padded to a fixed number of rows, and hints that are wrong: the named rows are all computed."""
+    a = setup(torch, 19, "bf16", "bf16", H, KV, 64, 16, news, [700, 90, 33, 640][:len(news)])
+    n = len(a["q"])
+    q = torch.zeros((rows, H, 64), dtype=torch.bfloat16, device="cuda")
+    q[:n] = a["q_gpu"]
+    out = torch.full_like(q, 5.0)
+    got, lse = call(torch, a, q=q, out=out, max_new=max_new)
+    holds(torch, a, (got[:n], lse[:n]))
+    assert (got[n:] == 5).all()

@@ -108,3 +108,14 @@ def test_rows_that_share_memory_are_refused():
     assert c._rows("q", wide[:, :4]) == (kv.BF16, 6 * 64)
     assert c._rows("q", wide[:1, :4]) == (kv.BF16, 4 * 64)
     assert c._rows("q", wide[:1].expand(1, 6, 64)) == (kv.BF16, 6 * 64)
+
+
+@pytest.mark.parametrize("kv_heads,group", [(8, 1), (8, 4), (1, 16), (1, 17), (2, 20)])
+def test_one_form_is_launched_whatever_rows_are_padding(lib, kv_heads, group):
+    """Rows of q may outnumber requests * max_new: over long texts every call needs room for cut tiles."""
+    for T in (1, 2, 7, 8, 64, 100, 5000):
+        for R in (1, 3, 60, 64, 700):
+            for most in (0, 1, 2, 16, 17, 400):
+                status, n = workspace(lib, cache(heads=kv_heads, D=128), attention(
+                    heads=kv_heads * group, requests=R, tokens=T, max_new=most, width=4096))
+                assert status == g.OK and n > 0, (T, R, most)
