@@ -503,7 +503,8 @@ gorio_status gorio_kv_store(const gorio_kv_cache *cache, gorio_kv_dtype dtype, c
  * visible to it if its table entry names a page, j % page_tokens is below the
  * page's fill, j < lens[b], and (j <= p and p - j < window, or j < prefix[b]).
  *   s_j = scale * (q . k_j); with a cap, s_j = cap * tanh(s_j / cap); then
- *   s_j -= slopes[h] * |p - j|   (with a cap, a score is good to 2^-22 of the cap)
+ *   s_j -= slopes[h] * |p - j|   (a capped score is good to 2^-15 up to a cap of 64, and to
+ *                                 2^-20 of itself past that)
  *   out = sum_j exp(s_j) v_j / sum_j exp(s_j) over the visible keys
  * Sums and the softmax are held in 32 bits, its weights rounded to q's type
  * for the product with the values.  A row that sees no key (or whose scores

@@ -66,7 +66,7 @@ AttendForm divide(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t
 AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint64_t *bytes) {
   AttendLaunch l{};
   l.e4m3 = c.dtype == GORIO_KV_E4M3;
-  l.more = a.cap > 0.f ? 2 : a.slopes ? 1 : 0;
+  l.more = a.cap > kQuickCap ? 3 : a.cap > 0.f ? 2 : a.slopes ? 1 : 0;
   const uint64_t group = a.heads / c.heads;
   // The most new tokens of a request, and the fewest of one that has any, as far as the host can
   // tell: rows of q may be padding, which counts as new tokens here, and max_new may be too small.

@@ -497,19 +497,42 @@ __device__ __forceinline__ float max16(const f32x16 &s) {
 // 2^x; -inf gives 0.
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Scores that are capped or biased, in log2: products x -> x * factor, or
+// Caps up to this one go by one exponential and one reciprocal a score, which is good to 2^-21 of
+// the cap then, 2^-15 at most.  Past it that error, which is as much of a weight, would grow with
+// the cap, so a score is worked out to 2^-20 of itself, in twelve more instructions: 4 chunks of
+// up to 500 tokens over 8192 take 171 us by a cap of 64 and 225 by one of 100, 4096 tokens over
+// 32768 2561 and 3618, 64 single tokens over 16384, which HBM bounds, 453 and 456.
+constexpr float kQuickCap = 64.f;
+
+// Scores that are capped or biased, in log2: products x -> x * scale log2 e, or
 // cap tanh(x scale / cap) log2 e, less slope * distance * log2 e.  With
-// E = 2^(2 x scale / cap log2 e), tanh = 1 - 2 / (1 + E), which is right at
+// E = 2^a, a = 2 x scale / cap log2 e, tanh = 1 - 2 / (1 + E), which is right at
 // both ends of E's range too; the quotient is below 1 and good to 2^-23, so the
-// result to about 2^-22 of the cap.
+// result to 2^-21 of the cap.  Where z = x scale / cap is below 1/2 that
+// difference loses the score, the more the smaller z is, and
+// z (1 - z^2 / 3 + 2 z^4 / 15 - ..) takes its place under a large cap.
 struct ScoreChange {
-  float factor, cap, twice, by, slope;
+  float to_log2, cap, twice, by, slope;
   __device__ __forceinline__ ScoreChange(float scale, float cap_, float slope_)
-      : factor(scale * kLog2e), cap(cap_ * kLog2e), twice(-2.f * cap_ * kLog2e),
+      : to_log2(scale * kLog2e), cap(cap_ * kLog2e), twice(-2.f * cap_ * kLog2e),
         by(cap_ > 0.f ? 2.f * kLog2e * scale / cap_ : 0.f), slope(-slope_ * kLog2e) {}
   // -1 / (1 + E): grows with the score, which is cap - twice * this
   __device__ __forceinline__ float quotient(float x) const { return __builtin_amdgcn_rcpf(-1.f - pow2(x * by)); }
   __device__ __forceinline__ float capped(float x) const { return __builtin_fmaf(quotient(x), -twice, cap); }
+  // the same for any cap.  The series of tanh(z) / z in z^2 = a^2 c up to z^14: at 1/2 the next
+  // term is 4e-9.
+  __device__ __forceinline__ float capped_exactly(float x) const {
+    constexpr float c = kLn2 / 2 * (kLn2 / 2);
+    const float t = x * to_log2, a = x * by, z2 = a * a * c;
+    float s = -929569.f / 638512875.f;
+    s = __builtin_fmaf(s, z2, 21844.f / 6081075.f);
+    s = __builtin_fmaf(s, z2, -1382.f / 155925.f);
+    s = __builtin_fmaf(s, z2, 62.f / 2835.f);
+    s = __builtin_fmaf(s, z2, -17.f / 315.f);
+    s = __builtin_fmaf(s, z2, 2.f / 15.f);
+    s = __builtin_fmaf(s, z2, -1.f / 3.f);
+    return fabsf(a) < kLog2e ? __builtin_fmaf(t * z2, s, t) : capped(x);
+  }
   // y less the bias at this distance
   __device__ __forceinline__ float biased(float y, float distance) const {
     return __builtin_fmaf(slope, fabsf(distance), y);

@@ -150,7 +150,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     for (int i = 0; i < 8; ++i) {
       float y = s2[i >> 2][i & 3];
       if constexpr (kMore) {
-        y = p.cap > 0.f ? change.capped(y) : y * to_log2;
+        y = p.cap > kQuickCap ? change.capped_exactly(y) : p.cap > 0.f ? change.capped(y) : y * change.to_log2;
         if (p.slopes) y = change.biased(y, (float)(pos - j0 - g * 4) - (float)((i >> 2) * 16 + (i & 3)));
       } else {
         y *= to_log2;

@@ -55,7 +55,8 @@ constexpr int kManyBlock = 64;  // keys
 constexpr float kSlack = 8.f;
 
 // kSteps: D <= 32 kSteps.  k8: pages of 8-bit values.  kMore: 1 if scores are biased, 2 if they
-// are capped, and biased if there are slopes.
+// are capped, and biased if there are slopes, 3 the same by a cap past kQuickCap (kernels of their
+// own: a branch in those of 2 made these spill up to 40 registers more, for caps of any size).
 template <typename Q, bool k8, int kSteps, int kMore>
 __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
                                           const KeyRange &range, const Part &part, uint32_t head) {
@@ -99,8 +100,8 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   const float scale = p.scale * (p.key_scale ? p.key_scale[head] : 1.f);
   // the running maximum is taken of the products as they are, so the factor has to be positive:
   // a negative one turns the queries' signs around
-  constexpr bool capped = kMore == 2;
-  const bool biased = kMore == 1 || (kMore == 2 && p.slopes);
+  constexpr bool capped = kMore >= 2, large = kMore == 3;
+  const bool biased = kMore == 1 || (capped && p.slopes);
   const uint32_t flip = !capped && scale < 0.f ? 0x80008000u : 0u;
   // 0 times a masked score's -inf would be NaN, and a bias is divided by it
   const float factor = scale == 0.f || (biased && fabsf(scale) < 1e-30f) ? 1e-30f : fabsf(scale) * kLog2e;
@@ -233,9 +234,9 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   }
   // A score in log2 is s * mul + add.  Without a cap s is the product, to which the bias is
   // added as what the product starts from.  With a cap s is -1 / (1 + E) (see ScoreChange), or,
-  // if there is a bias as well, the score itself.
-  const float mul = !capped ? factor : biased ? 1.f : -change.twice;
-  const float add = capped && !biased ? change.cap : 0.f;
+  // if the cap is large or there is a bias as well, the score itself.
+  const float mul = !capped ? factor : biased || large ? 1.f : -change.twice;
+  const float add = capped && !biased && !large ? change.cap : 0.f;
   const float start_slope = biased && !capped ? change.slope / factor : 0.f;
   auto start = [&](f32x16 &s, int32_t j) __attribute__((always_inline)) {
     if constexpr (kMore == 1) {
@@ -256,12 +257,21 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   auto changed = [&](f32x16 &s, int32_t j0) __attribute__((always_inline)) {
     if constexpr (capped) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = change.quotient(s[i]);
+      for (int i = 0; i < 16; ++i) {
+        if constexpr (large) {
+          s[i] = change.capped_exactly(s[i]);
+          __builtin_amdgcn_sched_barrier(0);  // one score's registers at a time
+        } else {
+          s[i] = change.quotient(s[i]);
+        }
+      }
       if (biased) {
         const float distance = (float)(pos - j0 - g * 4);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          s[i] = change.biased(__builtin_fmaf(s[i], -change.twice, change.cap), distance - (float)((i >> 2) * 8 + (i & 3)));
+        for (int i = 0; i < 16; ++i) {
+          if constexpr (!large) s[i] = __builtin_fmaf(s[i], -change.twice, change.cap);
+          s[i] = change.biased(s[i], distance - (float)((i >> 2) * 8 + (i & 3)));
+        }
       }
     }
   };

@@ -15,7 +15,7 @@ struct AttendForm {
 
 struct AttendLaunch {
   bool e4m3;  // 8-bit pages
-  int more;   // 1 if scores are biased, 2 if they are capped
+  int more;   // 1 if scores are biased, 2 if they are capped, 3 if by a cap past kQuickCap
   AttendForm few, many;
 };
 
@@ -49,7 +49,8 @@ hipError_t launch_steps(const AttendParams &p, const AttendLaunch &l, hipStream_
   switch (l.more) {
     case 0: return launch_forms<Q, k8, kSteps, 0>(p, l, s);
     case 1: return launch_forms<Q, k8, kSteps, 1>(p, l, s);
-    default: return launch_forms<Q, k8, kSteps, 2>(p, l, s);
+    case 2: return launch_forms<Q, k8, kSteps, 2>(p, l, s);
+    default: return launch_forms<Q, k8, kSteps, 3>(p, l, s);
   }
 }
 

@@ -260,9 +260,8 @@ class KVCache:
         fills (as tables): tokens that each page holds.  prefix (requests): the
         first positions, which all of a request's new tokens see.  slopes
         (heads, float32): a score loses slope * distance.  scale: 1/sqrt(D) by
-        default.  cap: scores become cap * tanh(score / cap), good to 2^-22 of the
-        cap.  window: the distance from which a key outside the prefix is not seen
-        (0: none).
+        default.  cap: scores become cap * tanh(score / cap).  window: the distance
+        from which a key outside the prefix is not seen (0: none).
         max_new: the most new tokens of a request, where the program knows it."""
         torch, L = _bind()
         dev, i32 = self.device, torch.int32
