@@ -515,7 +515,8 @@ struct ScoreChange {
   float to_log2, cap, twice, by, slope;
   __device__ __forceinline__ ScoreChange(float scale, float cap_, float slope_)
       : to_log2(scale * kLog2e), cap(cap_ * kLog2e), twice(-2.f * cap_ * kLog2e),
-        by(cap_ > 0.f ? 2.f * kLog2e * scale / cap_ : 0.f), slope(-slope_ * kLog2e) {}
+        // finite under a cap of no size too: a product of 0 stays one
+        by(cap_ > 0.f ? fminf(fmaxf(2.f * kLog2e * scale / cap_, -3e38f), 3e38f) : 0.f), slope(-slope_ * kLog2e) {}
   // -1 / (1 + E): grows with the score, which is cap - twice * this
   __device__ __forceinline__ float quotient(float x) const { return __builtin_amdgcn_rcpf(-1.f - pow2(x * by)); }
   __device__ __forceinline__ float capped(float x) const { return __builtin_fmaf(quotient(x), -twice, cap); }

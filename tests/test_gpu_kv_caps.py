@@ -52,3 +52,18 @@ def test_caps(torch, cap, spread, news, D, slopes):  # noqa: F811
     w_out, w_lse, bound, lse_bound = attend(a)
     assert (np.abs(lse - w_lse) <= lse_bound).all(), np.abs(lse - w_lse).max()
     assert (np.abs(out - w_out) <= bound).all(), np.abs(out - w_out).max()
+
+
+@pytest.mark.parametrize("news", [[1, 4], [50, 30]])
+@pytest.mark.parametrize("cap,scale", [(1e-42, 0.125), (1e-42, -0.125), (1e-3, 1e37)])
+def test_caps_of_no_size(torch, cap, scale, news):  # noqa: F811
+    """scale / cap passes float32: scores are 0 or the cap, and products of 0 stay 0."""
+    a = setup(torch, 31, "f16", "f16", 4, 2, 64, 16, news, [150, 130], cap=cap, scale=scale)
+    a["q_gpu"][::2] = 0
+    a["q"][::2] = 0
+    a["cap"] = cap
+    out, lse = (x.double().cpu().numpy() for x in call(torch, a))
+    w_out, w_lse, bound, _ = attend({**a, "scale": min(abs(scale), 1.0) * np.sign(scale)})
+    assert np.isfinite(out).all() and np.isfinite(lse).all()
+    few = 2.0 ** -15
+    assert (np.abs(lse - w_lse) <= few).all() and (np.abs(out - w_out) <= bound + few * np.abs(a["values"]).max()).all()
