@@ -446,7 +446,8 @@ typedef struct {
  * of the table gets the pages of nodes[b][0], nodes[b][1], ... one passage
  * after the other, each from a page's first place, as long as whole passages
  * fit into `limit` entries: the first that does not fit ends the row.  Ids at
- * or past n (a search's padding) are passed over.
+ * or past n (a search's padding) and passages that have no pages, whose first
+ * page is negative, are passed over.
  *   nodes:    requests x k (1 <= k <= 1024), e.g. from gorio_search.
  *   tables, fills: requests x width out: pages and the tokens that each holds;
  *             entries past the passages get -1 and page_tokens.

@@ -59,9 +59,10 @@ __global__ __launch_bounds__(kThreads) void attach_kernel(const uint32_t *nodes,
     bool node = false;
     if (r < k) {
       const uint32_t v = nodes[b * k + r];
-      node = v < n;
-      const int32_t held = node ? max(tokens[v], 0) : 0;
-      s_first[r] = node ? first_page[v] : -1;
+      const int32_t first = v < n ? first_page[v] : -1, all = v < n ? tokens[v] : 0;
+      node = first >= 0;
+      const int32_t held = node ? max(all, 0) : 0;
+      s_first[r] = first;
       s_held[r] = held;
       count = pages_of(held, page_tokens);
     }
@@ -98,7 +99,7 @@ __global__ __launch_bounds__(kThreads) void attach_kernel(const uint32_t *nodes,
         else lo = mid + 1;
       }
       const uint32_t i = e - (uint32_t)(s_end[lo] - pages_of(s_held[lo], page_tokens));
-      page = s_first[lo] + (int32_t)i;
+      page = max((int32_t)((uint32_t)s_first[lo] + i), -1);  // past 2^31 - 1 there is none
       fill = min(s_held[lo] - (int32_t)(i * page_tokens.d), (int32_t)page_tokens.d);
     }
     tables[b * width + e] = page;

@@ -112,8 +112,9 @@ def _count(name: str, value, least: int = 0) -> int:
 def kv_attach(nodes, first_page, tokens, page_tokens: int, width: int, limit: int | None = None):
     """(tables, fills, lens, attached): the pages of the passages that a search
     returned (gorio_kv_attach).  nodes: requests x k int32 or uint32 ids, as
-    Index.search returns them; first_page, tokens: int32 per node; limit: table
-    entries that passages may take of the `width` (default: all)."""
+    Index.search returns them; first_page, tokens: int32 per node, a first page
+    below 0 for one that has no pages and is passed over; limit: table entries
+    that passages may take of the `width` (default: all)."""
     torch, L = _bind()
     dev = _on_gpu("nodes", nodes)
     if nodes.dim() != 2:

@@ -544,3 +544,22 @@ def test_attend_rows_beyond_the_hint(torch, H, KV, news, rows, max_new):
     got, lse = call(torch, a, q=q, out=out, max_new=max_new)
     holds(torch, a, (got[:n], lse[:n]))
     assert (got[n:] == 5).all()
+
+
+@pytest.mark.parametrize("B,k", [(1, 4), (3, 300)])
+def test_attach_passes_over_passages_without_pages(torch, B, k):
+    """A first page below 0: as if the id were not there.  Pages past the largest name none."""
+    rng = np.random.default_rng([B, k])
+    n, page, width = 60, 8, 700
+    tokens = rng.integers(0, 4 * page, n).astype(np.int32)
+    first = rng.integers(0, 1000, n).astype(np.int32)
+    first[::3] = -1
+    first[4] = -2**31
+    nodes = rng.integers(0, n, (B, k)).astype(np.int32)
+    nodes[:, :4] = [3, 4, 5, 6]
+    want = ref.attach(np.where(first[nodes] < 0, -1, nodes), first, tokens, page, width, width)
+    got = g.kv_attach(ints(torch, nodes), ints(torch, first), ints(torch, tokens), page, width)
+    for x, y in zip(got, want):
+        assert np.array_equal(x.cpu().numpy(), y)
+    tables, fills, lens, _ = g.kv_attach(ints(torch, [[0]]), ints(torch, [2**31 - 2]), ints(torch, [4 * page]), page, 6)
+    assert tables.tolist() == [[2**31 - 2, 2**31 - 1, -1, -1, -1, -1]] and lens.tolist() == [4 * page]
