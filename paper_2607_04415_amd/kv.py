@@ -11,6 +11,8 @@ values are kept in pages in HBM:
 
 Argument marshalling only; the work is done by the library's HIP kernels, on
 torch's current stream of the tensors' device.  Nothing waits for the GPU.
+The calls serve: there are no gradients through pages, and tensors that require
+one are refused where torch records gradients.
 """
 from __future__ import annotations
 
@@ -100,6 +102,11 @@ def _on_gpu(name: str, a):
     if not a.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     return a.device
+
+
+def _no_gradients():
+    raise ValueError("attend and store compute no gradients: call them under torch.no_grad(), or with tensors that "
+                     "require none")
 
 
 def _count(name: str, value, least: int = 0) -> int:
@@ -241,6 +248,8 @@ class KVCache:
         """Keys and values of new tokens (tokens x heads x D each; rows may be
         parts of wider ones) into their slots (int64; below 0: not stored)."""
         torch, L = _bind()
+        if (keys.requires_grad or values.requires_grad) and torch.is_grad_enabled():
+            _no_gradients()
         code, key_stride = self._rows("keys", keys, self.heads)
         code2, value_stride = self._rows("values", values, self.heads)
         if code != code2 or keys.shape != values.shape:
@@ -266,6 +275,9 @@ class KVCache:
         max_new: the most new tokens of a request, where the program knows it."""
         torch, L = _bind()
         dev, i32 = self.device, torch.int32
+        if (q.requires_grad or self.keys.requires_grad or self.values.requires_grad or (
+                slopes is not None and slopes.requires_grad)) and torch.is_grad_enabled():
+            _no_gradients()
         code, q_stride = self._rows("q", q)
         T, H, D = q.shape
         B, width = tables.shape

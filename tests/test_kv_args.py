@@ -119,3 +119,24 @@ def test_one_form_is_launched_whatever_rows_are_padding(lib, kv_heads, group):
                 status, n = workspace(lib, cache(heads=kv_heads, D=128), attention(
                     heads=kv_heads * group, requests=R, tokens=T, max_new=most, width=4096))
                 assert status == g.OK and n > 0, (T, R, most)
+
+
+def test_gradients_are_refused_not_dropped(lib):
+    torch = pytest.importorskip("torch")
+    pages = torch.zeros(10, 2, 16, 64).bfloat16()
+    c = object.__new__(g.KVCache)               # refused before anything that needs a device
+    c.device, c.D, c.heads, c._layouts, c._codes = pages.device, 64, 2, {}, {torch.bfloat16: kv.BF16}
+    c.keys, c.values, c.key_scale, c.value_scale = pages, pages.clone(), None, None
+    rows = torch.zeros(3, 2, 64).bfloat16()
+    wants = rows.clone().requires_grad_()
+    slopes = torch.zeros(2, requires_grad=True)
+    ints = [torch.zeros(shape, dtype=torch.int32) for shape in ((2,), (1,), (1, 4))]
+    for call in (lambda: c.attend(wants, *ints), lambda: c.attend(rows, *ints, slopes=slopes),
+                 lambda: c.store(wants, rows, None), lambda: c.store(rows, wants, None)):
+        with pytest.raises(ValueError, match="no gradients"):
+            call()
+    c.values.requires_grad_()
+    with pytest.raises(ValueError, match="no gradients"):
+        c.attend(rows, *ints)
+    with torch.no_grad(), pytest.raises(TypeError, match="slots"):
+        c.store(wants, rows, torch.zeros(3))
