@@ -476,21 +476,25 @@ __device__ __forceinline__ float xor16(float x, float (*op)(float, float)) {
 __device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 
-// The largest, NaN passed over.  Written out: fmaxf of values that may be signalling NaN quiets
-// each of them first, an instruction a value.
+// The largest, NaN passed over (where all of a pair are NaN, it may be +inf).  Written out: fmaxf
+// of values that may be signalling NaN quiets each of them first, an instruction a value.  The
+// first two are compared by the compiler, as the middle one of them and +inf: it then waits, if it
+// has to, until the matrix instruction that gives the scores is done, which it does not do for
+// registers that inline assembly reads.
 __device__ __forceinline__ float max16(const f32x16 &s) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3\n"
-      "v_max3_f32 %0, %0, %4, %5\n"
-      "v_max3_f32 %0, %0, %6, %7\n"
-      "v_max3_f32 %0, %0, %8, %9\n"
-      "v_max3_f32 %0, %0, %10, %11\n"
-      "v_max3_f32 %0, %0, %12, %13\n"
-      "v_max3_f32 %0, %0, %14, %15\n"
-      "v_max_f32 %0, %0, %16"
-      : "=&v"(r)
-      : "v"(s[0]), "v"(s[1]), "v"(s[2]), "v"(s[3]), "v"(s[4]), "v"(s[5]), "v"(s[6]), "v"(s[7]), "v"(s[8]), "v"(s[9]),
-        "v"(s[10]), "v"(s[11]), "v"(s[12]), "v"(s[13]), "v"(s[14]), "v"(s[15]));
+  float inf = INFINITY;
+  asm volatile("" : "+s"(inf));  // the middle of three with a constant inf would become fmaxf
+  float r = __builtin_amdgcn_fmed3f(s[0], s[1], inf);
+  asm("v_max3_f32 %0, %0, %1, %2\n"
+      "v_max3_f32 %0, %0, %3, %4\n"
+      "v_max3_f32 %0, %0, %5, %6\n"
+      "v_max3_f32 %0, %0, %7, %8\n"
+      "v_max3_f32 %0, %0, %9, %10\n"
+      "v_max3_f32 %0, %0, %11, %12\n"
+      "v_max3_f32 %0, %0, %13, %14"
+      : "+&v"(r)
+      : "v"(s[2]), "v"(s[3]), "v"(s[4]), "v"(s[5]), "v"(s[6]), "v"(s[7]), "v"(s[8]), "v"(s[9]), "v"(s[10]), "v"(s[11]),
+        "v"(s[12]), "v"(s[13]), "v"(s[14]), "v"(s[15]));
   return r;
 }
 
