@@ -480,21 +480,27 @@ __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 // of values that may be signalling NaN quiets each of them first, an instruction a value.  The
 // first two are compared by the compiler, as the middle one of them and +inf: it then waits, if it
 // has to, until the matrix instruction that gives the scores is done, which it does not do for
-// registers that inline assembly reads.
+// registers that inline assembly reads.  kReciprocals: capped scores may come from a reciprocal
+// right before the assembly, which waits a state for it itself.
+template <bool kReciprocals>
 __device__ __forceinline__ float max16(const f32x16 &s) {
   float inf = INFINITY;
   asm volatile("" : "+s"(inf));  // the middle of three with a constant inf would become fmaxf
   float r = __builtin_amdgcn_fmed3f(s[0], s[1], inf);
-  asm("v_max3_f32 %0, %0, %1, %2\n"
-      "v_max3_f32 %0, %0, %3, %4\n"
-      "v_max3_f32 %0, %0, %5, %6\n"
-      "v_max3_f32 %0, %0, %7, %8\n"
-      "v_max3_f32 %0, %0, %9, %10\n"
-      "v_max3_f32 %0, %0, %11, %12\n"
-      "v_max3_f32 %0, %0, %13, %14"
-      : "+&v"(r)
-      : "v"(s[2]), "v"(s[3]), "v"(s[4]), "v"(s[5]), "v"(s[6]), "v"(s[7]), "v"(s[8]), "v"(s[9]), "v"(s[10]), "v"(s[11]),
-        "v"(s[12]), "v"(s[13]), "v"(s[14]), "v"(s[15]));
+#define GORIO_MAX14(first)                                                                                            \
+  asm(first "v_max3_f32 %0, %0, %1, %2\n"                                                                             \
+            "v_max3_f32 %0, %0, %3, %4\n"                                                                             \
+            "v_max3_f32 %0, %0, %5, %6\n"                                                                             \
+            "v_max3_f32 %0, %0, %7, %8\n"                                                                             \
+            "v_max3_f32 %0, %0, %9, %10\n"                                                                            \
+            "v_max3_f32 %0, %0, %11, %12\n"                                                                           \
+            "v_max3_f32 %0, %0, %13, %14"                                                                             \
+      : "+&v"(r)                                                                                                      \
+      : "v"(s[2]), "v"(s[3]), "v"(s[4]), "v"(s[5]), "v"(s[6]), "v"(s[7]), "v"(s[8]), "v"(s[9]), "v"(s[10]),           \
+        "v"(s[11]), "v"(s[12]), "v"(s[13]), "v"(s[14]), "v"(s[15]))
+  if constexpr (kReciprocals) GORIO_MAX14("s_nop 0\n");
+  else GORIO_MAX14("");
+#undef GORIO_MAX14
   return r;
 }
 

@@ -277,7 +277,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   };
   // The running maximum takes in 32 keys' scores; the sums are rescaled to it.
   auto rescale = [&](const f32x16 &s) __attribute__((always_inline)) {
-    float top = max16(s);
+    float top = max16<capped>(s);
     top = __builtin_fmaf(xor32(top, max_of), mul, add);
     if (__any((top > best + kSlack) | (best == -INFINITY))) {
       const float to = fmaxf(best, top);
