@@ -455,6 +455,7 @@ typedef struct {
  *             next position (a passage's last page is never written to by a
  *             request), and the prefix for gorio_kv_attend.
  *   attached: requests out, or NULL: passages in the row.
+ * No array that is written overlaps another.
  */
 gorio_status gorio_kv_attach(const uint32_t *nodes, uint64_t requests, uint32_t k,
                              const int32_t *first_page, const int32_t *tokens, uint64_t n,
@@ -476,7 +477,8 @@ gorio_status gorio_kv_attach(const uint32_t *nodes, uint64_t requests, uint32_t 
  *             where it has no page; -1 both past the last new token; new
  *             tokens past `tokens` are left out).
  *   taken:    1 out: pages that the entries needed, which may pass n_free.
- * positions, slots and taken may be NULL.  lens and before are different arrays.
+ * positions, slots and taken may be NULL.  lens and before are different arrays;
+ * no array that is written overlaps another.
  */
 gorio_status gorio_kv_plan(const int32_t *before, const int32_t *added, uint64_t requests,
                            uint32_t page_tokens, const int32_t *free_pages, uint64_t n_free,

@@ -63,6 +63,23 @@ class KvDevice {
   int prev_ = -1;
 };
 
+// Arrays of a call whose blocks run in any order: one that is written shares no byte with another.
+struct KvSpan {
+  const char *name;
+  const void *ptr;  // NULL: none
+  uint64_t bytes;
+  bool written;
+};
+inline gorio_status kv_apart(std::initializer_list<KvSpan> spans) {
+  for (const KvSpan *a = spans.begin(); a != spans.end(); ++a)
+    for (const KvSpan *b = a + 1; b != spans.end(); ++b) {
+      const uintptr_t x = (uintptr_t)a->ptr, y = (uintptr_t)b->ptr;
+      if ((a->written || b->written) && x && y && a->bytes && b->bytes && x < y + b->bytes && y < x + a->bytes)
+        return fail(GORIO_EINVAL, "%s and %s overlap", a->name, b->name);
+    }
+  return GORIO_OK;
+}
+
 inline gorio_status kv_launched(const char *what) {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? GORIO_OK : fail(GORIO_EDEVICE, "%s: %s", what, hipGetErrorString(e));

@@ -211,13 +211,21 @@ extern "C" gorio_status gorio_kv_attach(const uint32_t *nodes, uint64_t requests
   if (limit > width) return fail(GORIO_EINVAL, "limit=%u above width=%u", limit, width);
   if (requests == 0) return GORIO_OK;
   KvDevice dev;
-  const gorio_status st = dev.use({{"nodes", nodes, 4, false},
-                                   {"first_page", first_page, 4, n == 0},
-                                   {"tokens", tokens, 4, n == 0},
-                                   {"tables", tables, 4, false},
-                                   {"fills", fills, 4, false},
-                                   {"lens", lens, 4, false},
-                                   {"attached", attached, 4, true}});
+  gorio_status st = dev.use({{"nodes", nodes, 4, false},
+                             {"first_page", first_page, 4, n == 0},
+                             {"tokens", tokens, 4, n == 0},
+                             {"tables", tables, 4, false},
+                             {"fills", fills, 4, false},
+                             {"lens", lens, 4, false},
+                             {"attached", attached, 4, true}});
+  if (st != GORIO_OK) return st;
+  st = kv_apart({{"nodes", nodes, 4 * requests * k, false},
+                 {"first_page", first_page, 4 * n, false},
+                 {"tokens", tokens, 4 * n, false},
+                 {"tables", tables, 4 * requests * width, true},
+                 {"fills", fills, 4 * requests * width, true},
+                 {"lens", lens, 4 * requests, true},
+                 {"attached", attached, 4 * requests, true}});
   if (st != GORIO_OK) return st;
   attach_kernel<<<(uint32_t)requests, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
       nodes, k, first_page, tokens, n, make_fastdiv(page_tokens), width, limit, tables, fills, lens, attached);
@@ -236,15 +244,25 @@ extern "C" gorio_status gorio_kv_plan(const int32_t *before, const int32_t *adde
   if (requests == 0) return GORIO_OK;
   if (lens == before) return fail(GORIO_EINVAL, "lens and before are the same array");
   KvDevice dev;
-  const gorio_status st = dev.use({{"before", before, 4, false},
-                                   {"added", added, 4, false},
-                                   {"free_pages", free_pages, 4, n_free == 0},
-                                   {"tables", tables, 4, false},
-                                   {"lens", lens, 4, false},
-                                   {"starts", starts, 4, false},
-                                   {"positions", positions, 4, true},
-                                   {"slots", slots, 8, true},
-                                   {"taken", taken, 4, true}});
+  gorio_status st = dev.use({{"before", before, 4, false},
+                             {"added", added, 4, false},
+                             {"free_pages", free_pages, 4, n_free == 0},
+                             {"tables", tables, 4, false},
+                             {"lens", lens, 4, false},
+                             {"starts", starts, 4, false},
+                             {"positions", positions, 4, true},
+                             {"slots", slots, 8, true},
+                             {"taken", taken, 4, true}});
+  if (st != GORIO_OK) return st;
+  st = kv_apart({{"before", before, 4 * requests, false},
+                 {"added", added, 4 * requests, false},
+                 {"free_pages", free_pages, 4 * n_free, false},
+                 {"tables", tables, 4 * requests * width, true},
+                 {"lens", lens, 4 * requests, true},
+                 {"starts", starts, 4 * (requests + 1), true},
+                 {"positions", positions, 4 * tokens, true},
+                 {"slots", slots, 8 * tokens, true},
+                 {"taken", taken, 4, true}});
   if (st != GORIO_OK) return st;
   PlanParams p;
   p.before = before;

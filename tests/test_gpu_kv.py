@@ -563,3 +563,35 @@ def test_attach_passes_over_passages_without_pages(torch, B, k):
         assert np.array_equal(x.cpu().numpy(), y)
     tables, fills, lens, _ = g.kv_attach(ints(torch, [[0]]), ints(torch, [2**31 - 2]), ints(torch, [4 * page]), page, 6)
     assert tables.tolist() == [[2**31 - 2, 2**31 - 1, -1, -1, -1, -1]] and lens.tolist() == [4 * page]
+
+
+def test_arrays_that_are_written_overlap_no_other(torch):
+    """Blocks run in any order: lens where added lies would be read by one after another has written it."""
+    L, B, width, T = g.lib(), 3, 4, 6
+    x = ints(torch, np.zeros(200))
+    at = lambda i: x.data_ptr() + 4 * i
+    plan = dict(before=at(0), added=at(3), free=at(8), tables=at(20), lens=at(40), starts=at(44), positions=at(50),
+                slots=at(60), taken=at(80))
+
+    def status(**more):
+        a = {**plan, **more}
+        return L.gorio_kv_plan(a["before"], a["added"], B, 16, a["free"], 5, a["tables"], width, T, a["lens"],
+                               a["starts"], a["positions"], a["slots"], a["taken"], None)
+
+    assert status() == g.OK and status(positions=None, slots=None, taken=None) == g.OK
+    assert L.gorio_kv_plan(at(0), at(3), B, 16, at(21), 0, at(20), width, T, at(40), at(44), at(50), at(60), at(80),
+                           None) == g.OK              # no free page, wherever it points
+    for name, where in (("lens", at(3)), ("lens", at(5)), ("starts", at(2)), ("starts", at(42)), ("tables", at(12)),
+                        ("positions", at(19)), ("slots", at(52)), ("taken", at(31)), ("taken", at(4))):
+        assert status(**{name: where}) == g.EINVAL, (name, where)
+        assert b"overlap" in L.gorio_last_error()
+    attach = lambda tables, fills, lens, attached: L.gorio_kv_attach(
+        at(0), B, 2, at(10), at(20), 5, 16, width, width, tables, fills, lens, attached, None)
+    assert attach(at(30), at(42), at(54), at(57)) == g.OK and attach(at(30), at(42), at(54), None) == g.OK
+    for arrays in ((at(5), at(42), at(54), at(57)), (at(30), at(41), at(54), at(57)), (at(30), at(42), at(24), at(57)),
+                   (at(30), at(42), at(54), at(56))):
+        assert attach(*arrays) == g.EINVAL and b"overlap" in L.gorio_last_error()
+    torch.cuda.synchronize()
+    empty = [torch.empty(0, dtype=torch.int32, device="cuda") for _ in range(2)]
+    p = g.kv_plan(ints(torch, [0]), ints(torch, [0]), empty[0], ints(torch, [[-1]]), 16, 0)
+    assert p.lens.tolist() == [0] and p.taken.tolist() == [0]
