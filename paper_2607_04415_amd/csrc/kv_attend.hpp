@@ -13,8 +13,6 @@
 
 #include <hip/hip_runtime.h>
 
-#include <type_traits>
-
 #include "kv.hpp"
 
 namespace gorio {
@@ -600,15 +598,6 @@ __device__ __forceinline__ f32x4 not_finite_part(u32x4 a, u32x4 seen) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = not_finite_sum(up[i], down[i]);
   return r;
-}
-
-// f(0), f(1), .. f(n - 1) with numbers that are constants.
-template <int n, int i = 0, typename F>
-__device__ __forceinline__ void each(F &&f) {
-  if constexpr (i < n) {
-    f(std::integral_constant<int, i>{});
-    each<n, i + 1>(static_cast<F &&>(f));
-  }
 }
 
 // The low n bits, n of any size.
