@@ -227,7 +227,7 @@ struct WorkItem {
 
 __device__ __forceinline__ uint32_t tiles_of(const AttendParams &p, const Request &r) {
   const uint32_t rows = (uint32_t)r.added * p.group.d;
-  return (rows >= p.from) & (rows < p.upto) ? (rows + p.rows - 1) / p.rows : 0;
+  return ((rows >= p.from) & (rows < p.upto)) ? (rows + p.rows - 1) / p.rows : 0;
 }
 
 // Rows of a tile: row n is token n / group of the request's new ones, head
@@ -560,7 +560,10 @@ __device__ __forceinline__ bool any_not_finite(uint32_t w) {
 }
 template <typename Q>
 __device__ __forceinline__ bool any_not_finite4(u32x4 a) {
-  return any_not_finite<Q>(a.x) | any_not_finite<Q>(a.y) | any_not_finite<Q>(a.z) | any_not_finite<Q>(a.w);
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) any |= any_not_finite<Q>(a[i]);
+  return any;
 }
 template <typename Q>
 __device__ __forceinline__ u32x4 finite_only(u32x4 a) {

@@ -317,8 +317,9 @@ __global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParam
 }
 
 // Joins the parts of divided tiles: a workgroup a share and head, for the tile that begins in the
-// share and is cut at its end; 16 rows, 16 threads a row, so that a row's loads wait once (64 rows
-// a workgroup, four after the other: 128 new tokens over 2000 took 54 us in all, now 41).
+// share and is cut at its end; 16 rows, 16 threads a row (64 rows a workgroup, four after the other:
+// 128 new tokens over 2000 took 54 us in all, now 41).  A row's parts are added one after the
+// other, and each waits for its loads.
 //   out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts i
 // Bound by the latency of two dependent loads, 4 us, and for many tiles by reading the parts
 // (750 cut tiles of 128 rows, 64 elements: 50 MB in 14 us).
@@ -352,7 +353,6 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
         all = fmaf(ml[at + 1], by, all);
       }
       const uint32_t some = min(parts - i0, 16u);
-#pragma unroll 4
       for (uint32_t i = 0; i < some; ++i) {
         const float one = __shfl(by, (int)i, 16);
         const float *o = p.parts + slot(i0 + i) * p.D;
