@@ -206,7 +206,8 @@ __device__ __forceinline__ KeyRange key_range(const AttendParams &p, const Reque
 // tiles, one tile after the other, make a line of W blocks, and workgroup i of
 // the head takes an equal share of it: blocks i c .. (i + 1) c - 1, whatever
 // tiles they belong to.  So all workgroups run equally long, however ragged the
-// lengths, and a tile is cut only where a share ends in it.  A tile of up to
+// lengths (but for tiles of a few blocks, which cost more than their blocks),
+// and a tile is cut only where a share ends in it.  A tile of up to
 // `whole` blocks is not cut but goes to the share it begins in: parts of so few
 // blocks would cost more than they save.  What a workgroup computes of a cut
 // tile is a part: its sums go to the workspace, where it has two slots (a share
@@ -376,7 +377,9 @@ __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item)
   return true;
 }
 
-// The tile after w's on the line, if the line goes on.
+// The tile after w's on the line, if the line goes on.  Requests of the other form between two are
+// passed one at a time, each a wait for its lengths: 4 prompts of 200 tokens spread among 2000
+// single tokens take 803 us together, in front of them 683.
 __device__ __forceinline__ bool next_item(const AttendParams &p, WorkItem &w, uint64_t begin) {
   w.begin = begin;
   if (++w.tile < w.tiles) return true;

@@ -21,11 +21,13 @@
 // before that rounding.
 //
 // Measured, 64 requests of up to 16384 tokens, 8 key heads: 5.8 TB/s of keys
-// and values at D = 128 (450 us), 5.5 at 64, 5.9 at 256; from 8-bit pages 5.4
+// and values at D = 128 (449 us), 5.6 at 64, 5.9 at 256; from 8-bit pages 5.4
 // at 128 and 4.1 at 64, where a row is 64 bytes.
-// A copy on the same card moves 4.8 TB/s.  One request: 12 us for 64 tokens,
-// 15 for 1000, 42 for 32000, of which the first 12 are the wait for lengths,
-// table, keys and the joining kernel, one after the other.
+// A copy on the same card moves 4.8 TB/s.  One request: 10 us for 64 tokens,
+// 16 for 1000, 42 for 32000 (59 with two key heads, whose 125 parts the join
+// adds up one after the other), of which the first 10 are the wait for
+// lengths, table and keys, one after the other, and of the longer ones 3 to 5
+// the joining kernel.
 #pragma once
 
 #include <type_traits>

@@ -27,10 +27,14 @@
 // that the matrix units take; the sum adds them before that rounding.
 //
 // Measured, 4096 new tokens after 12288, two heads of queries to each of 8:
-// 660 TF at D = 64, 721 at 96, 894 at 128, 483 at 192, 647 at 256 (heads past
-// 128 are computed as 256 elements); from 8-bit pages 889 at 128 and 473 at
-// 256, where registers are spilled; with a cap, an exponential and a
-// reciprocal more a score, 744 at 128.  A large matrix product reaches 1210.
+// 689 TF at D = 64, 723 at 96, 913 at 128, 485 at 192, 648 at 256 (heads past
+// 128 are computed as 256 elements); from 8-bit pages 671, 747, 900, 359 and
+// 479; with a cap, an exponential and a reciprocal more a score, 752 at 128,
+// with one past 64 550.  A large matrix product reaches 1210.
+// Vector registers are spilled at D <= 64 from 8-bit pages (10 to 13 of them)
+// and under caps (9 to 33), at D <= 128 from 8-bit pages under caps (14, 15)
+// and under caps past 64 (2), at 96 under these (1), and past 128 (5 to 14, from
+// 8-bit pages 54 to 62).
 // Counters at D = 128: the matrix units work 43% of the time, and a SIMD
 // issues 72% of it, 6.7 vector instructions beside each matrix instruction.
 #pragma once
