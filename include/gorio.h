@@ -398,27 +398,38 @@ void gorio_free_index(gorio_index *ix);
  * that there is no kernel for), GORIO_EDEVICE.
  * ------------------------------------------------------------------------- */
 
-typedef enum { GORIO_KV_BF16 = 0, GORIO_KV_F16 = 1, GORIO_KV_E4M3 = 2 } gorio_kv_dtype;
+typedef enum { GORIO_KV_BF16 = 0, GORIO_KV_F16 = 1, GORIO_KV_E4M3 = 2, GORIO_KV_MX8 = 4, GORIO_KV_MX4 = 5 } gorio_kv_dtype;
+
+/* GORIO_KV_MX8 and GORIO_KV_MX4 are the microscaling formats of the Open Compute
+ * Project with e4m3 and e2m1 elements: elements 32 i .. 32 i + 31 of a row share
+ * a power of two, 2^E, kept as the byte E + 127.  An element stands for its
+ * value times 2^E; where the byte is 255, the elements stand for NaN.  e2m1 has
+ * the values 0, 0.5, 1, 1.5, 2, 3, 4 and 6 (codes 0..7) and their negatives
+ * (8..15), two a byte, the element with the even index in the low half. */
 
 /* The pages of one layer.  Element d of head h's key at place i of page p is
  * keys[p * page_stride + h * head_stride + i * token_stride + d]; values alike. */
 typedef struct {
     uint32_t dtype;         /* gorio_kv_dtype of keys and values */
     uint32_t heads;         /* key and value heads, 1..1024 */
-    uint32_t D;             /* elements of a head: a multiple of 8, 8..256 */
+    uint32_t D;             /* elements of a head: a multiple of 8, 8..256; of 32 with GORIO_KV_MX8, _MX4 */
     uint32_t page_tokens;   /* 1..65536 */
     uint64_t num_pages;     /* 1..2^31 - 1 */
     void *keys, *values;    /* 16-byte aligned */
-    uint64_t page_stride, head_stride, token_stride;  /* elements, multiples of 8; all three
-                               0 = packed pages, [page][head][token][D] */
+    uint64_t page_stride, head_stride, token_stride;  /* elements, multiples of 8 (of 32 with
+                               GORIO_KV_MX8, _MX4); all three 0 = packed pages, [page][head][token][D] */
     const float *key_scale, *value_scale;  /* GORIO_KV_E4M3: `heads` factors each; an element
                                stands for its 8-bit value times its head's factor.  NULL = 1 */
+    uint8_t *key_powers, *value_powers;  /* GORIO_KV_MX8, _MX4: the powers' bytes, at the 32nd part
+                               of their elements' offset: block i of the key above is
+                               key_powers[(p * page_stride + h * head_stride + place * token_stride) / 32 + i].
+                               Not read with other types */
 } gorio_kv_cache;
 
 /* One call's new tokens, and what they see. */
 typedef struct {
     uint32_t dtype;         /* gorio_kv_dtype of q and out: GORIO_KV_BF16 or GORIO_KV_F16, and that
-                               of the pages unless they are GORIO_KV_E4M3 */
+                               of the pages unless these hold 8 or 4 bits */
     uint32_t heads;         /* query heads, a multiple of the cache's; head h reads head
                                h / (heads / cache heads) */
     uint32_t requests, width;  /* rows and columns of tables */
@@ -492,12 +503,55 @@ gorio_status gorio_kv_plan(const int32_t *before, const int32_t *added, uint64_t
  * aligned), values alike.  A slot outside the pages stores nothing; slots of
  * one call are distinct.  Into GORIO_KV_E4M3 pages an element is divided by its
  * head's factor, clamped to +-448 and rounded to the nearest (ties to even).
+ * Into GORIO_KV_MX8 (MX4) pages: with a the largest size among a block's 32
+ * elements, E is the smallest number in -127..127 with a <= 448 * 2^E (6 * 2^E),
+ * so that no element is clamped, and each is divided by 2^E and rounded to the
+ * nearest (ties to even).  A block that holds a NaN or an infinity gets the byte
+ * 255 and elements of 0: all of it stands for NaN.
  *   dtype: of keys and values: the pages' type, or either 16-bit type for
- *          GORIO_KV_E4M3 pages.
+ *          pages of 8 or 4 bits.
  */
 gorio_status gorio_kv_store(const gorio_kv_cache *cache, gorio_kv_dtype dtype, const void *keys,
                             const void *values, uint64_t tokens, uint64_t key_stride,
                             uint64_t value_stride, const int64_t *slots, void *stream);
+
+/*
+ * Rows of the pages at `tokens` slots -> keys and values, laid out as those of
+ * gorio_kv_store (for other pages, for checks, for keys that are turned to
+ * other positions).  An element is what it stands for, rounded to the nearest
+ * of the rows' type (past its range to an infinity); a slot outside the pages
+ * gives a row of zeros, and a slot may be named more than once.
+ *   dtype: of keys and values: the pages' type, or either 16-bit type for
+ *          pages of 8 or 4 bits.
+ * Neither array shares memory with the other or with the cache.
+ */
+gorio_status gorio_kv_load(const gorio_kv_cache *cache, gorio_kv_dtype dtype, const int64_t *slots,
+                           uint64_t tokens, void *keys, void *values, uint64_t key_stride,
+                           uint64_t value_stride, void *stream);
+
+/*
+ * Which requests of a batch have their first pages in common (a prompt, or
+ * passages, that they were all given), for gorio_kv_attend_shared.  Requests
+ * b - 1 and b share common[b] positions: page_tokens times the number of leading
+ * entries in which their rows of the table, and of fills, are equal, but no
+ * more than the whole pages of held[b - 1] and of held[b].  Request b joins the
+ * group of the request before it if common[b] >= max(least, 1); the others
+ * begin a group each.  Order the requests so that those with the same pages
+ * follow one another.
+ *   tables:   requests x width; fills (or NULL) alike.
+ *   held:     requests: positions that all of a request's new tokens see, as far
+ *             as a window lets them: its tokens before the step, or its prefix.
+ *   least:    fewer positions than this are not worth a group's own work.
+ *   common:   requests out; common[0] = 0.
+ *   first:    requests + 1 out: group g is requests first[g]..first[g+1]; entries
+ *             past the last group hold `requests`, which makes empty groups.
+ *   shared:   requests out: what a request shares with all of its group, the
+ *             smallest of their common (0 for a request alone).
+ * requests is at most 2^20.  No array that is written overlaps another.
+ */
+gorio_status gorio_kv_share(const int32_t *tables, const int32_t *fills, const int32_t *held,
+                            uint64_t requests, uint32_t width, uint32_t page_tokens, uint32_t least,
+                            int32_t *common, int32_t *first, int32_t *shared, void *stream);
 
 /*
  * Attention of new tokens over pages.  New token i of request b stands at
@@ -512,7 +566,8 @@ gorio_status gorio_kv_store(const gorio_kv_cache *cache, gorio_kv_dtype dtype, c
  * Sums and the softmax are held in 32 bits, its weights rounded to q's type
  * for the product with the values.  A row that sees no key (or whose scores
  * are all -inf) gives zeros and an lse of -inf.  Keys and values that a row
- * does not see do not reach it, whatever they hold.  Rows of q past starts[requests] are left
+ * does not see do not reach it, whatever they hold.  Elements of GORIO_KV_MX8 and _MX4 pages are
+ * read as the nearest values of q's type.  Rows of q past starts[requests] are left
  * as they are in out.  starts is clamped to [0, tokens] and has to ascend.
  *   workspace: gorio_kv_workspace bytes of device memory, 16-byte aligned, for
  *              this call alone until it has run (NULL if 0).  Rows of few new

@@ -4,6 +4,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cstddef>
+#include <cstring>
 #include <initializer_list>
 
 #include "../../include/gorio.h"
@@ -87,10 +89,19 @@ inline gorio_status kv_launched(const char *what) {
 
 constexpr uint64_t kKvMost = 0x7FFFFFFFull;  // tokens, pages, requests: below 2^31
 
+// Elements of a block with a power of two of its own.
+constexpr uint32_t kMxBlock = 32;
+inline bool kv_is_mx(uint32_t dtype) { return dtype == GORIO_KV_MX8 || dtype == GORIO_KV_MX4; }
+// Bytes of so many elements.
+inline uint64_t kv_bytes(uint32_t dtype, uint64_t elements) {
+  return dtype == GORIO_KV_MX4 ? elements / 2 : dtype == GORIO_KV_MX8 || dtype == GORIO_KV_E4M3 ? elements : elements * 2;
+}
+
 // The cache's sizes and strides, the strides filled in.
 inline gorio_status kv_check_cache(const gorio_kv_cache *c, gorio_kv_cache *out) {
   if (!c) return fail(GORIO_EINVAL, "cache is NULL");
-  if (c->dtype > GORIO_KV_E4M3) return fail(GORIO_EINVAL, "cache dtype %u is no gorio_kv_dtype", c->dtype);
+  if (c->dtype > GORIO_KV_E4M3 && !kv_is_mx(c->dtype))
+    return fail(GORIO_EINVAL, "cache dtype %u is no gorio_kv_dtype", c->dtype);
   if (c->heads == 0 || c->heads > 1024) return fail(GORIO_EINVAL, "cache heads=%u, need 1..1024", c->heads);
   if (c->D == 0 || c->D % 8 != 0 || c->D > 256)
     return fail(GORIO_EINVAL, "D=%u, need a multiple of 8 in 8..256", c->D);
@@ -98,14 +109,18 @@ inline gorio_status kv_check_cache(const gorio_kv_cache *c, gorio_kv_cache *out)
     return fail(GORIO_EINVAL, "page_tokens=%u, need 1..65536", c->page_tokens);
   if (c->num_pages == 0 || c->num_pages > kKvMost)
     return fail(GORIO_EINVAL, "num_pages=%llu, need 1..2^31-1", (unsigned long long)c->num_pages);
-  *out = *c;
+  const uint32_t whole = kv_is_mx(c->dtype) ? kMxBlock : 8;  // elements
+  if (c->D % whole != 0) return fail(GORIO_EINVAL, "D=%u, need a multiple of %u for these pages", c->D, whole);
+  // a caller that knows no powers may have a shorter struct
+  memcpy(out, c, kv_is_mx(c->dtype) ? sizeof *c : offsetof(gorio_kv_cache, key_powers));
+  if (!kv_is_mx(c->dtype)) out->key_powers = out->value_powers = nullptr;
   if (c->page_stride == 0 && c->head_stride == 0 && c->token_stride == 0) {
     out->token_stride = c->D;
     out->head_stride = (uint64_t)c->D * c->page_tokens;
     out->page_stride = out->head_stride * c->heads;
   }
-  if (out->page_stride % 8 || out->head_stride % 8 || out->token_stride % 8)
-    return fail(GORIO_EINVAL, "the cache's strides must be multiples of 8 elements");
+  if (out->page_stride % whole || out->head_stride % whole || out->token_stride % whole)
+    return fail(GORIO_EINVAL, "the cache's strides must be multiples of %u elements", whole);
   if (c->dtype != GORIO_KV_E4M3 && (c->key_scale || c->value_scale))
     return fail(GORIO_EINVAL, "key_scale and value_scale belong to GORIO_KV_E4M3 pages");
   return GORIO_OK;

@@ -14,7 +14,7 @@ gorio_status check(const gorio_kv_cache *cache, const gorio_kv_attention *a, gor
   if (!a) return fail(GORIO_EINVAL, "attention is NULL");
   if (a->dtype != GORIO_KV_BF16 && a->dtype != GORIO_KV_F16)
     return fail(GORIO_EINVAL, "q must be bf16 or f16, not gorio_kv_dtype %u", a->dtype);
-  if (c->dtype != GORIO_KV_E4M3 && c->dtype != a->dtype)
+  if (c->dtype < GORIO_KV_E4M3 && c->dtype != a->dtype)
     return fail(GORIO_EUNSUPPORTED, "16-bit pages are read by queries of their own type");
   if (a->heads == 0 || a->heads % c->heads != 0 || a->heads > 65535)
     return fail(GORIO_EINVAL, "heads=%u, need a multiple of the cache's %u, at most 65535", a->heads, c->heads);
@@ -65,7 +65,7 @@ AttendForm divide(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t
 // The forms that a call needs, and its workspace, which they use in turn.
 AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint64_t *bytes) {
   AttendLaunch l{};
-  l.e4m3 = c.dtype == GORIO_KV_E4M3;
+  l.pages = c.dtype == GORIO_KV_E4M3 ? kPagesE4m3 : c.dtype == GORIO_KV_MX8 ? kPagesMx8 : c.dtype == GORIO_KV_MX4 ? kPagesMx4 : kPages16;
   l.more = a.cap > kQuickCap ? 3 : a.cap > 0.f ? 2 : a.slopes ? 1 : 0;
   const uint64_t group = a.heads / c.heads;
   // The most new tokens of a request, and the fewest of one that has any, as far as the host can
@@ -133,6 +133,8 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
                 {"cache values", c.values, 16, false},
                 {"key_scale", c.key_scale, 4, true},
                 {"value_scale", c.value_scale, 4, true},
+                {"key_powers", c.key_powers, 1, !kv_is_mx(c.dtype)},
+                {"value_powers", c.value_powers, 1, !kv_is_mx(c.dtype)},
                 {"workspace", workspace, 16, workspace_bytes == 0}});
   if (st != GORIO_OK) return st;
   uint64_t bytes = 0;
@@ -140,7 +142,7 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
   if (bytes > workspace_bytes)
     return fail(GORIO_EINVAL, "workspace of %llu bytes, need %llu", (unsigned long long)workspace_bytes,
                 (unsigned long long)bytes);
-  const uint32_t group = at.heads / c.heads, element = c.dtype == GORIO_KV_E4M3 ? 1 : 2;
+  const uint32_t group = at.heads / c.heads;
   AttendParams p;
   p.q = static_cast<const uint16_t *>(at.q);
   p.out = static_cast<uint16_t *>(at.out);
@@ -149,6 +151,8 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
   p.values = static_cast<const uint8_t *>(c.values);
   p.key_scale = c.key_scale;
   p.value_scale = c.value_scale;
+  p.key_powers = c.key_powers;
+  p.value_powers = c.value_powers;
   p.starts = at.starts;
   p.lens = at.lens;
   p.tables = at.tables;
@@ -158,9 +162,9 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
   p.parts = static_cast<float *>(workspace);
   p.q_stride = at.q_stride;
   p.out_stride = at.out_stride;
-  p.page_stride = c.page_stride * element;
-  p.head_stride = c.head_stride * element;
-  p.token_stride = c.token_stride * element;
+  p.page_stride = kv_bytes(c.dtype, c.page_stride);
+  p.head_stride = kv_bytes(c.dtype, c.head_stride);
+  p.token_stride = kv_bytes(c.dtype, c.token_stride);
   p.tokens = (uint32_t)at.tokens;
   p.num_pages = (uint32_t)c.num_pages;
   p.requests = at.requests;
@@ -175,8 +179,10 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
   p.cap = at.cap;
   p.window = at.window ? at.window : (uint32_t)kKvMost;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const bool f16 = at.dtype == GORIO_KV_F16;
-  const hipError_t e = l.e4m3 ? (f16 ? launch_attend_f16_e4m3(p, l, s) : launch_attend_bf16_e4m3(p, l, s))
-                              : (f16 ? launch_attend_f16(p, l, s) : launch_attend_bf16(p, l, s));
+  typedef hipError_t (*Launch)(const AttendParams &, const AttendLaunch &, hipStream_t);
+  static constexpr Launch kLaunch[2][4] = {
+      {launch_attend_bf16, launch_attend_bf16_e4m3, launch_attend_bf16_mx8, launch_attend_bf16_mx4},
+      {launch_attend_f16, launch_attend_f16_e4m3, launch_attend_f16_mx8, launch_attend_f16_mx4}};
+  const hipError_t e = kLaunch[at.dtype == GORIO_KV_F16][l.pages](p, l, s);
   return e == hipSuccess ? GORIO_OK : fail(GORIO_EDEVICE, "gorio_kv_attend: %s", hipGetErrorString(e));
 }

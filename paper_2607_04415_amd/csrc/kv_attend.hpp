@@ -13,6 +13,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "kv.hpp"
 
 namespace gorio {
@@ -41,9 +43,15 @@ struct KvBf16 {
     const bf16x2 v = {(__bf16)x, (__bf16)y};
     return __builtin_bit_cast(uint32_t, v);
   }
+  // Two values of 8 bits, or of 4, times a power of two: the nearest of this type, exactly the
+  // product where it has one.  `by` may be 0 for 2^-127 and inf for NaN: its exponent's bits count.
   template <bool kHi>
-  static __device__ __forceinline__ uint32_t widen(uint32_t w) {  // two 8-bit values, exactly
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, kHi));
+  static __device__ __forceinline__ uint32_t widen(uint32_t w, float by) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, by, kHi));
+  }
+  template <int kByte>
+  static __device__ __forceinline__ uint32_t widen4(uint32_t w, float by) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, by, kByte));
   }
 };
 
@@ -62,21 +70,48 @@ struct KvF16 {
     return __builtin_bit_cast(uint32_t, v);
   }
   template <bool kHi>
-  static __device__ __forceinline__ uint32_t widen(uint32_t w) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, kHi));
+  static __device__ __forceinline__ uint32_t widen(uint32_t w, float by) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, by, kHi));
   }
+  template <int kByte>
+  static __device__ __forceinline__ uint32_t widen4(uint32_t w, float by) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, by, kByte));
+  }
+};
+
+// What pages hold: 16-bit elements, e4m3 by a factor a head, e4m3 and e2m1 by a power of two for
+// each 32 of a row.
+enum PageKind : int { kPages16, kPagesE4m3, kPagesMx8, kPagesMx4 };
+template <int kPages>
+struct PageOf {
+  static constexpr bool kMx = kPages >= kPagesMx8;
+  static constexpr uint32_t bytes(uint32_t elements) {
+    return kPages == kPages16 ? elements * 2 : kPages == kPagesMx4 ? elements / 2 : elements;
+  }
+  // eight elements as they lie
+  typedef typename std::conditional<kPages == kPages16, u32x4,
+                                    typename std::conditional<kPages == kPagesMx4, uint32_t, u32x2>::type>::type Raw;
+  // the offset of a row's powers, from that of its elements
+  static __device__ __forceinline__ uint64_t powers(uint64_t bytes) { return bytes >> (kPages == kPagesMx4 ? 4 : 5); }
 };
 
 // Eight elements as they lie in the pages -> eight of the queries' type.
 template <typename Q>
-__device__ __forceinline__ u32x4 widened(u32x4 r) {
+__device__ __forceinline__ u32x4 widened(u32x4 r, float = 1.f) {
   return r;
 }
 template <typename Q>
-__device__ __forceinline__ u32x4 widened(u32x2 r) {
-  return u32x4{Q::template widen<false>(r.x), Q::template widen<true>(r.x), Q::template widen<false>(r.y),
-               Q::template widen<true>(r.y)};
+__device__ __forceinline__ u32x4 widened(u32x2 r, float by = 1.f) {
+  return u32x4{Q::template widen<false>(r.x, by), Q::template widen<true>(r.x, by), Q::template widen<false>(r.y, by),
+               Q::template widen<true>(r.y, by)};
 }
+template <typename Q>
+__device__ __forceinline__ u32x4 widened(uint32_t r, float by) {
+  return u32x4{Q::template widen4<0>(r, by), Q::template widen4<1>(r, by), Q::template widen4<2>(r, by),
+               Q::template widen4<3>(r, by)};
+}
+// A power's byte as such a factor.
+__device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // LDS by its 32-bit address: what is added to one as a constant goes into the instruction.
 typedef __attribute__((address_space(3))) uint8_t LdsBytes;
@@ -140,6 +175,7 @@ struct AttendParams {
   float *lse;
   const uint8_t *keys, *values;
   const float *key_scale, *value_scale;
+  const uint8_t *key_powers, *value_powers;
   const int32_t *starts, *lens, *tables, *fills, *prefix;
   const float *slopes;
   float *parts;  // workspace

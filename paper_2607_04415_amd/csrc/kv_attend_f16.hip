@@ -4,7 +4,7 @@
 namespace gorio {
 
 hipError_t launch_attend_f16(const AttendParams &p, const AttendLaunch &l, hipStream_t s) {
-  return launch_pages<KvF16, false>(p, l, s);
+  return launch_pages<KvF16, kPages16>(p, l, s);
 }
 
 }  // namespace gorio

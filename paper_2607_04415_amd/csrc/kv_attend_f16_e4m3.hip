@@ -4,7 +4,7 @@
 namespace gorio {
 
 hipError_t launch_attend_f16_e4m3(const AttendParams &p, const AttendLaunch &l, hipStream_t s) {
-  return launch_pages<KvF16, true>(p, l, s);
+  return launch_pages<KvF16, kPagesE4m3>(p, l, s);
 }
 
 }  // namespace gorio

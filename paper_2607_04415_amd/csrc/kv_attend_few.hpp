@@ -30,8 +30,6 @@
 // the joining kernel.
 #pragma once
 
-#include <type_traits>
-
 #include "kv_attend.hpp"
 
 namespace gorio {
@@ -42,16 +40,19 @@ __host__ __device__ constexpr int few_waves(int steps) { return steps > 4 ? 4 : 
 constexpr int kFewRows = 16;
 constexpr int kFewBlock = 32;  // keys
 
-// kSteps: 32-element steps of a head, D <= 32 kSteps.  k8: pages of 8-bit values.
+// kSteps: 32-element steps of a head, D <= 32 kSteps.  kPages: a PageKind.
 // kMore: scores are capped or biased.
-template <typename Q, bool k8, int kSteps, bool kMore>
+template <typename Q, int kPages, int kSteps, bool kMore>
 __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
                                          const KeyRange &range, const Part &part, uint32_t head) {
   constexpr int kFewWaves = few_waves(kSteps), kFewThreads = kFewWaves * 64;
   constexpr int kHalves = (kSteps + 3) / 4;  // 128 elements of a value
   constexpr int kDim = kHalves * 128;
   constexpr int kPad = kDim + 4;
-  typedef typename std::conditional<k8, u32x2, u32x4>::type Raw;  // 8 elements as they lie
+  typedef PageOf<kPages> Page;
+  typedef typename Page::Raw Raw;
+  constexpr bool kMx = Page::kMx;
+  __shared__ uint64_t s_power[kMx ? kFewWaves : 1][2][2][kFewBlock];  // as s_row, the rows' powers
   __shared__ uint64_t s_row[kFewWaves][2][2][kFewBlock];  // wave, turn, keys or values
   __shared__ float s_o[kFewWaves][kFewRows][kPad];
   __shared__ float s_m[kFewWaves][kFewRows], s_l[kFewWaves][kFewRows];
@@ -61,7 +62,6 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
   const uint64_t zeros = (uint64_t)(uintptr_t)kv_zeros;
-  constexpr int kElem = k8 ? 1 : 2;
 
   // this lane's query
   const uint32_t n = min((uint32_t)m, tile.rows - 1);  // rows past the last repeat it
@@ -97,10 +97,15 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
       const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
       s_row[wave][turn][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : 0;
       s_row[wave][turn][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : 0;
+      if constexpr (kMx) {
+        s_power[wave][turn][0][lane] = (uint64_t)(uintptr_t)p.key_powers + Page::powers(off);
+        s_power[wave][turn][1][lane] = (uint64_t)(uintptr_t)p.value_powers + Page::powers(off);
+      }
     }
     wave_lds_order();
     return (uint32_t)__ballot(there);
   };
+  uint8_t kp[2][kMx ? 2 : 1][kMx ? kSteps : 1], vp[2][kMx ? kHalves : 1][kMx ? 8 : 1];  // powers
   auto load_keys = [&](Raw (&k)[2][kSteps], int turn) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -108,8 +113,12 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         const uint32_t d = s * 32 + g * 8;
-        const uint64_t at = row && d < p.D ? row + d * kElem : zeros;
+        const uint64_t at = row && d < p.D ? row + Page::bytes(d) : zeros;
         k[i][s] = *reinterpret_cast<const Raw *>(at);
+        if constexpr (kMx) {
+          const uint64_t power = s_power[wave][turn][0][i * 16 + m] + s;
+          kp[turn][i][s] = *reinterpret_cast<const uint8_t *>(row && d < p.D ? power : zeros);
+        }
       }
     }
   };
@@ -118,8 +127,12 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint64_t row = s_row[wave][turn][1][(i >> 2) * 16 + g * 4 + (i & 3)];
-      const uint64_t at = row && d < p.D ? row + d * kElem : zeros;
+      const uint64_t at = row && d < p.D ? row + Page::bytes(d) : zeros;
       v[i] = *reinterpret_cast<const Raw *>(at);
+      if constexpr (kMx) {
+        const uint64_t power = s_power[wave][turn][1][(i >> 2) * 16 + g * 4 + (i & 3)] + d / kMxBlock;
+        vp[turn][half][i] = *reinterpret_cast<const uint8_t *>(row && d < p.D ? power : zeros);
+      }
     }
   };
   // Block x, with the next one's keys and values on their way; the registers alternate.
@@ -145,7 +158,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     for (int i = 0; i < 2; ++i) {
       s2[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) s2[i] = Q::mfma16(widened<Q>(k[t0][i][s]), q[s], s2[i]);
+      for (int s = 0; s < kSteps; ++s) s2[i] = Q::mfma16(widened<Q>(k[t0][i][s], power_of(kMx ? kp[t0][kMx ? i : 0][kMx ? s : 0] : 127)), q[s], s2[i]);
     }
     float e[8];
 #pragma unroll
@@ -193,7 +206,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     for (int h = 0; h < kHalves; ++h) {
       u32x4 vw[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) vw[i] = widened<Q>(v[t0][h][i]);
+      for (int i = 0; i < 8; ++i) vw[i] = widened<Q>(v[t0][h][i], power_of(kMx ? vp[t0][kMx ? h : 0][kMx ? i : 0] : 127));
       // A weight of 0 keeps a value out of a row, unless the value is NaN or inf.  Such
       // values in a block that some rows see only in part go in apart from the others.
       bool odd = false;
@@ -300,7 +313,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   }
 }
 
-template <typename Q, bool k8, int kSteps, bool kMore>
+template <typename Q, int kPages, int kSteps, bool kMore>
 __global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
@@ -310,7 +323,7 @@ __global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParam
     const KeyRange range = key_range<kFewBlock>(p, w.r, tile.first, tile.last);
     const uint32_t blocks = (uint32_t)max(range.count, 1);
     const Part part = part_of(p, w, blocks, index);
-    if (!part.none) few_part<Q, k8, kSteps, kMore>(p, w, tile, range, part, head);
+    if (!part.none) few_part<Q, kPages, kSteps, kMore>(p, w, tile, range, part, head);
     const uint64_t end = w.begin + blocks;
     if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end))
       return note_cut<kFewRows>(p, index, head, w, tile, part, blocks);

@@ -39,8 +39,6 @@
 // issues 72% of it, 6.7 vector instructions beside each matrix instruction.
 #pragma once
 
-#include <type_traits>
-
 #include "kv_attend.hpp"
 
 namespace gorio {
@@ -58,26 +56,29 @@ constexpr int kManyBlock = 64;  // keys
 // f16's range, and a sum of them loses nothing): most blocks then rescale nothing.
 constexpr float kSlack = 8.f;
 
-// kSteps: D <= 32 kSteps.  k8: pages of 8-bit values.  kMore: 1 if scores are biased, 2 if they
+// kSteps: D <= 32 kSteps.  kPages: a PageKind.  kMore: 1 if scores are biased, 2 if they
 // are capped, and biased if there are slopes, 3 the same by a cap past kQuickCap (kernels of their
-// own: a branch in those of 2 made these spill up to 40 registers more, for caps of any size).
-template <typename Q, bool k8, int kSteps, int kMore>
+// own: a branch in those of 2 made these spill up to 40 registers more, for caps of any size).  Pages
+// of blocks with powers have no kernels of 1: those of 3 serve biases without a cap as well.
+template <typename Q, int kPages, int kSteps, int kMore>
 __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
                                           const KeyRange &range, const Part &part, uint32_t head) {
   constexpr int kManyWaves = many_waves(kSteps), kManyThreads = kManyWaves * 64, kManyRows = kManyWaves * 32;
   constexpr int kDim = kSteps * 32, kChunks = kDim / 8;                              // 16-byte pieces of a row
   constexpr int kPasses = kManyBlock * kChunks / kManyThreads;                       // pieces a thread
   static_assert(kPasses * kManyThreads == kManyBlock * kChunks, "pieces divide");
-  constexpr bool kTurned = (kChunks & (kChunks - 1)) == 0, kDirect = kTurned && !k8;  // see `turned`
+  constexpr bool kTurned = (kChunks & (kChunks - 1)) == 0, kDirect = kTurned && kPages == kPages16;  // see `turned`
   constexpr int kKeyRow = kTurned ? kDim : kDim + 8;                                 // elements
   constexpr int kValueRow = kDim;
   static_assert(kTurned || (kDim * 2) % 256 == 192, "rows of values fall on different banks");
-  constexpr int kElem = k8 ? 1 : 2;
-  typedef typename std::conditional<k8, u32x2, u32x4>::type Raw;
+  typedef PageOf<kPages> Page;
+  typedef typename Page::Raw Raw;
+  constexpr bool kMx = Page::kMx;
   constexpr uint32_t kKeyBytes = kManyBlock * kKeyRow * 2, kValueBytes = kManyBlock * kValueRow * 2;
   __shared__ __align__(1024) uint8_t s_kv[2 * (kKeyBytes + kValueBytes)];  // keys, keys, values, values
   constexpr int kRing = kManyWaves * 2;                 // blocks
   __shared__ uint64_t s_row[kRing][2][kManyBlock];      // block, keys or values
+  __shared__ uint64_t s_power[kMx ? kRing : 1][2][kManyBlock];  // as s_row, the rows' powers
   __shared__ uint64_t s_there[kRing];
   // Values that are NaN or inf in a block that not all rows see: a weight of 0 would not keep
   // them out of a row.  They are 0 in s_kv; here are the keys that have one at an element,
@@ -131,6 +132,10 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
     const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
     s_row[x & (kRing - 1)][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : zeros;
     s_row[x & (kRing - 1)][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : zeros;
+    if constexpr (kMx) {
+      s_power[x & (kRing - 1)][0][lane] = there ? (uint64_t)(uintptr_t)p.key_powers + Page::powers(off) : zeros;
+      s_power[x & (kRing - 1)][1][lane] = there ? (uint64_t)(uintptr_t)p.value_powers + Page::powers(off) : zeros;
+    }
     const uint64_t bits = __ballot(there);
     if (lane == 0) s_there[x & (kRing - 1)] = bits;
   };
@@ -148,6 +153,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
     return kChunks == 8 ? (key >> 1 & 1u) << 2 | (key >> 2 & 3u) : (key & 3u) << 2 | (key >> 2 & 3u);
   };
   Raw stage[2][kDirect ? 1 : kPasses];
+  uint8_t powers[2][kMx ? kPasses : 1];
   const uint32_t lds = (uint32_t)(uintptr_t)(LdsBytes *)s_kv;
   constexpr uint32_t kKeys[2] = {0, kKeyBytes}, kValues[2] = {2 * kKeyBytes, 2 * kKeyBytes + kValueBytes};
   // The values of block x and the keys half a block later: 32.. of block x, ..31 of x + 1.
@@ -155,11 +161,20 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
     const uint32_t key = ((i * kManyWaves + wave) * 64 + lane) / kChunks;
     return kv ? s_row[x & (kRing - 1)][1][key] : s_row[(x + (key >> 5)) & (kRing - 1)][0][key ^ 32];
   };
+  auto powers_of = [&](int32_t x, int kv, int i) __attribute__((always_inline)) -> uint64_t {
+    if constexpr (!kMx) return 0;
+    const uint32_t key = ((i * kManyWaves + wave) * 64 + lane) / kChunks;
+    return kv ? s_power[x & (kRing - 1)][1][key] : s_power[(x + (key >> 5)) & (kRing - 1)][0][key ^ 32];
+  };
   const bool whole_rows = p.D == kDim;
-  auto load_row = [&](uint64_t row, int kv, int i, uint32_t to, bool whole) __attribute__((always_inline)) {
+  auto load_row = [&](uint64_t row, uint64_t power, int kv, int i, uint32_t to, bool whole) __attribute__((always_inline)) {
     const uint32_t piece = (i * kManyWaves + wave) * 64 + lane, c = piece % kChunks;
     const uint32_t d = (kDirect ? c ^ turned(piece / kChunks) : c) * 8;
-    const uint64_t at = whole || d < p.D ? row + d * kElem : zeros;
+    const uint64_t at = whole || d < p.D ? row + Page::bytes(d) : zeros;
+    if constexpr (kMx) {
+      const uint64_t one = whole || d < p.D ? power + d / kMxBlock : zeros;
+      powers[kv][i] = *reinterpret_cast<const uint8_t *>(one);
+    }
     if constexpr (kDirect) {
       typedef __attribute__((address_space(1))) const uint32_t global_u32;
       __builtin_amdgcn_global_load_lds((global_u32 *)at, (LdsBytes *)(uintptr_t)(lds + to + (i * kManyWaves + wave) * 1024),
@@ -169,16 +184,16 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
     }
   };
   auto load = [&](int32_t x, int kv, uint32_t to) __attribute__((always_inline)) {
-    uint64_t row[kPasses];
+    uint64_t row[kPasses], power[kPasses];
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) row[i] = row_of(x, kv, i);
+    for (int i = 0; i < kPasses; ++i) row[i] = row_of(x, kv, i), power[i] = powers_of(x, kv, i);
     __builtin_amdgcn_sched_barrier(0);  // all rows are read before the first is waited for
     if (whole_rows) {
 #pragma unroll
-      for (int i = 0; i < kPasses; ++i) load_row(row[i], kv, i, to, true);
+      for (int i = 0; i < kPasses; ++i) load_row(row[i], power[i], kv, i, to, true);
     } else {
 #pragma unroll
-      for (int i = 0; i < kPasses; ++i) load_row(row[i], kv, i, to, false);
+      for (int i = 0; i < kPasses; ++i) load_row(row[i], power[i], kv, i, to, false);
     }
   };
   auto put = [&](int kv, uint32_t to) __attribute__((always_inline)) {
@@ -186,7 +201,8 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
 #pragma unroll
       for (int i = 0; i < kPasses; ++i) {
         const uint32_t piece = (i * kManyWaves + wave) * 64 + lane, key = piece / kChunks, c = piece % kChunks;
-        *lds_at<u32x4>(lds + to + key * (kv ? kValueRow : kKeyRow) * 2 + (kTurned ? c ^ turned(key) : c) * 16) = widened<Q>(stage[kv][i]);
+        *lds_at<u32x4>(lds + to + key * (kv ? kValueRow : kKeyRow) * 2 + (kTurned ? c ^ turned(key) : c) * 16) =
+            widened<Q>(stage[kv][i], power_of(kMx ? powers[kv][kMx ? i : 0] : 127));
       }
     }
   };
@@ -263,7 +279,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         if constexpr (large) {
-          s[i] = change.capped_exactly(s[i]);
+          s[i] = kMx && p.cap == 0.f ? s[i] * change.to_log2 : change.capped_exactly(s[i]);
           __builtin_amdgcn_sched_barrier(0);  // one score's registers at a time
         } else {
           s[i] = change.quotient(s[i]);
@@ -499,7 +515,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
 
 // Workgroups a CU: three for D <= 64, in 168 registers (8 requests of 1000 tokens over 8000: 127
 // us; two workgroups, with room for more registers, 137), two for 96.
-template <typename Q, bool k8, int kSteps, int kMore>
+template <typename Q, int kPages, int kSteps, int kMore>
 __global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps > 2 ? 2 : 3) void attend_many(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
@@ -509,7 +525,7 @@ __global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps >
     const KeyRange range = key_range<kManyBlock>(p, w.r, tile.first, tile.last);
     const uint32_t blocks = (uint32_t)max(range.count, 1);
     const Part part = part_of(p, w, blocks, index);
-    if (!part.none) many_part<Q, k8, kSteps, kMore>(p, w, tile, range, part, head);
+    if (!part.none) many_part<Q, kPages, kSteps, kMore>(p, w, tile, range, part, head);
     const uint64_t end = w.begin + blocks;
     if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end))
       return note_cut<many_rows(kSteps)>(p, index, head, w, tile, part, blocks);

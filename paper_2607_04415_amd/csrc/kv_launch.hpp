@@ -14,12 +14,12 @@ struct AttendForm {
 };
 
 struct AttendLaunch {
-  bool e4m3;  // 8-bit pages
+  int pages;  // a PageKind
   int more;   // 1 if scores are biased, 2 if they are capped, 3 if by a cap past kQuickCap
   AttendForm few, many;
 };
 
-template <typename Q, bool k8, int kSteps, int kMore>
+template <typename Q, int kPages, int kSteps, int kMore>
 hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
   auto divide = [&](const AttendForm &f) {
     p.rows = f.rows;
@@ -32,44 +32,49 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
   };
   if (l.few.shares) {
     divide(l.few);
-    attend_few<Q, k8, kSteps, (kMore > 0)><<<l.few.shares * p.kv_heads, few_waves(kSteps) * 64, 0, s>>>(p);
+    attend_few<Q, kPages, kSteps, (kMore > 0)><<<l.few.shares * p.kv_heads, few_waves(kSteps) * 64, 0, s>>>(p);
     if (l.few.cuts) attend_join<Q, kFewRows><<<(l.few.shares - 1) * p.kv_heads, 256, 0, s>>>(p);
   }
   if (l.many.shares) {
     divide(l.many);
-    attend_many<Q, k8, kSteps, kMore><<<l.many.shares * p.kv_heads, many_waves(kSteps) * 64, 0, s>>>(p);
+    attend_many<Q, kPages, kSteps, kMore><<<l.many.shares * p.kv_heads, many_waves(kSteps) * 64, 0, s>>>(p);
     if (l.many.cuts)
       attend_join<Q, many_rows(kSteps)><<<dim3((l.many.shares - 1) * p.kv_heads, many_rows(kSteps) / 16), 256, 0, s>>>(p);
   }
   return hipGetLastError();
 }
 
-template <typename Q, bool k8, int kSteps>
+template <typename Q, int kPages, int kSteps>
 hipError_t launch_steps(const AttendParams &p, const AttendLaunch &l, hipStream_t s) {
+  if constexpr (!PageOf<kPages>::kMx)
+    if (l.more == 1) return launch_forms<Q, kPages, kSteps, 1>(p, l, s);
   switch (l.more) {
-    case 0: return launch_forms<Q, k8, kSteps, 0>(p, l, s);
-    case 1: return launch_forms<Q, k8, kSteps, 1>(p, l, s);
-    case 2: return launch_forms<Q, k8, kSteps, 2>(p, l, s);
-    default: return launch_forms<Q, k8, kSteps, 3>(p, l, s);
+    case 0: return launch_forms<Q, kPages, kSteps, 0>(p, l, s);
+    case 2: return launch_forms<Q, kPages, kSteps, 2>(p, l, s);
+    default: return launch_forms<Q, kPages, kSteps, 3>(p, l, s);
   }
 }
 
 // 32-element steps of the kernels for a head of D elements.
 inline int steps_of(uint32_t D) { return D <= 64 ? 2 : D <= 96 ? 3 : D <= 128 ? 4 : 8; }
 
-template <typename Q, bool k8>
+template <typename Q, int kPages>
 hipError_t launch_pages(const AttendParams &p, const AttendLaunch &l, hipStream_t s) {
   switch (steps_of(p.D)) {
-    case 2: return launch_steps<Q, k8, 2>(p, l, s);
-    case 3: return launch_steps<Q, k8, 3>(p, l, s);
-    case 4: return launch_steps<Q, k8, 4>(p, l, s);
-    default: return launch_steps<Q, k8, 8>(p, l, s);
+    case 2: return launch_steps<Q, kPages, 2>(p, l, s);
+    case 3: return launch_steps<Q, kPages, 3>(p, l, s);
+    case 4: return launch_steps<Q, kPages, 4>(p, l, s);
+    default: return launch_steps<Q, kPages, 8>(p, l, s);
   }
 }
 
 hipError_t launch_attend_bf16(const AttendParams &p, const AttendLaunch &l, hipStream_t s);
 hipError_t launch_attend_bf16_e4m3(const AttendParams &p, const AttendLaunch &l, hipStream_t s);
+hipError_t launch_attend_bf16_mx8(const AttendParams &p, const AttendLaunch &l, hipStream_t s);
+hipError_t launch_attend_bf16_mx4(const AttendParams &p, const AttendLaunch &l, hipStream_t s);
 hipError_t launch_attend_f16(const AttendParams &p, const AttendLaunch &l, hipStream_t s);
 hipError_t launch_attend_f16_e4m3(const AttendParams &p, const AttendLaunch &l, hipStream_t s);
+hipError_t launch_attend_f16_mx8(const AttendParams &p, const AttendLaunch &l, hipStream_t s);
+hipError_t launch_attend_f16_mx4(const AttendParams &p, const AttendLaunch &l, hipStream_t s);
 
 }  // namespace gorio

@@ -11,6 +11,8 @@
 // the quotient in 32 bits.
 #include "kv.hpp"
 
+#include "kv_mx.hpp"
+
 using namespace gorio;
 
 namespace {
@@ -19,6 +21,7 @@ struct StoreParams {
   const uint16_t *keys, *values;  // 16-bit elements, bf16 or f16
   uint8_t *to_keys, *to_values;
   const float *key_scale, *value_scale;
+  uint8_t *key_powers, *value_powers;
   const int64_t *slots;
   uint64_t key_stride, value_stride;  // elements
   uint64_t page_stride, head_stride, token_stride;
@@ -27,10 +30,6 @@ struct StoreParams {
   FastDiv per_row, per_token;  // parts of a head's row, and of a token
   FastDiv page_tokens;
 };
-
-__device__ __forceinline__ float to_float(uint16_t bits, bool f16) {
-  return f16 ? (float)__builtin_bit_cast(_Float16, bits) : __uint_as_float((uint32_t)bits << 16);
-}
 
 // +-448 is the largest value of the 8-bit type; a NaN stays one.
 __device__ __forceinline__ float clamp_e4m3(float x) { return x > 448.f ? 448.f : x < -448.f ? -448.f : x; }
@@ -57,7 +56,8 @@ struct Divisor {
 
 constexpr uint32_t kParts = 1024;
 
-// Eight elements as they are (kTo 0), or bf16 (1) or f16 (2) to e4m3.
+// Eight elements as they are (kTo 0), or bf16 (1) or f16 (2) to e4m3; 3 to 6: bf16 and f16 to
+// e4m3 and to e2m1 by blocks.
 template <int kTo>
 __device__ __forceinline__ void put(uint8_t *pages, uint64_t to, const uint4 &x, bool scaled, float scale) {
   if constexpr (kTo == 0) {
@@ -87,6 +87,33 @@ __device__ __forceinline__ void put(uint8_t *pages, uint64_t to, const uint4 &x,
   }
 }
 
+// Eight elements of a block of 32, whose other parts the quad's other lanes hold, to `to` elements
+// from the pages' start on; `to` is of the block's first lane in the block's own.
+template <bool kF16, bool k4>
+__device__ __forceinline__ void put_mx(uint8_t *pages, uint8_t *powers, uint64_t to, const uint4 &x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t most = 0;  // sizes' bits, NaN and inf above all others
+#pragma unroll
+  for (int i = 0; i < 4; ++i) most = max(max(most, w[i] & 0x7FFFu), w[i] >> 16 & 0x7FFFu);
+  most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xB1, 0xF, 0xF, true));  // lanes 1, 0, 3, 2
+  most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x4E, 0xF, 0xF, true));  // lanes 2, 3, 0, 1
+  const uint32_t power = mx_power<k4>(to_float((uint16_t)most, kF16));
+  const float by = mx_inverse(power);
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = to_float((uint16_t)(w[i / 2] >> (16 * (i & 1))), kF16) * by;
+  if (power == 255) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = 0.f;
+  }
+  if constexpr (k4) {
+    *reinterpret_cast<uint32_t *>(pages + to / 2) = to_e2m1(f);
+  } else {
+    *reinterpret_cast<uint2 *>(pages + to) = to_e4m3(f);
+  }
+  if (to % kMxBlock == 0) powers[to / kMxBlock] = (uint8_t)power;
+}
+
 template <int kTo>
 __global__ __launch_bounds__(256) void store_kernel(StoreParams p) {
   const uint64_t part0 = (uint64_t)blockIdx.x * kParts, token0 = part0 / p.per_token.d;
@@ -104,13 +131,19 @@ __global__ __launch_bounds__(256) void store_kernel(StoreParams p) {
     if (page >= p.num_pages) continue;
     const uint32_t place = (uint32_t)((uint64_t)slot - page * p.page_tokens.d);
     const uint32_t from = head * p.per_row.d * 8 + d;
-    const float by_key = kTo && p.key_scale ? p.key_scale[head] : 1.f;
-    const float by_value = kTo && p.value_scale ? p.value_scale[head] : 1.f;
+    const float by_key = kTo && kTo < 3 && p.key_scale ? p.key_scale[head] : 1.f;
+    const float by_value = kTo && kTo < 3 && p.value_scale ? p.value_scale[head] : 1.f;
     const uint4 k = *reinterpret_cast<const uint4 *>(p.keys + token * p.key_stride + from);
     const uint4 v = *reinterpret_cast<const uint4 *>(p.values + token * p.value_stride + from);
     const uint64_t to = page * p.page_stride + head * p.head_stride + place * p.token_stride + d;
-    put<kTo>(p.to_keys, to, k, p.key_scale, by_key);
-    put<kTo>(p.to_values, to, v, p.value_scale, by_value);
+    if constexpr (kTo >= 3) {
+      // the lanes of a block are in here together: its token's slot, and the end, are theirs alike
+      put_mx<(kTo & 1) == 0, (kTo > 4)>(p.to_keys, p.key_powers, to, k);
+      put_mx<(kTo & 1) == 0, (kTo > 4)>(p.to_values, p.value_powers, to, v);
+    } else {
+      put<kTo>(p.to_keys, to, k, p.key_scale, by_key);
+      put<kTo>(p.to_values, to, v, p.value_scale, by_value);
+    }
   }
 }
 
@@ -124,7 +157,7 @@ extern "C" gorio_status gorio_kv_store(const gorio_kv_cache *cache, gorio_kv_dty
   if (st != GORIO_OK) return st;
   if (dtype != GORIO_KV_BF16 && dtype != GORIO_KV_F16)
     return fail(GORIO_EINVAL, "keys and values must be bf16 or f16, not gorio_kv_dtype %d", (int)dtype);
-  if (c.dtype != GORIO_KV_E4M3 && (gorio_kv_dtype)c.dtype != dtype)
+  if (c.dtype < GORIO_KV_E4M3 && (gorio_kv_dtype)c.dtype != dtype)
     return fail(GORIO_EUNSUPPORTED, "16-bit pages take keys and values of their own type");
   if (tokens > kKvMost) return fail(GORIO_EINVAL, "tokens=%llu too large", (unsigned long long)tokens);
   if (key_stride == 0) key_stride = (uint64_t)c.heads * c.D;
@@ -139,7 +172,9 @@ extern "C" gorio_status gorio_kv_store(const gorio_kv_cache *cache, gorio_kv_dty
                 {"cache keys", c.keys, 16, false},
                 {"cache values", c.values, 16, false},
                 {"key_scale", c.key_scale, 4, true},
-                {"value_scale", c.value_scale, 4, true}});
+                {"value_scale", c.value_scale, 4, true},
+                {"key_powers", c.key_powers, 1, !kv_is_mx(c.dtype)},
+                {"value_powers", c.value_powers, 1, !kv_is_mx(c.dtype)}});
   if (st != GORIO_OK) return st;
   StoreParams p;
   p.keys = static_cast<const uint16_t *>(keys);
@@ -148,6 +183,8 @@ extern "C" gorio_status gorio_kv_store(const gorio_kv_cache *cache, gorio_kv_dty
   p.to_values = static_cast<uint8_t *>(c.values);
   p.key_scale = c.key_scale;
   p.value_scale = c.value_scale;
+  p.key_powers = c.key_powers;
+  p.value_powers = c.value_powers;
   p.slots = slots;
   p.key_stride = key_stride;
   p.value_stride = value_stride;
@@ -163,8 +200,13 @@ extern "C" gorio_status gorio_kv_store(const gorio_kv_cache *cache, gorio_kv_dty
   const uint64_t grid = (p.parts + kParts - 1) / kParts;
   if (grid >= 1ull << 24) return fail(GORIO_EINVAL, "tokens=%llu too large", (unsigned long long)tokens);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (c.dtype != GORIO_KV_E4M3) store_kernel<0><<<(uint32_t)grid, 256, 0, s>>>(p);
-  else if (dtype == GORIO_KV_BF16) store_kernel<1><<<(uint32_t)grid, 256, 0, s>>>(p);
-  else store_kernel<2><<<(uint32_t)grid, 256, 0, s>>>(p);
+  const bool f16 = dtype == GORIO_KV_F16;
+  auto launch = [&](void (*kernel)(StoreParams)) { kernel<<<(uint32_t)grid, 256, 0, s>>>(p); };
+  switch (c.dtype) {
+    case GORIO_KV_E4M3: launch(f16 ? store_kernel<2> : store_kernel<1>); break;
+    case GORIO_KV_MX8: launch(f16 ? store_kernel<4> : store_kernel<3>); break;
+    case GORIO_KV_MX4: launch(f16 ? store_kernel<6> : store_kernel<5>); break;
+    default: launch(store_kernel<0>);
+  }
   return kv_launched("gorio_kv_store");
 }

@@ -20,7 +20,7 @@ import ctypes
 import struct
 from typing import NamedTuple
 
-BF16, F16, E4M3 = 0, 1, 2
+BF16, F16, E4M3, MX8, MX4 = 0, 1, 2, 4, 5
 
 
 class CacheDesc(ctypes.Structure):
@@ -28,7 +28,7 @@ class CacheDesc(ctypes.Structure):
     _fields_ = [(f, ctypes.c_uint32) for f in ("dtype", "heads", "D", "page_tokens")] + [
         ("num_pages", ctypes.c_uint64), ("keys", ctypes.c_void_p), ("values", ctypes.c_void_p)] + [
         (f, ctypes.c_uint64) for f in ("page_stride", "head_stride", "token_stride")] + [
-        ("key_scale", ctypes.c_void_p), ("value_scale", ctypes.c_void_p)]
+        (f, ctypes.c_void_p) for f in ("key_scale", "value_scale", "key_powers", "value_powers")]
 
 
 class AttentionDesc(ctypes.Structure):
@@ -54,6 +54,10 @@ def declare(L):
     L.gorio_kv_plan.argtypes = [v, v, u64, u32, v, u64, v, u32, u64, v, v, v, v, v, v]
     L.gorio_kv_store.restype = i32
     L.gorio_kv_store.argtypes = [v, i32, v, v, u64, u64, u64, v, v]
+    L.gorio_kv_load.restype = i32
+    L.gorio_kv_load.argtypes = [v, i32, v, u64, v, v, u64, u64, v]
+    L.gorio_kv_share.restype = i32
+    L.gorio_kv_share.argtypes = [v, v, v, u64, u32, u32, u32, v, v, v, v]
     L.gorio_kv_attend.restype = i32
     L.gorio_kv_attend.argtypes = [v, v, v, u64, v]
     L.gorio_kv_workspace.restype = i32
@@ -181,18 +185,59 @@ def kv_plan(before, added, free_pages, tables, page_tokens: int, tokens: int) ->
     return KVPlan(starts, lens, positions, slots, taken)
 
 
+class KVSharing(NamedTuple):
+    """What kv_share returns, on the device, int32: first (requests + 1), the
+    groups' first requests, and shared (requests), the positions that a request
+    shares with its group; common (requests), those it shares with the request
+    before it.  A program that knows its groups makes first (groups + 1) and
+    shared by itself."""
+    first: object
+    shared: object
+    common: object = None
+
+
+def kv_share(tables, held, page_tokens: int, *, fills=None, least: int = 256) -> KVSharing:
+    """Which neighbouring requests have their first pages in common
+    (gorio_kv_share), for KVCache.attend.  held (requests, int32): positions
+    that all of a request's new tokens see, its tokens before the step or its
+    prefix; least: fewer positions than this are not shared."""
+    torch, L = _bind()
+    dev = _on_gpu("tables", tables)
+    if tables.dim() != 2:
+        raise ValueError(f"tables must be (requests, width), not {tuple(tables.shape)}")
+    B, width = tables.shape
+    _need("tables", tables, torch.int32, tables.shape, dev)
+    _need("held", held, torch.int32, (B,), dev)
+    if fills is not None:
+        _need("fills", fills, torch.int32, tables.shape, dev)
+    first = torch.empty(B + 1, dtype=torch.int32, device=dev)
+    shared, common = torch.empty_like(held), torch.empty_like(held)
+    if B == 0:
+        return KVSharing(first.zero_(), shared, common)
+    _done(L.gorio_kv_share(tables.data_ptr(), None if fills is None else fills.data_ptr(), held.data_ptr(), B, width,
+                           _count("page_tokens", page_tokens), _count("least", least), common.data_ptr(),
+                           first.data_ptr(), shared.data_ptr(), _stream(dev)))
+    return KVSharing(first, shared, common)
+
+
 class KVCache:
     """The pages of one layer: `keys` and `values` are the program's own
     tensors, pages x heads x page_tokens x D (any strides that are multiples of
     8 elements, the last dimension contiguous), bfloat16, float16 or
     float8_e4m3fn; with 8 bits, key_scale and value_scale (float32, one a head)
-    are what an element is to be multiplied by."""
+    are what an element is to be multiplied by.
+
+    Pages whose elements share a power of two by blocks of 32 (D a multiple of
+    32): keys and values float8_e4m3fn, or float4_e2m1fn_x2 whose last dimension
+    is D / 2, with key_scale and value_scale float8_e8m0fnu, pages x heads x
+    page_tokens x D / 32, which `store` writes as well; their strides are those
+    of the elements divided by 32."""
 
     def __init__(self, keys, values, key_scale=None, value_scale=None):
         import torch
-        codes = {torch.bfloat16: BF16, torch.float16: F16, torch.float8_e4m3fn: E4M3}
+        codes = {torch.bfloat16: BF16, torch.float16: F16, torch.float8_e4m3fn: E4M3, torch.float4_e2m1fn_x2: MX4}
         if keys.dtype not in codes:
-            raise TypeError(f"keys must be bfloat16, float16 or float8_e4m3fn, not {keys.dtype}")
+            raise TypeError(f"keys must be bfloat16, float16, float8_e4m3fn or float4_e2m1fn_x2, not {keys.dtype}")
         if keys.dim() != 4:
             raise ValueError(f"keys must be (pages, heads, page_tokens, D), not {tuple(keys.shape)}")
         if any(n > 1 and step == 0 for n, step in zip(keys.shape, keys.stride())):
@@ -204,7 +249,25 @@ class KVCache:
         pages, heads, page_tokens, D = keys.shape
         if keys.stride(3) != 1:
             raise ValueError("the last dimension of keys must be contiguous")
-        if keys.dtype == torch.float8_e4m3fn:
+        code, wide = codes[keys.dtype], 1                              # wide: elements of one of torch's
+        if code == MX4 or any(s is not None and s.dtype == torch.float8_e8m0fnu for s in (key_scale, value_scale)):
+            if code not in (E4M3, MX4):
+                raise ValueError("scales of float8_e8m0fnu belong to float8_e4m3fn and float4_e2m1fn_x2 pages")
+            code, wide = (MX4, 2) if code == MX4 else (MX8, 1)
+            D *= wide
+            if D % 32:
+                raise ValueError(f"D is {D}, need a multiple of 32 for these pages")
+            steps = tuple(n * wide / 32 for n in keys.stride()[:3]) + (1,)
+            if key_scale is None or value_scale is None:
+                raise ValueError("key_scale and value_scale are needed for these pages")
+            for name, scale in (("key_scale", key_scale), ("value_scale", value_scale)):
+                if scale.dtype != torch.float8_e8m0fnu:
+                    raise TypeError(f"{name} must be float8_e8m0fnu, not {scale.dtype}")
+                if scale.shape != (pages, heads, page_tokens, D // 32) or scale.device != dev:
+                    raise ValueError(f"{name} must have shape {(pages, heads, page_tokens, D // 32)} on {dev}")
+                if any(n > 1 and a != b for n, a, b in zip(scale.shape, scale.stride(), steps)):
+                    raise ValueError(f"the strides of {name} must be those of the elements divided by 32, {steps}")
+        elif code == E4M3:
             for name, scale in (("key_scale", key_scale), ("value_scale", value_scale)):
                 if scale is not None:
                     _need(name, scale, torch.float32, (heads,), dev)
@@ -212,12 +275,12 @@ class KVCache:
             raise ValueError("key_scale and value_scale belong to float8_e4m3fn pages")
         self.keys, self.values, self.key_scale, self.value_scale = keys, values, key_scale, value_scale
         self.heads, self.page_tokens, self.D, self.device = heads, page_tokens, D, dev
-        self._code = codes[keys.dtype]
-        self._codes = codes
-        self._desc = CacheDesc(self._code, heads, D, page_tokens, pages, keys.data_ptr(), values.data_ptr(),
-                               keys.stride(0), keys.stride(1), keys.stride(2),
-                               None if key_scale is None else key_scale.data_ptr(),
-                               None if value_scale is None else value_scale.data_ptr())
+        self._code = code
+        self._codes = {torch.bfloat16: BF16, torch.float16: F16}
+        at = [None if s is None else s.data_ptr() for s in (key_scale, value_scale)]
+        scales = [None, None, *at] if code in (MX8, MX4) else [*at, None, None]
+        self._desc = CacheDesc(code, heads, D, page_tokens, pages, keys.data_ptr(), values.data_ptr(),
+                               *(n * wide for n in keys.stride()[:3]), *scales)
         self._ref = ctypes.addressof(self._desc)
         self._layouts, self._spaces = {}, {}    # what _rows found of a layout; workspace bytes of a call's sizes
 
@@ -231,8 +294,8 @@ class KVCache:
             return known
         if x.dim() != 3 or x.shape[2] != self.D or (heads is not None and x.shape[1] != heads):
             raise ValueError(f"{name} must be (tokens, {heads or 'heads'}, {self.D}), not {tuple(x.shape)}")
-        code = self._codes.get(x.dtype, E4M3)
-        if code == E4M3:
+        code = self._codes.get(x.dtype)
+        if code is None:
             raise TypeError(f"{name} must be bfloat16 or float16, not {x.dtype}")
         T, H, D = x.shape
         if (D > 1 and x.stride(2) != 1) or (H > 1 and x.stride(1) != D):
@@ -259,6 +322,34 @@ class KVCache:
         if T:
             _done(L.gorio_kv_store(self._ref, code, keys.data_ptr(), values.data_ptr(), T, key_stride, value_stride,
                                    slots.data_ptr(), _stream(self.device)))
+
+    def load(self, slots, dtype=None, keys=None, values=None):
+        """(keys, values): the rows of the pages at `slots` (int64), tokens x heads x
+        D each, of the pages' type, or bfloat16 or float16 as `dtype` says where
+        they hold 8 or 4 bits; zeros where a slot is below 0 or past the pages.
+        keys, values: rows to write to (they may be parts of wider ones)."""
+        torch, L = _bind()
+        if dtype is None:
+            dtype = keys.dtype if keys is not None else self.keys.dtype if self._code <= F16 else torch.bfloat16
+        _need("slots", slots, torch.int64, (slots.numel(),), self.device)
+        T, at = slots.numel(), []
+        code = self._codes.get(dtype)
+        if code is None:
+            raise TypeError(f"rows are bfloat16 or float16, not {dtype}")
+        rows = [keys, values]
+        for i, name in enumerate(("keys", "values")):
+            if rows[i] is None:
+                rows[i] = torch.empty((T, self.heads, self.D), dtype=dtype, device=self.device)
+            got, stride = self._rows(name, rows[i], self.heads)
+            if got != code or rows[i].shape[0] != T:
+                raise ValueError(f"{name} must be {T} rows of {dtype}")
+            at.append(stride)
+        if any(x.requires_grad for x in rows) and torch.is_grad_enabled():
+            _no_gradients()
+        if T:
+            _done(L.gorio_kv_load(self._ref, code, slots.data_ptr(), T, rows[0].data_ptr(), rows[1].data_ptr(), *at,
+                                  _stream(self.device)))
+        return tuple(rows)
 
     def attend(self, q, starts, lens, tables, *, fills=None, prefix=None, slopes=None, scale: float | None = None,
                cap: float = 0.0, window: int = 0, max_new: int = 0, out=None, with_lse: bool = False):
