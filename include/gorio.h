@@ -580,6 +580,35 @@ gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio_kv_attenti
 gorio_status gorio_kv_workspace(const gorio_kv_cache *cache, const gorio_kv_attention *a,
                                 uint64_t *bytes);
 
+/* Groups of neighbouring requests that have their first pages in common, as gorio_kv_share finds
+ * them.  Every request is in one of them. */
+typedef struct {
+    uint32_t groups;        /* 1..requests; some may be empty */
+    const int32_t *first;   /* groups + 1: group g is requests first[g]..first[g+1]; ascends from 0 to requests */
+    const int32_t *shared;  /* requests: positions that a request shares with its group, the same for
+                               all of a group */
+} gorio_kv_sharing;
+
+/*
+ * gorio_kv_attend for a batch in which requests share a long prefix: the
+ * positions below shared[b] are looked up in the row of tables (and fills) of
+ * the first request of b's group, and their keys and values are read once for
+ * all rows of the group, and not once for each request.  Where the tables are
+ * as gorio_kv_share found them, the result is that of gorio_kv_attend beyond
+ * rounding, whatever else the call asks for: what a row sees of the shared
+ * positions goes by its own position, prefix, window and length.  A call with
+ * a window and without a prefix reads them for each request.
+ *   workspace: gorio_kv_workspace_shared bytes, about tokens * heads * (D + 2)
+ *              floats more than without: the sums over the shared positions.
+ */
+gorio_status gorio_kv_attend_shared(const gorio_kv_cache *cache, const gorio_kv_attention *a,
+                                    const gorio_kv_sharing *sharing, void *workspace,
+                                    uint64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that gorio_kv_attend_shared needs; from the sizes alone. */
+gorio_status gorio_kv_workspace_shared(const gorio_kv_cache *cache, const gorio_kv_attention *a,
+                                       const gorio_kv_sharing *sharing, uint64_t *bytes);
+
 /*
  * Message for the last failing call on this thread ("" if none).  Errors are
  * returned as status codes so that no failure of the transport path (Sec. 4)

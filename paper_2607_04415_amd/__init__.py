@@ -62,7 +62,8 @@ class IndexInfo(ctypes.Structure):
 EXPORTS = ("gorio_build_index", "gorio_set_cache", "gorio_set_backing", "gorio_set_query_order",
            "gorio_search", "gorio_search_noalloc", "gorio_index_info_get", "gorio_copy_pages", "gorio_locality_order",
            "gorio_cluster_order", "gorio_set_scheduler", "gorio_kv_attach", "gorio_kv_plan", "gorio_kv_store",
-           "gorio_kv_load", "gorio_kv_share", "gorio_kv_attend", "gorio_kv_workspace", "gorio_free_index", "gorio_last_error")
+           "gorio_kv_load", "gorio_kv_share", "gorio_kv_attend", "gorio_kv_workspace", "gorio_kv_attend_shared",
+           "gorio_kv_workspace_shared", "gorio_free_index", "gorio_last_error")
 
 _lib = None
 

@@ -62,8 +62,19 @@ AttendForm divide(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t
   return f;
 }
 
+// What a group's rows carry, in the workspace before the parts.
+uint64_t carry_bytes(const gorio_kv_cache &c, const gorio_kv_attention &a) {
+  return (a.tokens * a.heads * (c.D + 2) * sizeof(float) + 15) / 16 * 16;
+}
+
+// The groups that a call computes the shared positions of.  A window without a prefix hides most
+// of what a long one shares, so such calls read it for each request.
+uint32_t groups_of(const gorio_kv_attention &a, const gorio_kv_sharing *sharing) {
+  return sharing && !(a.window && !a.prefix) ? sharing->groups : 0;
+}
+
 // The forms that a call needs, and its workspace, which they use in turn.
-AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint64_t *bytes) {
+AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t groups, uint64_t *bytes) {
   AttendLaunch l{};
   l.pages = c.dtype == GORIO_KV_E4M3 ? kPagesE4m3 : c.dtype == GORIO_KV_MX8 ? kPagesMx8 : c.dtype == GORIO_KV_MX4 ? kPagesMx4 : kPages16;
   l.more = a.cap > kQuickCap ? 3 : a.cap > 0.f ? 2 : a.slopes ? 1 : 0;
@@ -92,33 +103,51 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   if (few) l.few = divide(c, a, kFewRows, kFewBlock, 8, 16, 256, many);
   if (many) l.many = divide(c, a, many_rows(steps), kManyBlock, 4, 8, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
   if (few && many) l.few.upto = l.many.from = kFewUpto;
+  if (groups) {
+    l.groups = groups;
+    l.group = divide(c, a, many_rows(steps), kManyBlock, 4, 0, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
+  }
   auto room = [&](const AttendForm &f) -> uint64_t {  // of a share and key head: two parts, and which tile is cut
     return f.cuts ? (uint64_t)f.shares * c.heads * (2 * (c.D + 2) * sizeof(float) * f.rows + sizeof(Cut)) : 0;
   };
-  *bytes = std::max(room(l.few), room(l.many));
+  *bytes = std::max({room(l.few), room(l.many), room(l.group)}) + (groups ? carry_bytes(c, a) : 0);
   return l;
 }
 
 }  // namespace
 
-extern "C" gorio_status gorio_kv_workspace(const gorio_kv_cache *cache, const gorio_kv_attention *a, uint64_t *bytes) {
-  gorio_kv_cache c;
-  gorio_kv_attention at;
-  const gorio_status st = check(cache, a, &c, &at);
-  if (st != GORIO_OK) return st;
-  if (!bytes) return fail(GORIO_EINVAL, "bytes is NULL");
-  *bytes = 0;
-  if (at.tokens && at.requests) (void)forms_of(c, at, bytes);
+namespace {
+
+gorio_status check_sharing(const gorio_kv_attention &a, const gorio_kv_sharing *sharing) {
+  if (sharing && a.requests && (sharing->groups == 0 || sharing->groups > a.requests))
+    return fail(GORIO_EINVAL, "groups=%u, need 1..%u, the requests", sharing->groups, a.requests);
   return GORIO_OK;
 }
 
-extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio_kv_attention *a, void *workspace,
-                                        uint64_t workspace_bytes, void *stream) {
+gorio_status workspace_of(const gorio_kv_cache *cache, const gorio_kv_attention *a, const gorio_kv_sharing *sharing,
+                          uint64_t *bytes) {
   gorio_kv_cache c;
   gorio_kv_attention at;
   gorio_status st = check(cache, a, &c, &at);
   if (st != GORIO_OK) return st;
+  st = check_sharing(at, sharing);
+  if (st != GORIO_OK) return st;
+  if (!bytes) return fail(GORIO_EINVAL, "bytes is NULL");
+  *bytes = 0;
+  if (at.tokens && at.requests) (void)forms_of(c, at, groups_of(at, sharing), bytes);
+  return GORIO_OK;
+}
+
+gorio_status attend(const gorio_kv_cache *cache, const gorio_kv_attention *a, const gorio_kv_sharing *sharing,
+                    void *workspace, uint64_t workspace_bytes, void *stream) {
+  gorio_kv_cache c;
+  gorio_kv_attention at;
+  gorio_status st = check(cache, a, &c, &at);
+  if (st != GORIO_OK) return st;
+  st = check_sharing(at, sharing);
+  if (st != GORIO_OK) return st;
   if (at.tokens == 0 || at.requests == 0) return GORIO_OK;
+  const uint32_t groups = groups_of(at, sharing);
   KvDevice dev;
   st = dev.use({{"q", at.q, 16, false},
                 {"out", at.out, 16, false},
@@ -129,6 +158,8 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
                 {"fills", at.fills, 4, true},
                 {"prefix", at.prefix, 4, true},
                 {"slopes", at.slopes, 4, true},
+                {"first", sharing ? sharing->first : nullptr, 4, !sharing},
+                {"shared", sharing ? sharing->shared : nullptr, 4, !sharing},
                 {"cache keys", c.keys, 16, false},
                 {"cache values", c.values, 16, false},
                 {"key_scale", c.key_scale, 4, true},
@@ -138,7 +169,7 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
                 {"workspace", workspace, 16, workspace_bytes == 0}});
   if (st != GORIO_OK) return st;
   uint64_t bytes = 0;
-  const AttendLaunch l = forms_of(c, at, &bytes);
+  const AttendLaunch l = forms_of(c, at, groups, &bytes);
   if (bytes > workspace_bytes)
     return fail(GORIO_EINVAL, "workspace of %llu bytes, need %llu", (unsigned long long)workspace_bytes,
                 (unsigned long long)bytes);
@@ -159,7 +190,12 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
   p.fills = at.fills;
   p.prefix = at.prefix;
   p.slopes = at.slopes;
-  p.parts = static_cast<float *>(workspace);
+  p.first = groups ? sharing->first : nullptr;
+  p.shared = groups ? sharing->shared : nullptr;
+  p.carry = groups ? static_cast<float *>(workspace) : nullptr;
+  p.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + (groups ? carry_bytes(c, at) : 0));
+  p.all_requests = at.requests;
+  p.grouped = false;
   p.q_stride = at.q_stride;
   p.out_stride = at.out_stride;
   p.page_stride = kv_bytes(c.dtype, c.page_stride);
@@ -185,4 +221,28 @@ extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio
       {launch_attend_f16, launch_attend_f16_e4m3, launch_attend_f16_mx8, launch_attend_f16_mx4}};
   const hipError_t e = kLaunch[at.dtype == GORIO_KV_F16][l.pages](p, l, s);
   return e == hipSuccess ? GORIO_OK : fail(GORIO_EDEVICE, "gorio_kv_attend: %s", hipGetErrorString(e));
+}
+
+}  // namespace
+
+extern "C" gorio_status gorio_kv_workspace(const gorio_kv_cache *cache, const gorio_kv_attention *a, uint64_t *bytes) {
+  return workspace_of(cache, a, nullptr, bytes);
+}
+
+extern "C" gorio_status gorio_kv_attend(const gorio_kv_cache *cache, const gorio_kv_attention *a, void *workspace,
+                                        uint64_t workspace_bytes, void *stream) {
+  return attend(cache, a, nullptr, workspace, workspace_bytes, stream);
+}
+
+extern "C" gorio_status gorio_kv_workspace_shared(const gorio_kv_cache *cache, const gorio_kv_attention *a,
+                                                  const gorio_kv_sharing *sharing, uint64_t *bytes) {
+  if (!sharing) return fail(GORIO_EINVAL, "sharing is NULL");
+  return workspace_of(cache, a, sharing, bytes);
+}
+
+extern "C" gorio_status gorio_kv_attend_shared(const gorio_kv_cache *cache, const gorio_kv_attention *a,
+                                               const gorio_kv_sharing *sharing, void *workspace,
+                                               uint64_t workspace_bytes, void *stream) {
+  if (!sharing) return fail(GORIO_EINVAL, "sharing is NULL");
+  return attend(cache, a, sharing, workspace, workspace_bytes, stream);
 }

@@ -179,6 +179,15 @@ struct AttendParams {
   const int32_t *starts, *lens, *tables, *fills, *prefix;
   const float *slopes;
   float *parts;  // workspace
+  // Shared prefixes (NULL without): group g is requests first[g]..first[g + 1], and request b's
+  // positions below shared[b] lie in the pages of its group's first.  A launch of its own, in which
+  // a group stands for a request, leaves of each row the sums over those positions in `carry`
+  // (D floats a row, all rows, then their maximum and sum of weights); the launches after it
+  // start behind them and add these.
+  const int32_t *first, *shared;
+  float *carry;
+  uint32_t all_requests;
+  bool grouped;  // this launch's requests are groups
   uint64_t q_stride, out_stride;                    // elements
   uint64_t page_stride, head_stride, token_stride;  // bytes
   uint32_t tokens, num_pages, requests, width, heads, kv_heads, D;
@@ -196,6 +205,9 @@ struct AttendParams {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// 2^x; -inf gives 0.
+__device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
+
 // A row of zeros that lanes without a key (or past a head's D) read instead of
 // memory that is not theirs: a 0 from here, times any weight, adds nothing.
 __device__ __align__(16) static uint32_t kv_zeros[128];
@@ -203,10 +215,38 @@ __device__ __align__(16) static uint32_t kv_zeros[128];
 // A request as the kernels see it: every value clamped into its range.
 struct Request {
   int32_t start, added, len, prefix;
+  int32_t skip;  // positions that were computed for the group
+  uint32_t row;  // of the tables
 };
 
+// Shared positions that are computed for the group: whole blocks of either form, so that the
+// requests' own blocks begin where the group's end.
+constexpr int32_t kSharedBlock = 64;
+__device__ __forceinline__ int32_t shared_of(const AttendParams &p, uint32_t b) {
+  const int64_t held = (int64_t)p.width * p.page_tokens.d;  // below 2^31
+  return (int32_t)min((int64_t)max(p.shared[b], 0), held) & -kSharedBlock;
+}
+
+// A group as a request: its requests' tokens, which follow one another, and the shared positions.
+__device__ __forceinline__ uint32_t first_of(const AttendParams &p, uint32_t g) {
+  return (uint32_t)min(max(p.first[g], 0), (int32_t)p.all_requests);
+}
+__device__ __forceinline__ Request group_of(const AttendParams &p, uint32_t g) {
+  Request r{};
+  r.row = first_of(p, g);
+  const uint32_t end = first_of(p, g + 1);
+  if (r.row >= end) return r;
+  r.len = r.prefix = shared_of(p, r.row);
+  r.start = min(max(p.starts[r.row], 0), (int32_t)p.tokens);
+  r.added = r.len ? max(min(max(p.starts[end], 0), (int32_t)p.tokens) - r.start, 0) : 0;
+  return r;
+}
+
 __device__ __forceinline__ Request request_of(const AttendParams &p, uint32_t b) {
+  if (p.grouped) return group_of(p, b);
   Request r;
+  r.row = b;
+  r.skip = p.shared ? shared_of(p, b) : 0;
   r.start = min(max(p.starts[b], 0), (int32_t)p.tokens);
   r.added = max(min(max(p.starts[b + 1], 0), (int32_t)p.tokens) - r.start, 0);
   r.len = max(p.lens[b], 0);
@@ -215,11 +255,11 @@ __device__ __forceinline__ Request request_of(const AttendParams &p, uint32_t b)
 }
 
 // The key blocks of kBlock keys that a run of tokens at positions first..last
-// sees something of: `head` blocks from 0 (the prefix), then those from `near`
-// on (the window), `count` in all.
+// sees something of: `head` blocks from `skip` on (the prefix), then those from
+// `near` on (the window), `count` in all.
 struct KeyRange {
-  int32_t head, near, count, end;  // end: no key from here on is seen
-  __device__ __forceinline__ int32_t block(int32_t x) const { return x < head ? x : x - head + near; }
+  int32_t skip, head, near, count, end;  // end: no key from here on is seen
+  __device__ __forceinline__ int32_t block(int32_t x) const { return x < head ? x + skip : x - head + near; }
 };
 
 template <int kBlock>
@@ -229,8 +269,10 @@ __device__ __forceinline__ KeyRange key_range(const AttendParams &p, const Reque
   const int32_t prefix = min(r.prefix, held);
   k.end = min(held, max(last + 1, prefix));
   const int32_t from = (int32_t)max((int64_t)first - p.window + 1, (int64_t)0);
-  k.head = (prefix + kBlock - 1) / kBlock;
-  k.near = max(k.head, from / kBlock);
+  k.skip = r.skip / kBlock;
+  const int32_t seen = max((prefix + kBlock - 1) / kBlock, k.skip);
+  k.head = seen - k.skip;
+  k.near = max(seen, from / kBlock);
   const int32_t ends = (k.end + kBlock - 1) / kBlock;
   k.count = k.head + max(ends - k.near, 0);
   return k;
@@ -317,7 +359,8 @@ __device__ __forceinline__ uint64_t one(uint64_t v) {
 }
 __device__ __forceinline__ Request one(const Request &r) {
   return Request{__builtin_amdgcn_readfirstlane(r.start), __builtin_amdgcn_readfirstlane(r.added),
-                 __builtin_amdgcn_readfirstlane(r.len), __builtin_amdgcn_readfirstlane(r.prefix)};
+                 __builtin_amdgcn_readfirstlane(r.len), __builtin_amdgcn_readfirstlane(r.prefix),
+                 __builtin_amdgcn_readfirstlane(r.skip), (uint32_t)__builtin_amdgcn_readfirstlane((int)r.row)};
 }
 
 // The tile of the block that share number `index` begins with, or false if the line ends before.
@@ -449,6 +492,81 @@ __device__ __forceinline__ Part part_of(const AttendParams &p, const WorkItem &w
   return a;
 }
 
+// Tokens of a group's tile: of a group's tokens each has its own request's position and prefix.
+struct TokenSees {
+  int32_t pos, prefix;
+};
+struct TileSees {
+  int32_t first, last, prefix;  // least and largest position, least prefix
+};
+
+// Fills in `tokens` for the tile's tokens and returns what all of them see, the same to all threads.
+template <int kThreads, int kRows>
+__device__ TileSees place_tokens(const AttendParams &p, const WorkItem &w, const Tile &tile, TokenSees *tokens) {
+  static_assert(kRows <= kThreads, "a thread a token");
+  __shared__ TileSees s_sees[kThreads / 64];
+  const uint32_t t0 = w.r.start + fastdiv(tile.row0, p.group);
+  const uint32_t count = w.r.start + fastdiv(tile.row0 + tile.rows - 1, p.group) + 1 - t0;  // at most kRows
+  if (threadIdx.x < kRows) tokens[threadIdx.x] = TokenSees{-1, 0};  // of no request: sees nothing
+  __syncthreads();
+  const uint32_t end = first_of(p, w.request + 1);
+  for (uint32_t b = w.r.row + threadIdx.x; b < end; b += kThreads) {
+    const uint32_t from = (uint32_t)min(max(p.starts[b], 0), (int32_t)p.tokens);
+    const uint32_t upto = (uint32_t)min(max(p.starts[b + 1], 0), (int32_t)p.tokens);
+    if (from >= t0 + count || upto <= t0) continue;
+    const int32_t len = max(p.lens[b], 0), prefix = p.prefix ? min(max(p.prefix[b], 0), len) : 0;
+    for (uint32_t t = max(from, t0); t < min(upto, t0 + count); ++t)
+      tokens[t - t0] = TokenSees{len - (int32_t)(upto - t), prefix};
+  }
+  __syncthreads();
+  TileSees s{0x7FFFFFFF, -1, 0x7FFFFFFF};
+  if (threadIdx.x < count) {
+    const TokenSees mine = tokens[threadIdx.x];
+    s = TileSees{mine.pos, mine.pos, mine.prefix};
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    s.first = min(s.first, __shfl_xor(s.first, d));
+    s.last = max(s.last, __shfl_xor(s.last, d));
+    s.prefix = min(s.prefix, __shfl_xor(s.prefix, d));
+  }
+  if ((threadIdx.x & 63) == 0) s_sees[threadIdx.x >> 6] = s;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kThreads / 64; ++i) {
+    s.first = min(s.first, s_sees[i].first);
+    s.last = max(s.last, s_sees[i].last);
+    s.prefix = min(s.prefix, s_sees[i].prefix);
+  }
+  return TileSees{__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.last),
+                  __builtin_amdgcn_readfirstlane(s.prefix)};
+}
+
+// A row's sums over its group's shared positions: where they lie, and how they count beside sums
+// over others with the maximum `best`.
+struct Carried {
+  const float *o;
+  float m, l, by;  // maximum, sum of weights, factor of both
+};
+__device__ __forceinline__ uint64_t carried_row(const AttendParams &p, uint64_t token, uint32_t head) {
+  return token * p.heads + head;
+}
+__device__ __forceinline__ float *carried_sums(const AttendParams &p, uint64_t row) {
+  return p.carry + (uint64_t)p.tokens * p.heads * p.D + row * 2;
+}
+// Takes them in: `best` becomes the larger maximum; returns the factor of the sums that had it.
+__device__ __forceinline__ float take_carried(const AttendParams &p, uint64_t row, float &best, Carried &c) {
+  const float *ml = carried_sums(p, row);
+  c.o = p.carry + row * p.D;
+  c.m = ml[0];
+  c.l = ml[1];
+  const float most = fmaxf(best, c.m), from = most == -INFINITY ? 0.f : most;
+  const float keep = pow2(best - from);
+  c.by = pow2(c.m - from);
+  best = most;
+  return keep;
+}
+
 // What the joining kernel needs of the tile that begins in a share and is cut at its end; parts
 // is 0 if there is none.  Written by the share's workgroup behind the parts' sums: to find the
 // tile again from the lengths took the joining kernel 12 us for 264 tiles.
@@ -492,7 +610,7 @@ __device__ __forceinline__ KeyLook key_look(const AttendParams &p, const WorkIte
   k.seen = in_part & (j < end) & (near | (j < w.r.prefix));
   const uint32_t at = (uint32_t)(k.seen ? j : 0), e = fastdiv(at, p.page_tokens);
   k.place = at - e * p.page_tokens.d;
-  const uint64_t entry = (uint64_t)w.request * p.width + e;
+  const uint64_t entry = (uint64_t)w.r.row * p.width + e;
   k.page = p.tables[entry];
   k.fill = p.fills ? p.fills[entry] : 0x7FFFFFFF;
   return k;
@@ -540,9 +658,6 @@ __device__ __forceinline__ float max16(const f32x16 &s) {
 #undef GORIO_MAX14
   return r;
 }
-
-// 2^x; -inf gives 0.
-__device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Caps up to this one go by one exponential and one reciprocal a score, which is good to 2^-21 of
 // the cap then, 2^-15 at most.  Past it that error, which is as much of a weight, would grow with

@@ -268,7 +268,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   float most = s_m[0][row];
 #pragma unroll
   for (int i = 1; i < kFewWaves; ++i) most = fmaxf(most, s_m[i][row]);
-  const float base = most == -INFINITY ? 0.f : most;
+  float base = most == -INFINITY ? 0.f : most;
   float by[kFewWaves], all = 0.f;
 #pragma unroll
   for (int i = 0; i < kFewWaves; ++i) {
@@ -279,6 +279,15 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   const uint64_t t_out = (uint64_t)(w.r.start + tk);
   const float vs = p.value_scale ? p.value_scale[head] : 1.f;
   const bool divided = part.divided;
+  const bool carries = w.r.skip > 0 && part.from == 0;  // the group's sums join as those of one wave more
+  Carried carried{nullptr, 0.f, 0.f, 0.f};
+  if (carries) {
+    const float keep = take_carried(p, carried_row(p, t_out, hq), most, carried);
+    base = most == -INFINITY ? 0.f : most;
+    all = all * keep + carried.l * carried.by;
+#pragma unroll
+    for (int i = 0; i < kFewWaves; ++i) by[i] *= keep;
+  }
   const float norm = divided ? 1.f : all != 0.f ? vs / all : 0.f;
   const uint64_t slot = ((uint64_t)part.slot * p.kv_heads + head) * kFewRows + row;
 #pragma unroll
@@ -294,6 +303,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = fmaf(o4[e], by[j], y[e]);
       }
+      if (carries) y += *reinterpret_cast<const f32x4 *>(carried.o + d + i) * carried.by;
       y *= norm;
       if (divided)
         *reinterpret_cast<f32x4 *>(p.parts + slot * p.D + d + i) = y;
@@ -331,7 +341,7 @@ __global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParam
   }
 }
 
-// Joins the parts of divided tiles: a workgroup a share and head, for the tile that begins in the
+// Joins the parts of divided tiles, of a group's into what its rows carry: a workgroup a share and head, for the tile that begins in the
 // share and is cut at its end; 16 rows, 16 threads a row (64 rows a workgroup, four after the other:
 // 128 new tokens over 2000 took 54 us in all, now 41).  A row's parts are added one after the
 // other, and each waits for its loads.
@@ -386,6 +396,22 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
     const float norm = all != 0.f ? vs / all : 0.f;
     const uint32_t tk = fastdiv(cut.row0 + row, p.group), hq = head * p.group.d + (cut.row0 + row - tk * p.group.d);
     const uint64_t t_out = (uint64_t)(cut.start + tk);
+    if (p.grouped) {
+      const uint64_t at = carried_row(p, t_out, hq);
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const uint32_t d = i ? d1 : d0;
+        if (d >= p.D) continue;
+        *reinterpret_cast<f32x4 *>(p.carry + at * p.D + d) = y[i];
+        *reinterpret_cast<f32x4 *>(p.carry + at * p.D + d + 4) = y[i + 1];
+      }
+      if (lane == 0) {
+        float *sums = carried_sums(p, at);
+        sums[0] = most;
+        sums[1] = all;
+      }
+      return;
+    }
     uint16_t *out = p.out + t_out * p.out_stride + (uint64_t)hq * p.D;
 #pragma unroll
     for (int i = 0; i < 4; i += 2) {

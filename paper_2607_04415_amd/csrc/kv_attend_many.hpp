@@ -61,7 +61,7 @@ constexpr float kSlack = 8.f;
 // own: a branch in those of 2 made these spill up to 40 registers more, for caps of any size).  Pages
 // of blocks with powers have no kernels of 1: those of 3 serve biases without a cap as well.
 template <typename Q, int kPages, int kSteps, int kMore>
-__device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
+__device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem &w, Tile tile,
                                           const KeyRange &range, const Part &part, uint32_t head) {
   constexpr int kManyWaves = many_waves(kSteps), kManyThreads = kManyWaves * 64, kManyRows = kManyWaves * 32;
   constexpr int kDim = kSteps * 32, kChunks = kDim / 8;                              // 16-byte pieces of a row
@@ -86,6 +86,17 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   __shared__ uint64_t s_odd[2][kDim];
   __shared__ uint32_t s_any_odd[kManyWaves];
 
+  __shared__ TokenSees s_tokens[kManyRows];  // of a group's tile
+  // Positions below it are seen by all rows of the tile.  What a group's rows see differs, and
+  // w.r.prefix is its end there: no row sees more.
+  int32_t sure = w.r.prefix;
+  if (p.grouped) {
+    const TileSees s = place_tokens<kManyThreads, kManyRows>(p, w, tile, s_tokens);
+    tile.first = s.first;
+    tile.last = s.last;
+    sure = s.prefix;
+  }
+
   const int32_t x0 = (int32_t)part.from, x_end = min(range.count, (int32_t)part.upto);
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -99,8 +110,10 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   const uint32_t row = min(tile.row0 + (uint32_t)wave * 32 + m, tile.row0 + tile.rows - 1);
   const uint32_t token = fastdiv(row, p.group), gh = row - token * p.group.d;
   const int32_t base = w.r.len - w.r.added;
-  const int32_t pos = base + (int32_t)token;
-  const int32_t first = base + (int32_t)fastdiv(wave_row, p.group), last = base + (int32_t)fastdiv(wave_end, p.group);
+  const uint32_t in_tile = token - fastdiv(tile.row0, p.group);
+  const int32_t pos = p.grouped ? s_tokens[in_tile].pos : base + (int32_t)token;
+  const int32_t first = p.grouped ? tile.first : base + (int32_t)fastdiv(wave_row, p.group);
+  const int32_t last = p.grouped ? tile.last : base + (int32_t)fastdiv(wave_end, p.group);
   const uint32_t qhead = head * p.group.d + gh;
   const float scale = p.scale * (p.key_scale ? p.key_scale[head] : 1.f);
   // the running maximum is taken of the products as they are, so the factor has to be positive:
@@ -142,7 +155,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   // Every row of the tile sees every key of block x that is there, by its position.
   auto all_see = [&](int32_t x) __attribute__((always_inline)) {
     const int32_t j0 = range.block(x) * kManyBlock;
-    return (j0 + kManyBlock - 1 <= tile.first && (int64_t)tile.last - j0 < p.window) || j0 + kManyBlock <= w.r.prefix;
+    return (j0 + kManyBlock - 1 <= tile.first && (int64_t)tile.last - j0 < p.window) || j0 + kManyBlock <= sure;
   };
 
   // A thread's pieces of a block.  Straight from memory into LDS, a wave's 64 pieces lie one
@@ -395,7 +408,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
                            (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bits);
     bool odd = false;
     if (__builtin_expect(!all_see(x), 0)) odd = set_apart(v_now);
-    const bool near = (j0 + kManyBlock - 1 <= first && (int64_t)last - j0 < p.window) || j0 + kManyBlock <= w.r.prefix;
+    const bool near = (j0 + kManyBlock - 1 <= first && (int64_t)last - j0 < p.window) || j0 + kManyBlock <= sure;
     const bool any = (j0 <= last && (int64_t)j0 + kManyBlock - 1 > (int64_t)first - p.window) || j0 < w.r.prefix;
     const bool masked = !near | odd | (there != ~0ull);
     uint64_t sees = ~0ull;
@@ -403,7 +416,8 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       int32_t here = pos;
       asm("" : "+v"(here));  // what follows from it is worked out here, not kept in registers
       const int32_t oldest = (int32_t)max((int64_t)here - p.window + 1, (int64_t)0);  // the window's first key
-      sees = !any ? 0 : there & ((low_bits(here - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(w.r.prefix - j0));
+      const int32_t prefix = p.grouped ? s_tokens[in_tile].prefix : w.r.prefix;
+      sees = !any ? 0 : there & ((low_bits(here - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(prefix - j0));
     }
     auto mask = [&](f32x16 &s, uint32_t seen) __attribute__((always_inline)) {
       if (masked) {
@@ -487,7 +501,23 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   const bool divided = part.divided;
   const uint64_t t_out = (uint64_t)(w.r.start + token_out);
   const float vs = p.value_scale ? p.value_scale[head] : 1.f;
-  const float norm = divided ? 1.f : sum != 0.f ? vs / sum : 0.f;
+  const uint64_t row_carried = carried_row(p, t_out, head_out);
+  if (w.r.skip > 0 && part.from == 0) {  // the group's sums
+    Carried c;
+    const float keep = take_carried(p, row_carried, best, c);
+    sum = sum * keep + c.l * c.by;
+#pragma unroll
+    for (int t = 0; t < kSteps; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t d = t * 32 + i * 8 + g * 4;
+        if (d >= p.D) continue;
+        const f32x4 more = *reinterpret_cast<const f32x4 *>(c.o + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[t][i * 4 + e] = o[t][i * 4 + e] * keep + more[e] * c.by;
+      }
+  }
+  const float norm = divided || p.grouped ? 1.f : sum != 0.f ? vs / sum : 0.f;
   const uint64_t slot = ((uint64_t)part.slot * p.kv_heads + head) * kManyRows + wave * 32 + m;
 #pragma unroll
   for (int t = 0; t < kSteps; ++t)
@@ -498,6 +528,8 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       const f32x4 y = {o[t][i * 4] * norm, o[t][i * 4 + 1] * norm, o[t][i * 4 + 2] * norm, o[t][i * 4 + 3] * norm};
       if (divided)
         *reinterpret_cast<f32x4 *>(p.parts + slot * p.D + d) = y;
+      else if (p.grouped)
+        *reinterpret_cast<f32x4 *>(p.carry + row_carried * p.D + d) = y;
       else
         *reinterpret_cast<u32x2 *>(p.out + t_out * p.out_stride + (uint64_t)head_out * p.D + d) =
             u32x2{Q::pack(y.x, y.y), Q::pack(y.z, y.w)};
@@ -507,6 +539,10 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       float *ml = p.parts + (uint64_t)p.shares * 2 * p.kv_heads * kManyRows * p.D + slot * 2;
       ml[0] = best;
       ml[1] = sum;
+    } else if (p.grouped) {
+      float *sums = carried_sums(p, row_carried);
+      sums[0] = best;
+      sums[1] = sum;
     } else if (p.lse) {
       p.lse[t_out * p.heads + head_out] = sum != 0.f ? (best + __log2f(sum)) * kLn2 : -INFINITY;
     }

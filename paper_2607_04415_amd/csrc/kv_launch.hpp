@@ -17,6 +17,8 @@ struct AttendLaunch {
   int pages;  // a PageKind
   int more;   // 1 if scores are biased, 2 if they are capped, 3 if by a cap past kQuickCap
   AttendForm few, many;
+  AttendForm group;  // the form for many rows over the groups' shared positions, before the others
+  uint32_t groups;
 };
 
 template <typename Q, int kPages, int kSteps, int kMore>
@@ -30,17 +32,25 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
     p.whole = f.whole;
     p.cuts = f.cuts;
   };
+  auto run_many = [&](const AttendForm &f) {
+    divide(f);
+    attend_many<Q, kPages, kSteps, kMore><<<f.shares * p.kv_heads, many_waves(kSteps) * 64, 0, s>>>(p);
+    if (f.cuts)
+      attend_join<Q, many_rows(kSteps)><<<dim3((f.shares - 1) * p.kv_heads, many_rows(kSteps) / 16), 256, 0, s>>>(p);
+  };
+  if (l.group.shares) {
+    p.grouped = true;
+    p.requests = l.groups;
+    run_many(l.group);
+    p.grouped = false;
+    p.requests = p.all_requests;
+  }
   if (l.few.shares) {
     divide(l.few);
     attend_few<Q, kPages, kSteps, (kMore > 0)><<<l.few.shares * p.kv_heads, few_waves(kSteps) * 64, 0, s>>>(p);
     if (l.few.cuts) attend_join<Q, kFewRows><<<(l.few.shares - 1) * p.kv_heads, 256, 0, s>>>(p);
   }
-  if (l.many.shares) {
-    divide(l.many);
-    attend_many<Q, kPages, kSteps, kMore><<<l.many.shares * p.kv_heads, many_waves(kSteps) * 64, 0, s>>>(p);
-    if (l.many.cuts)
-      attend_join<Q, many_rows(kSteps)><<<dim3((l.many.shares - 1) * p.kv_heads, many_rows(kSteps) / 16), 256, 0, s>>>(p);
-  }
+  if (l.many.shares) run_many(l.many);
   return hipGetLastError();
 }
 

@@ -41,8 +41,14 @@ class AttentionDesc(ctypes.Structure):
         ("max_new", ctypes.c_uint32)]
 
 
+class SharingDesc(ctypes.Structure):
+    """gorio_kv_sharing"""
+    _fields_ = [("groups", ctypes.c_uint32), ("first", ctypes.c_void_p), ("shared", ctypes.c_void_p)]
+
+
 _ATTENTION = struct.Struct("4IQ2P2Q7P2f2I")   # AttentionDesc's fields, packed at once
-assert _ATTENTION.size == ctypes.sizeof(AttentionDesc)
+_SHARING = struct.Struct("I4x2P")
+assert _ATTENTION.size == ctypes.sizeof(AttentionDesc) and _SHARING.size == ctypes.sizeof(SharingDesc)
 
 
 def declare(L):
@@ -62,6 +68,10 @@ def declare(L):
     L.gorio_kv_attend.argtypes = [v, v, v, u64, v]
     L.gorio_kv_workspace.restype = i32
     L.gorio_kv_workspace.argtypes = [v, v, v]
+    L.gorio_kv_attend_shared.restype = i32
+    L.gorio_kv_attend_shared.argtypes = [v, v, v, v, u64, v]
+    L.gorio_kv_workspace_shared.restype = i32
+    L.gorio_kv_workspace_shared.argtypes = [v, v, v, v]
 
 
 _torch = _L = None
@@ -352,7 +362,8 @@ class KVCache:
         return tuple(rows)
 
     def attend(self, q, starts, lens, tables, *, fills=None, prefix=None, slopes=None, scale: float | None = None,
-               cap: float = 0.0, window: int = 0, max_new: int = 0, out=None, with_lse: bool = False):
+               cap: float = 0.0, window: int = 0, max_new: int = 0, out=None, with_lse: bool = False,
+               sharing: KVSharing | None = None):
         """Attention of the new tokens `q` (tokens x heads x D) over the pages
         (gorio_kv_attend): request b's are rows starts[b]..starts[b+1], the last
         of its lens[b] tokens, in the pages that tables[b] names.  Returns out,
@@ -363,7 +374,9 @@ class KVCache:
         (heads, float32): a score loses slope * distance.  scale: 1/sqrt(D) by
         default.  cap: scores become cap * tanh(score / cap).  window: the distance
         from which a key outside the prefix is not seen (0: none).
-        max_new: the most new tokens of a request, where the program knows it."""
+        max_new: the most new tokens of a request, where the program knows it.
+        sharing: which requests have their first pages in common, from kv_share;
+        these are then read once for all of a group (gorio_kv_attend_shared)."""
         torch, L = _bind()
         dev, i32 = self.device, torch.int32
         if (q.requires_grad or self.keys.requires_grad or self.values.requires_grad or (
@@ -394,14 +407,28 @@ class KVCache:
                             tables.data_ptr(), 0 if fills is None else fills.data_ptr(),
                             0 if prefix is None else prefix.data_ptr(), 0 if slopes is None else slopes.data_ptr(),
                             D ** -0.5 if scale is None else scale, cap, window, max_new)
-        sizes = (code, T, H, B, width, max_new)
+        groups, share = 0, None
+        if sharing is not None and B:
+            groups = sharing.first.numel() - 1
+            _need("sharing.first", sharing.first, i32, (groups + 1,), dev)
+            _need("sharing.shared", sharing.shared, i32, (B,), dev)
+            share = _SHARING.pack(max(groups, 0), sharing.first.data_ptr(), sharing.shared.data_ptr())
+        # a window without a prefix needs no room for what is shared
+        sizes = (code, T, H, B, width, max_new, share and groups, share and window and prefix is None)
         need = self._spaces.get(sizes)
         if need is None:
             got = ctypes.c_uint64()
-            _done(L.gorio_kv_workspace(self._ref, a, ctypes.addressof(got)))
+            if share is None:
+                _done(L.gorio_kv_workspace(self._ref, a, ctypes.addressof(got)))
+            else:
+                _done(L.gorio_kv_workspace_shared(self._ref, a, share, ctypes.addressof(got)))
             if len(self._spaces) > 4096:
                 self._spaces.clear()
             need = self._spaces[sizes] = got.value
         space = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-        _done(L.gorio_kv_attend(self._ref, a, None if space is None else space.data_ptr(), need, _stream(dev)))
+        at = None if space is None else space.data_ptr()
+        if share is None:
+            _done(L.gorio_kv_attend(self._ref, a, at, need, _stream(dev)))
+        else:
+            _done(L.gorio_kv_attend_shared(self._ref, a, share, at, need, _stream(dev)))
         return (out, lse) if with_lse else out

@@ -58,3 +58,24 @@ def test_share_refusals(lib, requests, width, page, least, text):  # noqa: F811
     assert lib.gorio_kv_share(None, None, None, requests, width, page, least, None, None, None, None) == g.EINVAL
     assert text in lib.gorio_last_error().decode()
     assert lib.gorio_kv_share(None, None, None, 0, 4, 16, 1, None, None, None, None) == g.OK
+
+
+def test_sharing(lib):  # noqa: F811
+    c, a = cache(dtype=kv.MX4), attention(requests=5, tokens=7)
+    n, s = ctypes.c_uint64(), kv.SharingDesc(groups=2)
+    need = lambda share: lib.gorio_kv_workspace_shared(ctypes.byref(c), ctypes.byref(a), share, ctypes.byref(n))
+    assert need(ctypes.byref(s)) == g.OK
+    assert n.value >= 7 * 4 * (64 + 2) * 4                      # of each row its sums, a maximum and a sum of weights
+    a.window = 10                                               # nothing is shared then
+    assert need(ctypes.byref(s)) == g.OK and n.value == workspace(lib, c, a)[1]
+    assert need(None) == g.EINVAL and b"sharing is NULL" in lib.gorio_last_error()
+    for groups in (0, 6, 2**32 - 1):
+        s.groups = groups
+        assert need(ctypes.byref(s)) == g.EINVAL and b"groups" in lib.gorio_last_error()
+        assert lib.gorio_kv_attend_shared(ctypes.byref(c), ctypes.byref(a), ctypes.byref(s), None, 0, None) == g.EINVAL
+    s.groups = 5
+    assert lib.gorio_kv_attend_shared(ctypes.byref(c), ctypes.byref(a), None, None, 0, None) == g.EINVAL
+    assert lib.gorio_kv_attend_shared(ctypes.byref(c), ctypes.byref(a), ctypes.byref(s), None, 0, None) == g.EINVAL
+    assert b"q is NULL" in lib.gorio_last_error()
+    a.tokens = 0
+    assert lib.gorio_kv_attend_shared(ctypes.byref(c), ctypes.byref(a), ctypes.byref(s), None, 0, None) == g.OK
