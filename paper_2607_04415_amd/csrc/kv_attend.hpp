@@ -187,7 +187,7 @@ struct AttendParams {
   const int32_t *first, *shared;
   float *carry;
   uint32_t all_requests;
-  bool grouped;  // this launch's requests are groups
+  bool grouped;  // this launch's requests are groups (the joining kernel asks; the others are made for it)
   uint64_t q_stride, out_stride;                    // elements
   uint64_t page_stride, head_stride, token_stride;  // bytes
   uint32_t tokens, num_pages, requests, width, heads, kv_heads, D;
@@ -242,8 +242,10 @@ __device__ __forceinline__ Request group_of(const AttendParams &p, uint32_t g) {
   return r;
 }
 
+// kGroup: the launch's requests are groups.
+template <bool kGroup>
 __device__ __forceinline__ Request request_of(const AttendParams &p, uint32_t b) {
-  if (p.grouped) return group_of(p, b);
+  if constexpr (kGroup) return group_of(p, b);
   Request r;
   r.row = b;
   r.skip = p.shared ? shared_of(p, b) : 0;
@@ -365,7 +367,7 @@ __device__ __forceinline__ Request one(const Request &r) {
 
 // The tile of the block that share number `index` begins with, or false if the line ends before.
 // Every thread of the workgroup gets the same answer.
-template <int kThreads, int kBlock>
+template <int kThreads, int kBlock, bool kGroup>
 __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item) {
   __shared__ uint64_t s_sums[kThreads / 64], s_begin, s_line;
   __shared__ uint32_t s_tiles[kThreads], s_counts[kThreads / 64], s_found[2];  // request, tile
@@ -387,7 +389,7 @@ __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item)
     for (uint32_t b0 = 0; b0 < p.requests; b0 += kThreads) {
       const uint32_t b = b0 + threadIdx.x;
       Request own{};
-      if (b < p.requests) own = request_of(p, b);
+      if (b < p.requests) own = request_of<kGroup>(p, b);
       const uint32_t mine = b < p.requests ? tiles_of(p, own) : 0;
       if (!__syncthreads_or(mine > 1)) {  // single tokens: a thread's request is its tile
         request = b;
@@ -422,7 +424,7 @@ __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item)
           }
           tile = f - (r ? s_tiles[r - 1] : 0);
           request = b0 + r;
-          its = request_of(p, request);
+          its = request_of<kGroup>(p, request);
           blocks = blocks_of<kBlock>(p, its, tile);
         }
         end = at + scan_threads<kThreads>((uint64_t)blocks, s_sums);
@@ -459,13 +461,14 @@ __device__ bool find_item(const AttendParams &p, uint32_t index, WorkItem &item)
 // The tile after w's on the line, if the line goes on.  Requests of the other form between two are
 // passed one at a time, each a wait for its lengths: 4 prompts of 200 tokens spread among 2000
 // single tokens take 803 us together, in front of them 683.
+template <bool kGroup>
 __device__ __forceinline__ bool next_item(const AttendParams &p, WorkItem &w, uint64_t begin) {
   w.begin = begin;
   if (++w.tile < w.tiles) return true;
   w.tile = 0;
   do {
     if (++w.request >= p.requests) return false;
-    w.r = one(request_of(p, w.request));
+    w.r = one(request_of<kGroup>(p, w.request));
     w.tiles = tiles_of(p, w.r);
   } while (w.tiles == 0);
   return true;
@@ -492,38 +495,40 @@ __device__ __forceinline__ Part part_of(const AttendParams &p, const WorkItem &w
   return a;
 }
 
-// Tokens of a group's tile: of a group's tokens each has its own request's position and prefix.
-struct TokenSees {
+// Rows of a group's tile: each has its own request's position and prefix.
+struct RowSees {
   int32_t pos, prefix;
 };
 struct TileSees {
   int32_t first, last, prefix;  // least and largest position, least prefix
 };
 
-// Fills in `tokens` for the tile's tokens and returns what all of them see, the same to all threads.
+// Fills in `rows` for the tile's rows and returns what all of them see, the same to all threads.
+// Rows past the last repeat it.
 template <int kThreads, int kRows>
-__device__ TileSees place_tokens(const AttendParams &p, const WorkItem &w, const Tile &tile, TokenSees *tokens) {
-  static_assert(kRows <= kThreads, "a thread a token");
+__device__ TileSees place_rows(const AttendParams &p, const WorkItem &w, const Tile &tile, RowSees *rows) {
+  static_assert(kRows <= kThreads, "a thread a row");
   __shared__ TileSees s_sees[kThreads / 64];
-  const uint32_t t0 = w.r.start + fastdiv(tile.row0, p.group);
-  const uint32_t count = w.r.start + fastdiv(tile.row0 + tile.rows - 1, p.group) + 1 - t0;  // at most kRows
-  if (threadIdx.x < kRows) tokens[threadIdx.x] = TokenSees{-1, 0};  // of no request: sees nothing
-  __syncthreads();
-  const uint32_t end = first_of(p, w.request + 1);
-  for (uint32_t b = w.r.row + threadIdx.x; b < end; b += kThreads) {
-    const uint32_t from = (uint32_t)min(max(p.starts[b], 0), (int32_t)p.tokens);
-    const uint32_t upto = (uint32_t)min(max(p.starts[b + 1], 0), (int32_t)p.tokens);
-    if (from >= t0 + count || upto <= t0) continue;
-    const int32_t len = max(p.lens[b], 0), prefix = p.prefix ? min(max(p.prefix[b], 0), len) : 0;
-    for (uint32_t t = max(from, t0); t < min(upto, t0 + count); ++t)
-      tokens[t - t0] = TokenSees{len - (int32_t)(upto - t), prefix};
+  const uint32_t row = tile.row0 + min((uint32_t)threadIdx.x, tile.rows - 1);
+  const int32_t token = w.r.start + (int32_t)fastdiv(row, p.group);
+  RowSees mine{-1, 0};  // of no request: sees nothing
+  // the group's request that has the token: the last that begins at or before it
+  uint32_t lo = w.r.row, hi = first_of(p, w.request + 1) - 1;
+  if (threadIdx.x < kRows) {
+    while (lo < hi) {
+      const uint32_t mid = lo + (hi - lo + 1) / 2;
+      if (p.starts[mid] <= token) lo = mid;
+      else hi = mid - 1;
+    }
+    const int32_t from = min(max(p.starts[lo], 0), (int32_t)p.tokens), upto = min(max(p.starts[lo + 1], 0), (int32_t)p.tokens);
+    if (token >= from && token < upto) {
+      const int32_t len = max(p.lens[lo], 0);
+      mine = RowSees{len - (upto - token), p.prefix ? min(max(p.prefix[lo], 0), len) : 0};
+    }
+    rows[threadIdx.x] = mine;
   }
-  __syncthreads();
   TileSees s{0x7FFFFFFF, -1, 0x7FFFFFFF};
-  if (threadIdx.x < count) {
-    const TokenSees mine = tokens[threadIdx.x];
-    s = TileSees{mine.pos, mine.pos, mine.prefix};
-  }
+  if (threadIdx.x < kRows) s = TileSees{mine.pos, mine.pos, mine.prefix};
 #pragma unroll
   for (int d = 32; d; d >>= 1) {
     s.first = min(s.first, __shfl_xor(s.first, d));

@@ -327,7 +327,7 @@ template <typename Q, int kPages, int kSteps, bool kMore>
 __global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
-  if (!find_item<few_waves(kSteps) * 64, kFewBlock>(p, index, w)) return note_cut<kFewRows>(p, index, head);
+  if (!find_item<few_waves(kSteps) * 64, kFewBlock, false>(p, index, w)) return note_cut<kFewRows>(p, index, head);
   for (;;) {
     const Tile tile = tile_of(p, w.r, w.tile);
     const KeyRange range = key_range<kFewBlock>(p, w.r, tile.first, tile.last);
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParam
     const Part part = part_of(p, w, blocks, index);
     if (!part.none) few_part<Q, kPages, kSteps, kMore>(p, w, tile, range, part, head);
     const uint64_t end = w.begin + blocks;
-    if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end))
+    if (end >= (index + 1) * w.share || end >= w.line || !next_item<false>(p, w, end))
       return note_cut<kFewRows>(p, index, head, w, tile, part, blocks);
     __syncthreads();  // the next tile's sums go where this one's are read
   }

@@ -59,8 +59,9 @@ constexpr float kSlack = 8.f;
 // kSteps: D <= 32 kSteps.  kPages: a PageKind.  kMore: 1 if scores are biased, 2 if they
 // are capped, and biased if there are slopes, 3 the same by a cap past kQuickCap (kernels of their
 // own: a branch in those of 2 made these spill up to 40 registers more, for caps of any size).  Pages
-// of blocks with powers have no kernels of 1: those of 3 serve biases without a cap as well.
-template <typename Q, int kPages, int kSteps, int kMore>
+// of blocks with powers, and groups, have no kernels of 1: those of 3 serve biases without a cap as
+// well.  kGroup: the launch's requests are groups (a branch made the others spill 5 to 8 registers).
+template <typename Q, int kPages, int kSteps, int kMore, bool kGroup>
 __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem &w, Tile tile,
                                           const KeyRange &range, const Part &part, uint32_t head) {
   constexpr int kManyWaves = many_waves(kSteps), kManyThreads = kManyWaves * 64, kManyRows = kManyWaves * 32;
@@ -86,12 +87,12 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   __shared__ uint64_t s_odd[2][kDim];
   __shared__ uint32_t s_any_odd[kManyWaves];
 
-  __shared__ TokenSees s_tokens[kManyRows];  // of a group's tile
+  __shared__ RowSees s_rows[kGroup ? kManyRows : 1];  // of a group's tile
   // Positions below it are seen by all rows of the tile.  What a group's rows see differs, and
   // w.r.prefix is its end there: no row sees more.
   int32_t sure = w.r.prefix;
-  if (p.grouped) {
-    const TileSees s = place_tokens<kManyThreads, kManyRows>(p, w, tile, s_tokens);
+  if constexpr (kGroup) {
+    const TileSees s = place_rows<kManyThreads, kManyRows>(p, w, tile, s_rows);
     tile.first = s.first;
     tile.last = s.last;
     sure = s.prefix;
@@ -110,10 +111,9 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   const uint32_t row = min(tile.row0 + (uint32_t)wave * 32 + m, tile.row0 + tile.rows - 1);
   const uint32_t token = fastdiv(row, p.group), gh = row - token * p.group.d;
   const int32_t base = w.r.len - w.r.added;
-  const uint32_t in_tile = token - fastdiv(tile.row0, p.group);
-  const int32_t pos = p.grouped ? s_tokens[in_tile].pos : base + (int32_t)token;
-  const int32_t first = p.grouped ? tile.first : base + (int32_t)fastdiv(wave_row, p.group);
-  const int32_t last = p.grouped ? tile.last : base + (int32_t)fastdiv(wave_end, p.group);
+  const int32_t pos = kGroup ? s_rows[kGroup ? wave * 32 + m : 0].pos : base + (int32_t)token;
+  const int32_t first = kGroup ? tile.first : base + (int32_t)fastdiv(wave_row, p.group);
+  const int32_t last = kGroup ? tile.last : base + (int32_t)fastdiv(wave_end, p.group);
   const uint32_t qhead = head * p.group.d + gh;
   const float scale = p.scale * (p.key_scale ? p.key_scale[head] : 1.f);
   // the running maximum is taken of the products as they are, so the factor has to be positive:
@@ -292,7 +292,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         if constexpr (large) {
-          s[i] = kMx && p.cap == 0.f ? s[i] * change.to_log2 : change.capped_exactly(s[i]);
+          s[i] = (kMx || kGroup) && p.cap == 0.f ? s[i] * change.to_log2 : change.capped_exactly(s[i]);
           __builtin_amdgcn_sched_barrier(0);  // one score's registers at a time
         } else {
           s[i] = change.quotient(s[i]);
@@ -416,7 +416,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       int32_t here = pos;
       asm("" : "+v"(here));  // what follows from it is worked out here, not kept in registers
       const int32_t oldest = (int32_t)max((int64_t)here - p.window + 1, (int64_t)0);  // the window's first key
-      const int32_t prefix = p.grouped ? s_tokens[in_tile].prefix : w.r.prefix;
+      const int32_t prefix = kGroup ? s_rows[kGroup ? wave * 32 + m : 0].prefix : w.r.prefix;
       sees = !any ? 0 : there & ((low_bits(here - j0 + 1) & ~low_bits(oldest - j0)) | low_bits(prefix - j0));
     }
     auto mask = [&](f32x16 &s, uint32_t seen) __attribute__((always_inline)) {
@@ -502,7 +502,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   const uint64_t t_out = (uint64_t)(w.r.start + token_out);
   const float vs = p.value_scale ? p.value_scale[head] : 1.f;
   const uint64_t row_carried = carried_row(p, t_out, head_out);
-  if (w.r.skip > 0 && part.from == 0) {  // the group's sums
+  if (!kGroup && w.r.skip > 0 && part.from == 0) {  // the group's sums
     Carried c;
     const float keep = take_carried(p, row_carried, best, c);
     sum = sum * keep + c.l * c.by;
@@ -517,7 +517,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
         for (int e = 0; e < 4; ++e) o[t][i * 4 + e] = o[t][i * 4 + e] * keep + more[e] * c.by;
       }
   }
-  const float norm = divided || p.grouped ? 1.f : sum != 0.f ? vs / sum : 0.f;
+  const float norm = divided || kGroup ? 1.f : sum != 0.f ? vs / sum : 0.f;
   const uint64_t slot = ((uint64_t)part.slot * p.kv_heads + head) * kManyRows + wave * 32 + m;
 #pragma unroll
   for (int t = 0; t < kSteps; ++t)
@@ -528,7 +528,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       const f32x4 y = {o[t][i * 4] * norm, o[t][i * 4 + 1] * norm, o[t][i * 4 + 2] * norm, o[t][i * 4 + 3] * norm};
       if (divided)
         *reinterpret_cast<f32x4 *>(p.parts + slot * p.D + d) = y;
-      else if (p.grouped)
+      else if (kGroup)
         *reinterpret_cast<f32x4 *>(p.carry + row_carried * p.D + d) = y;
       else
         *reinterpret_cast<u32x2 *>(p.out + t_out * p.out_stride + (uint64_t)head_out * p.D + d) =
@@ -539,7 +539,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
       float *ml = p.parts + (uint64_t)p.shares * 2 * p.kv_heads * kManyRows * p.D + slot * 2;
       ml[0] = best;
       ml[1] = sum;
-    } else if (p.grouped) {
+    } else if (kGroup) {
       float *sums = carried_sums(p, row_carried);
       sums[0] = best;
       sums[1] = sum;
@@ -551,19 +551,19 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
 
 // Workgroups a CU: three for D <= 64, in 168 registers (8 requests of 1000 tokens over 8000: 127
 // us; two workgroups, with room for more registers, 137), two for 96.
-template <typename Q, int kPages, int kSteps, int kMore>
+template <typename Q, int kPages, int kSteps, int kMore, bool kGroup>
 __global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps > 2 ? 2 : 3) void attend_many(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
-  if (!find_item<many_waves(kSteps) * 64, kManyBlock>(p, index, w)) return note_cut<many_rows(kSteps)>(p, index, head);
+  if (!find_item<many_waves(kSteps) * 64, kManyBlock, kGroup>(p, index, w)) return note_cut<many_rows(kSteps)>(p, index, head);
   for (;;) {
     const Tile tile = tile_of(p, w.r, w.tile);
     const KeyRange range = key_range<kManyBlock>(p, w.r, tile.first, tile.last);
     const uint32_t blocks = (uint32_t)max(range.count, 1);
     const Part part = part_of(p, w, blocks, index);
-    if (!part.none) many_part<Q, kPages, kSteps, kMore>(p, w, tile, range, part, head);
+    if (!part.none) many_part<Q, kPages, kSteps, kMore, kGroup>(p, w, tile, range, part, head);
     const uint64_t end = w.begin + blocks;
-    if (end >= (index + 1) * w.share || end >= w.line || !next_item(p, w, end))
+    if (end >= (index + 1) * w.share || end >= w.line || !next_item<kGroup>(p, w, end))
       return note_cut<many_rows(kSteps)>(p, index, head, w, tile, part, blocks);
     __syncthreads();
   }

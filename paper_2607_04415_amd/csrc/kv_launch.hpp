@@ -32,16 +32,16 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
     p.whole = f.whole;
     p.cuts = f.cuts;
   };
-  auto run_many = [&](const AttendForm &f) {
+  auto run_many = [&](const AttendForm &f, void (*kernel)(AttendParams)) {
     divide(f);
-    attend_many<Q, kPages, kSteps, kMore><<<f.shares * p.kv_heads, many_waves(kSteps) * 64, 0, s>>>(p);
+    kernel<<<f.shares * p.kv_heads, many_waves(kSteps) * 64, 0, s>>>(p);
     if (f.cuts)
       attend_join<Q, many_rows(kSteps)><<<dim3((f.shares - 1) * p.kv_heads, many_rows(kSteps) / 16), 256, 0, s>>>(p);
   };
   if (l.group.shares) {
     p.grouped = true;
     p.requests = l.groups;
-    run_many(l.group);
+    run_many(l.group, attend_many<Q, kPages, kSteps, kMore == 1 ? 3 : kMore, true>);
     p.grouped = false;
     p.requests = p.all_requests;
   }
@@ -50,7 +50,7 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
     attend_few<Q, kPages, kSteps, (kMore > 0)><<<l.few.shares * p.kv_heads, few_waves(kSteps) * 64, 0, s>>>(p);
     if (l.few.cuts) attend_join<Q, kFewRows><<<(l.few.shares - 1) * p.kv_heads, 256, 0, s>>>(p);
   }
-  if (l.many.shares) run_many(l.many);
+  if (l.many.shares) run_many(l.many, attend_many<Q, kPages, kSteps, kMore, false>);
   return hipGetLastError();
 }
 
