@@ -57,6 +57,7 @@ AttendForm divide(const gorio_kv_cache &c, const gorio_kv_attention &a, uint32_t
   f.upto = 0xFFFFFFFFu;
   f.least = least;
   f.whole = whole;
+  f.pad = 1;
   f.shares = (uint32_t)std::min<uint64_t>(std::max(all / c.heads, 1u), (tiles * blocks + least - 1) / least);
   f.cuts = f.shares > 1 && blocks > whole;
   return f;
@@ -100,10 +101,12 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   // Workgroups: as many as run at once, a CU each for few rows, which has 128 KB of loads under way
   // then (64 requests of 16384 tokens take 451 us, and 454 with twice as many workgroups); for many
   // rows see attend_many.
-  if (few) l.few = divide(c, a, kFewRows, kFewBlock, 8, 16, 256, many);
+  if (few) l.few = divide(c, a, kFewRows, kFewBlock, groups ? 4 : 8, 16, groups ? 512 : 256, many);
   if (many) l.many = divide(c, a, many_rows(steps), kManyBlock, 4, 8, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
   if (few && many) l.few.upto = l.many.from = kFewUpto;
   if (groups) {
+    l.few.pad = l.few.whole;
+    l.many.pad = l.many.whole;
     l.groups = groups;
     l.group = divide(c, a, many_rows(steps), kManyBlock, 4, 0, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
   }

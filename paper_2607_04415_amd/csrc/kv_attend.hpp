@@ -199,6 +199,7 @@ struct AttendParams {
   uint32_t from, upto;   // requests with this many rows a key head, from <= rows < upto
   uint32_t shares, least;  // workgroups of a key head, at most; key blocks of a share, at least
   uint32_t whole;          // key blocks of a tile that is not cut, at most
+  uint32_t pad;            // of a tile on the line, at least
   bool cuts;               // a tile may be cut
 };
 
@@ -333,7 +334,7 @@ __device__ __forceinline__ Tile tile_of(const AttendParams &p, const Request &r,
 template <int kBlock>
 __device__ __forceinline__ uint32_t blocks_of(const AttendParams &p, const Request &r, uint32_t tile) {
   const Tile t = tile_of(p, r, tile);
-  return (uint32_t)max(key_range<kBlock>(p, r, t.first, t.last).count, 1);
+  return max((uint32_t)max(key_range<kBlock>(p, r, t.first, t.last).count, 1), p.pad);
 }
 
 // Inclusive sum over the threads, in thread order.
@@ -483,6 +484,7 @@ struct Part {
 };
 
 __device__ __forceinline__ Part part_of(const AttendParams &p, const WorkItem &w, uint32_t blocks, uint32_t index) {
+  // blocks: the tile's own, without what it is padded by; a tile that may be cut is not padded
   const uint64_t begin = index * w.share, end = min(begin + w.share, w.line);
   Part a{0, blocks, index * 2 + (w.begin > begin ? 1 : 0), false, false};
   if (blocks <= p.whole) {
@@ -509,22 +511,32 @@ template <int kThreads, int kRows>
 __device__ TileSees place_rows(const AttendParams &p, const WorkItem &w, const Tile &tile, RowSees *rows) {
   static_assert(kRows <= kThreads, "a thread a row");
   __shared__ TileSees s_sees[kThreads / 64];
+  __shared__ int32_t s_starts[kThreads];
   const uint32_t row = tile.row0 + min((uint32_t)threadIdx.x, tile.rows - 1);
   const int32_t token = w.r.start + (int32_t)fastdiv(row, p.group);
   RowSees mine{-1, 0};  // of no request: sees nothing
-  // the group's request that has the token: the last that begins at or before it
-  uint32_t lo = w.r.row, hi = first_of(p, w.request + 1) - 1;
+  // the group's request that has the token: the last that begins at or before it, by a bisection
+  // in LDS of every so many-th request's start, and among those between in memory
+  const uint32_t count = first_of(p, w.request + 1) - w.r.row, step = (count + kThreads - 1) / kThreads;
+  if (threadIdx.x * step < count) s_starts[threadIdx.x] = p.starts[w.r.row + threadIdx.x * step];
+  __syncthreads();
   if (threadIdx.x < kRows) {
+    uint32_t lo = 0, hi = (count - 1) / step;
+    while (lo < hi) {
+      const uint32_t mid = (lo + hi + 1) / 2;
+      if (s_starts[mid] <= token) lo = mid;
+      else hi = mid - 1;
+    }
+    lo = w.r.row + lo * step;
+    hi = min(lo + step, w.r.row + count) - 1;
     while (lo < hi) {
       const uint32_t mid = lo + (hi - lo + 1) / 2;
       if (p.starts[mid] <= token) lo = mid;
       else hi = mid - 1;
     }
     const int32_t from = min(max(p.starts[lo], 0), (int32_t)p.tokens), upto = min(max(p.starts[lo + 1], 0), (int32_t)p.tokens);
-    if (token >= from && token < upto) {
-      const int32_t len = max(p.lens[lo], 0);
-      mine = RowSees{len - (upto - token), p.prefix ? min(max(p.prefix[lo], 0), len) : 0};
-    }
+    const int32_t len = max(p.lens[lo], 0), prefix = p.prefix ? min(max(p.prefix[lo], 0), len) : 0;
+    if (token >= from && token < upto) mine = RowSees{len - (upto - token), prefix};
     rows[threadIdx.x] = mine;
   }
   TileSees s{0x7FFFFFFF, -1, 0x7FFFFFFF};

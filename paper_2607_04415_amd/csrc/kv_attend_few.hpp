@@ -36,23 +36,49 @@ namespace gorio {
 
 // Waves of a workgroup: 64 requests of 16384 tokens take 235 us at D = 64 and 451 at 128 with
 // eight, 256 and 456 with four.  256 elements take the registers of twice as many.
-__host__ __device__ constexpr int few_waves(int steps) { return steps > 4 ? 4 : 8; }
+__host__ __device__ constexpr int few_waves(int steps, bool brief) { return steps > 4 || brief ? 4 : 8; }
 constexpr int kFewRows = 16;
 constexpr int kFewBlock = 32;  // keys
 
-// kSteps: 32-element steps of a head, D <= 32 kSteps.  kPages: a PageKind.
+// The powers of a row's blocks, of which there are `count`, up to kBlocks.
+template <int kBlocks, typename Powers>
+__device__ __forceinline__ Powers load_powers(const uint8_t *from, uint32_t count) {
+  uint32_t w[kBlocks / 4];
+  if (count == kBlocks) {
+    __builtin_memcpy(w, from, kBlocks);  // a load or two, of any alignment
+  } else {
+#pragma unroll
+    for (int i = 0; i < kBlocks / 4; ++i) w[i] = 0;
+#pragma unroll
+    for (int i = 0; i < kBlocks - 1; ++i)
+      if ((uint32_t)i < count) w[i / 4] |= (uint32_t)from[i] << (i % 4) * 8;
+  }
+  if constexpr (kBlocks == 8) return Powers{w[0], w[1]};
+  else return w[0];
+}
+
+// kSteps: 32-element steps of a head, D <= 32 kSteps (2, 4 or 8 with powers).  kPages: a PageKind.
 // kMore: scores are capped or biased.
-template <typename Q, int kPages, int kSteps, bool kMore>
+template <typename Q, int kPages, int kSteps, bool kMore, int kFewWaves>
 __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
                                          const KeyRange &range, const Part &part, uint32_t head) {
-  constexpr int kFewWaves = few_waves(kSteps), kFewThreads = kFewWaves * 64;
+  constexpr int kFewThreads = kFewWaves * 64;
   constexpr int kHalves = (kSteps + 3) / 4;  // 128 elements of a value
   constexpr int kDim = kHalves * 128;
   constexpr int kPad = kDim + 4;
   typedef PageOf<kPages> Page;
   typedef typename Page::Raw Raw;
   constexpr bool kMx = Page::kMx;
-  __shared__ uint64_t s_power[kMx ? kFewWaves : 1][2][2][kFewBlock];  // as s_row, the rows' powers
+  // Powers of a row's blocks, a byte each; the lanes that look a key up load them and hand them
+  // out a block later.
+  constexpr int kBlocks = kSteps > 4 ? 8 : 4;
+  typedef typename std::conditional<(kSteps > 4), u32x2, uint32_t>::type Powers;
+  __shared__ __align__(16) Powers s_power[kMx ? kFewWaves : 1][2][kFewBlock];  // keys, values
+  // Elements of a key in a lane, which need not be every fourth eight of them: with powers they
+  // follow one another, so that they are one load, or few, and their powers one or two.
+  constexpr int kWords = kPages == kPagesMx4 ? kSteps : kSteps * 2, kLoad = kWords < 4 ? kWords : 4;
+  typedef typename std::conditional<kLoad == 2, u32x2, u32x4>::type Load;
+  auto element = [](int s, int g) __attribute__((always_inline)) -> uint32_t { return kMx ? g * 8 * kSteps + s * 8 : s * 32 + g * 8; };
   __shared__ uint64_t s_row[kFewWaves][2][2][kFewBlock];  // wave, turn, keys or values
   __shared__ float s_o[kFewWaves][kFewRows][kPad];
   __shared__ float s_m[kFewWaves][kFewRows], s_l[kFewWaves][kFewRows];
@@ -74,7 +100,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     const uint16_t *row = p.q + (uint64_t)(w.r.start + token) * p.q_stride + (uint64_t)qhead * p.D;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-      const uint32_t d = s * 32 + g * 8;
+      const uint32_t d = element(s, g);
       q[s] = d < p.D ? *reinterpret_cast<const u32x4 *>(row + d) : u32x4{0, 0, 0, 0};
     }
   }
@@ -87,37 +113,50 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
 #pragma unroll
   for (int t = 0; t < kHalves * 8; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // Rows of block x into LDS, and its keys' bits: lanes 0..31 a key each.
+  // Rows of block x into LDS, and its keys' bits: lanes 0..31 a key each, with powers the others too.
   auto place_of = [&](int32_t x) __attribute__((always_inline)) {
-    return key_look(p, w, tile, (x < x_end) & (lane < kFewBlock), range.block(x) * kFewBlock + (lane & 31), range.end);
+    return key_look(p, w, tile, (x < x_end) & (kMx || lane < kFewBlock), range.block(x) * kFewBlock + (lane & 31), range.end);
   };
+  Powers powers{};  // of a key (lanes 0..31) or value (32..63) of the block whose rows were handed out last
   auto hand_out = [&](const KeyLook &k, int turn) __attribute__((always_inline)) -> uint32_t {
     const bool there = key_there(p, k);
+    const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
     if (lane < kFewBlock) {
-      const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
       s_row[wave][turn][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : 0;
       s_row[wave][turn][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : 0;
-      if constexpr (kMx) {
-        s_power[wave][turn][0][lane] = (uint64_t)(uintptr_t)p.key_powers + Page::powers(off);
-        s_power[wave][turn][1][lane] = (uint64_t)(uintptr_t)p.value_powers + Page::powers(off);
-      }
+    }
+    if constexpr (kMx) {
+      const uint8_t *from = (lane < kFewBlock ? p.key_powers : p.value_powers) + Page::powers(off);
+      if (!there) from = reinterpret_cast<const uint8_t *>(kv_zeros);
+      powers = load_powers<kBlocks, Powers>(from, p.D / kMxBlock);
     }
     wave_lds_order();
     return (uint32_t)__ballot(there);
   };
-  uint8_t kp[2][kMx ? 2 : 1][kMx ? kSteps : 1], vp[2][kMx ? kHalves : 1][kMx ? 8 : 1];  // powers
   auto load_keys = [&](Raw (&k)[2][kSteps], int turn) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint64_t row = s_row[wave][turn][0][i * 16 + m];
+      if constexpr (kMx) {
+        uint32_t words[kWords];
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const uint32_t d = s * 32 + g * 8;
-        const uint64_t at = row && d < p.D ? row + Page::bytes(d) : zeros;
-        k[i][s] = *reinterpret_cast<const Raw *>(at);
-        if constexpr (kMx) {
-          const uint64_t power = s_power[wave][turn][0][i * 16 + m] + s;
-          kp[turn][i][s] = *reinterpret_cast<const uint8_t *>(row && d < p.D ? power : zeros);
+        for (int u = 0; u < kWords / kLoad; ++u) {
+          const uint32_t d = element(u * kLoad * kSteps / kWords, g);
+          const Load some = *reinterpret_cast<const Load *>(row && d < p.D ? row + Page::bytes(d) : zeros);
+#pragma unroll
+          for (int c = 0; c < kLoad; ++c) words[u * kLoad + c] = some[c];
+        }
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          if constexpr (kPages == kPagesMx4) k[i][s] = words[s];
+          else if constexpr (kPages == kPagesMx8) k[i][s] = u32x2{words[2 * s], words[2 * s + 1]};
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const uint32_t d = element(s, g);
+          const uint64_t at = row && d < p.D ? row + Page::bytes(d) : zeros;
+          k[i][s] = *reinterpret_cast<const Raw *>(at);
         }
       }
     }
@@ -129,11 +168,21 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
       const uint64_t row = s_row[wave][turn][1][(i >> 2) * 16 + g * 4 + (i & 3)];
       const uint64_t at = row && d < p.D ? row + Page::bytes(d) : zeros;
       v[i] = *reinterpret_cast<const Raw *>(at);
-      if constexpr (kMx) {
-        const uint64_t power = s_power[wave][turn][1][(i >> 2) * 16 + g * 4 + (i & 3)] + d / kMxBlock;
-        vp[turn][half][i] = *reinterpret_cast<const uint8_t *>(row && d < p.D ? power : zeros);
-      }
     }
+  };
+  // What the powers of step s of a key, and of a value's half, multiply by, from LDS.
+  auto key_factor = [&](int i, int s) __attribute__((always_inline)) -> float {
+    if constexpr (!kMx) return 1.f;
+    const Powers all = s_power[kMx ? wave : 0][0][i * 16 + m];
+    const uint32_t block = element(s, g) / kMxBlock;
+    if constexpr (kSteps > 4) return power_of((block < 4 ? all.x : all.y) >> (block & 3) * 8 & 255);
+    else return power_of(all >> block * 8 & 255);
+  };
+  auto value_factor = [&](int i, int half) __attribute__((always_inline)) -> float {
+    if constexpr (!kMx) return 1.f;
+    const Powers all = s_power[kMx ? wave : 0][1][(i >> 2) * 16 + g * 4 + (i & 3)];
+    if constexpr (kSteps > 4) return power_of((half ? all.y : all.x) >> (m >> 2) * 8 & 255);
+    else return power_of(all >> (m >> 2) * 8 & 255);
   };
   // Block x, with the next one's keys and values on their way; the registers alternate.
   Raw k[2][2][kSteps], v[2][kHalves][8];
@@ -149,6 +198,10 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     constexpr int t0 = decltype(turn)::value, t1 = 1 - t0;
     const int32_t j0 = range.block(x) * kFewBlock;
     const uint32_t there_now = there[t0];
+    if constexpr (kMx) {
+      s_power[wave][lane >> 5][lane & 31] = powers;
+      wave_lds_order();
+    }
     there[t1] = hand_out(next, t1);
     next = place_of(x + 2 * kFewWaves);
     load(std::integral_constant<int, t1>{});
@@ -158,7 +211,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     for (int i = 0; i < 2; ++i) {
       s2[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) s2[i] = Q::mfma16(widened<Q>(k[t0][i][s], power_of(kMx ? kp[t0][kMx ? i : 0][kMx ? s : 0] : 127)), q[s], s2[i]);
+      for (int s = 0; s < kSteps; ++s) s2[i] = Q::mfma16(widened<Q>(k[t0][i][s], key_factor(i, s)), q[s], s2[i]);
     }
     float e[8];
 #pragma unroll
@@ -206,7 +259,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     for (int h = 0; h < kHalves; ++h) {
       u32x4 vw[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) vw[i] = widened<Q>(v[t0][h][i], power_of(kMx ? vp[t0][kMx ? h : 0][kMx ? i : 0] : 127));
+      for (int i = 0; i < 8; ++i) vw[i] = widened<Q>(v[t0][h][i], value_factor(i, h));
       // A weight of 0 keeps a value out of a row, unless the value is NaN or inf.  Such
       // values in a block that some rows see only in part go in apart from the others.
       bool odd = false;
@@ -323,18 +376,18 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   }
 }
 
-template <typename Q, int kPages, int kSteps, bool kMore>
-__global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParams p) {
+template <typename Q, int kPages, int kSteps, bool kMore, int kWaves>
+__global__ __launch_bounds__(kWaves * 64, kWaves == 4 && kSteps <= 4 ? 2 : 1) void attend_few(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
-  if (!find_item<few_waves(kSteps) * 64, kFewBlock, false>(p, index, w)) return note_cut<kFewRows>(p, index, head);
+  if (!find_item<kWaves * 64, kFewBlock, false>(p, index, w)) return note_cut<kFewRows>(p, index, head);
   for (;;) {
     const Tile tile = tile_of(p, w.r, w.tile);
     const KeyRange range = key_range<kFewBlock>(p, w.r, tile.first, tile.last);
     const uint32_t blocks = (uint32_t)max(range.count, 1);
     const Part part = part_of(p, w, blocks, index);
-    if (!part.none) few_part<Q, kPages, kSteps, kMore>(p, w, tile, range, part, head);
-    const uint64_t end = w.begin + blocks;
+    if (!part.none) few_part<Q, kPages, kSteps, kMore, kWaves>(p, w, tile, range, part, head);
+    const uint64_t end = w.begin + max(blocks, p.pad);
     if (end >= (index + 1) * w.share || end >= w.line || !next_item<false>(p, w, end))
       return note_cut<kFewRows>(p, index, head, w, tile, part, blocks);
     __syncthreads();  // the next tile's sums go where this one's are read
@@ -343,12 +396,12 @@ __global__ __launch_bounds__(few_waves(kSteps) * 64) void attend_few(AttendParam
 
 // Joins the parts of divided tiles, of a group's into what its rows carry: a workgroup a share and head, for the tile that begins in the
 // share and is cut at its end; 16 rows, 16 threads a row (64 rows a workgroup, four after the other:
-// 128 new tokens over 2000 took 54 us in all, now 41).  A row's parts are added one after the
-// other, and each waits for its loads.
+// 128 new tokens over 2000 took 54 us in all, now 41).  A row's parts are added in order, and those
+// of eight are loaded together.  kWide: heads of more than 128 elements.
 //   out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts i
 // Bound by the latency of two dependent loads, 4 us, and for many tiles by reading the parts
 // (750 cut tiles of 128 rows, 64 elements: 50 MB in 14 us).
-template <typename Q, int kRows>
+template <typename Q, int kRows, bool kWide>
 __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
   const uint32_t s0 = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - s0 * p.kv_heads;
   const Cut cut = cuts_of<kRows>(p)[blockIdx.x];
@@ -365,6 +418,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
 #pragma unroll
     for (int d = 8; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
     const float from = most == -INFINITY ? 0.f : most;
+    constexpr int kEights = kWide ? 2 : 1, kTogether = 8;
     f32x4 y[4];  // 8 elements, and 8 more of a head past 128
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -378,16 +432,25 @@ __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
         all = fmaf(ml[at + 1], by, all);
       }
       const uint32_t some = min(parts - i0, 16u);
-      for (uint32_t i = 0; i < some; ++i) {
-        const float one = __shfl(by, (int)i, 16);
-        const float *o = p.parts + slot(i0 + i) * p.D;
-        if (d0 < p.D) {
-          y[0] += *reinterpret_cast<const f32x4 *>(o + d0) * one;
-          y[1] += *reinterpret_cast<const f32x4 *>(o + d0 + 4) * one;
-        }
-        if (d1 < p.D) {
-          y[2] += *reinterpret_cast<const f32x4 *>(o + d1) * one;
-          y[3] += *reinterpret_cast<const f32x4 *>(o + d1 + 4) * one;
+      for (uint32_t i = 0; i < some; i += kTogether) {
+        f32x4 o[kTogether][2 * kEights];
+#pragma unroll
+        for (uint32_t u = 0; u < kTogether; ++u)
+#pragma unroll
+          for (int h = 0; h < kEights; ++h) {
+            const uint32_t d = d0 + h * 128;
+            o[u][2 * h] = o[u][2 * h + 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (i + u < some && d < p.D) {
+              const float *at = p.parts + slot(i0 + i + u) * p.D + d;
+              o[u][2 * h] = *reinterpret_cast<const f32x4 *>(at);
+              o[u][2 * h + 1] = *reinterpret_cast<const f32x4 *>(at + 4);
+            }
+          }
+#pragma unroll
+        for (uint32_t u = 0; u < kTogether; ++u) {
+          const float one = __shfl(by, (int)(i + u), 16);  // 0 past the last part
+#pragma unroll
+          for (int h = 0; h < 2 * kEights; ++h) y[h] += o[u][h] * one;
         }
       }
     }

@@ -562,7 +562,7 @@ __global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps >
     const uint32_t blocks = (uint32_t)max(range.count, 1);
     const Part part = part_of(p, w, blocks, index);
     if (!part.none) many_part<Q, kPages, kSteps, kMore, kGroup>(p, w, tile, range, part, head);
-    const uint64_t end = w.begin + blocks;
+    const uint64_t end = w.begin + max(blocks, p.pad);
     if (end >= (index + 1) * w.share || end >= w.line || !next_item<kGroup>(p, w, end))
       return note_cut<many_rows(kSteps)>(p, index, head, w, tile, part, blocks);
     __syncthreads();

@@ -9,7 +9,7 @@ namespace gorio {
 
 // One form's launch: AttendParams' fields for the division of its work.
 struct AttendForm {
-  uint32_t rows, from, upto, shares, least, whole;
+  uint32_t rows, from, upto, shares, least, whole, pad;
   bool cuts;  // a tile may be cut
 };
 
@@ -30,13 +30,14 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
     p.shares = f.shares;
     p.least = f.least;
     p.whole = f.whole;
+    p.pad = f.pad;
     p.cuts = f.cuts;
   };
   auto run_many = [&](const AttendForm &f, void (*kernel)(AttendParams)) {
     divide(f);
     kernel<<<f.shares * p.kv_heads, many_waves(kSteps) * 64, 0, s>>>(p);
     if (f.cuts)
-      attend_join<Q, many_rows(kSteps)><<<dim3((f.shares - 1) * p.kv_heads, many_rows(kSteps) / 16), 256, 0, s>>>(p);
+      attend_join<Q, many_rows(kSteps), (kSteps > 4)><<<dim3((f.shares - 1) * p.kv_heads, many_rows(kSteps) / 16), 256, 0, s>>>(p);
   };
   if (l.group.shares) {
     p.grouped = true;
@@ -47,8 +48,13 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
   }
   if (l.few.shares) {
     divide(l.few);
-    attend_few<Q, kPages, kSteps, (kMore > 0)><<<l.few.shares * p.kv_heads, few_waves(kSteps) * 64, 0, s>>>(p);
-    if (l.few.cuts) attend_join<Q, kFewRows><<<(l.few.shares - 1) * p.kv_heads, 256, 0, s>>>(p);
+    constexpr int kFew = PageOf<kPages>::kMx && kSteps == 3 ? 4 : kSteps;  // a key's lanes take equal numbers of eights
+    constexpr int kWaves = few_waves(kFew, false), kShort = few_waves(kFew, true);
+    if (l.group.shares)
+      attend_few<Q, kPages, kFew, (kMore > 0), kShort><<<l.few.shares * p.kv_heads, kShort * 64, 0, s>>>(p);
+    else
+      attend_few<Q, kPages, kFew, (kMore > 0), kWaves><<<l.few.shares * p.kv_heads, kWaves * 64, 0, s>>>(p);
+    if (l.few.cuts) attend_join<Q, kFewRows, (kSteps > 4)><<<(l.few.shares - 1) * p.kv_heads, 256, 0, s>>>(p);
   }
   if (l.many.shares) run_many(l.many, attend_many<Q, kPages, kSteps, kMore, false>);
   return hipGetLastError();
