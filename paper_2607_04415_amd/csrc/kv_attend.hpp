@@ -113,6 +113,13 @@ __device__ __forceinline__ u32x4 widened(uint32_t r, float by) {
 // A power's byte as such a factor.
 __device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// Memory by its address.  Without the address space it would be read as what may be LDS, and every
+// wait for LDS would wait for the loads that are on their way.
+template <typename T>
+__device__ __forceinline__ T load_at(uint64_t address) {
+  return *(const __attribute__((address_space(1))) T *)(uintptr_t)address;
+}
+
 // LDS by its 32-bit address: what is added to one as a constant goes into the instruction.
 typedef __attribute__((address_space(3))) uint8_t LdsBytes;
 template <typename T>

@@ -40,18 +40,20 @@ __host__ __device__ constexpr int few_waves(int steps, bool brief) { return step
 constexpr int kFewRows = 16;
 constexpr int kFewBlock = 32;  // keys
 
-// The powers of a row's blocks, of which there are `count`, up to kBlocks.
-template <int kBlocks, typename Powers>
-__device__ __forceinline__ Powers load_powers(const uint8_t *from, uint32_t count) {
+// The powers of a row's blocks, of which there are `count`, up to kBlocks, or (kAll) as many.
+template <int kBlocks, typename Powers, bool kAll>
+__device__ __forceinline__ Powers load_powers(uint64_t from, uint32_t count) {
+  typedef uint32_t Anywhere __attribute__((aligned(1)));  // a load of any alignment
   uint32_t w[kBlocks / 4];
-  if (count == kBlocks) {
-    __builtin_memcpy(w, from, kBlocks);  // a load or two, of any alignment
-  } else {
+  if constexpr (kAll) {
+#pragma unroll
+    for (int i = 0; i < kBlocks / 4; ++i) w[i] = load_at<Anywhere>(from + i * 4);
+  } else {  // the last one again for those past it
 #pragma unroll
     for (int i = 0; i < kBlocks / 4; ++i) w[i] = 0;
 #pragma unroll
-    for (int i = 0; i < kBlocks - 1; ++i)
-      if ((uint32_t)i < count) w[i / 4] |= (uint32_t)from[i] << (i % 4) * 8;
+    for (int i = 0; i < kBlocks; ++i)
+      w[i / 4] |= (uint32_t)load_at<uint8_t>(from + min((uint32_t)i, count - 1)) << (i % 4) * 8;
   }
   if constexpr (kBlocks == 8) return Powers{w[0], w[1]};
   else return w[0];
@@ -118,31 +120,32 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     return key_look(p, w, tile, (x < x_end) & (kMx || lane < kFewBlock), range.block(x) * kFewBlock + (lane & 31), range.end);
   };
   Powers powers{};  // of a key (lanes 0..31) or value (32..63) of the block whose rows were handed out last
-  auto hand_out = [&](const KeyLook &k, int turn) __attribute__((always_inline)) -> uint32_t {
+  auto hand_out = [&](const KeyLook &k, int turn, auto whole_rows) __attribute__((always_inline)) -> uint32_t {
     const bool there = key_there(p, k);
     const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
     if (lane < kFewBlock) {
-      s_row[wave][turn][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : 0;
-      s_row[wave][turn][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : 0;
+      s_row[wave][turn][0][lane] = there ? (uint64_t)(uintptr_t)p.keys + off : zeros;
+      s_row[wave][turn][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : zeros;
     }
     if constexpr (kMx) {
-      const uint8_t *from = (lane < kFewBlock ? p.key_powers : p.value_powers) + Page::powers(off);
-      if (!there) from = reinterpret_cast<const uint8_t *>(kv_zeros);
-      powers = load_powers<kBlocks, Powers>(from, p.D / kMxBlock);
+      const uint64_t from = there ? (uint64_t)(uintptr_t)(lane < kFewBlock ? p.key_powers : p.value_powers) + Page::powers(off)
+                                  : zeros;
+      powers = load_powers<kBlocks, Powers, decltype(whole_rows)::value>(from, p.D / kMxBlock);
     }
     wave_lds_order();
     return (uint32_t)__ballot(there);
   };
-  auto load_keys = [&](Raw (&k)[2][kSteps], int turn) __attribute__((always_inline)) {
+  auto load_keys = [&](Raw (&k)[2][kSteps], int turn, auto whole_rows) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const uint64_t row = s_row[wave][turn][0][i * 16 + m];
+      uint64_t row = s_row[wave][turn][0][i * 16 + m];
+      asm("" : "+v"(row));  // read by all lanes, also by those whose elements end before: no branch
       if constexpr (kMx) {
         uint32_t words[kWords];
 #pragma unroll
         for (int u = 0; u < kWords / kLoad; ++u) {
           const uint32_t d = element(u * kLoad * kSteps / kWords, g);
-          const Load some = *reinterpret_cast<const Load *>(row && d < p.D ? row + Page::bytes(d) : zeros);
+          const Load some = load_at<Load>(decltype(whole_rows)::value || d < p.D ? row + Page::bytes(d) : zeros);
 #pragma unroll
           for (int c = 0; c < kLoad; ++c) words[u * kLoad + c] = some[c];
         }
@@ -155,19 +158,18 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
           const uint32_t d = element(s, g);
-          const uint64_t at = row && d < p.D ? row + Page::bytes(d) : zeros;
-          k[i][s] = *reinterpret_cast<const Raw *>(at);
+          k[i][s] = load_at<Raw>(decltype(whole_rows)::value || d < p.D ? row + Page::bytes(d) : zeros);
         }
       }
     }
   };
-  auto load_values = [&](Raw (&v)[8], int half, int turn) __attribute__((always_inline)) {
+  auto load_values = [&](Raw (&v)[8], int half, int turn, auto whole_rows) __attribute__((always_inline)) {
     const uint32_t d = half * 128 + m * 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint64_t row = s_row[wave][turn][1][(i >> 2) * 16 + g * 4 + (i & 3)];
-      const uint64_t at = row && d < p.D ? row + Page::bytes(d) : zeros;
-      v[i] = *reinterpret_cast<const Raw *>(at);
+      uint64_t row = s_row[wave][turn][1][(i >> 2) * 16 + g * 4 + (i & 3)];
+      asm("" : "+v"(row));
+      v[i] = load_at<Raw>(decltype(whole_rows)::value || d < p.D ? row + Page::bytes(d) : zeros);
     }
   };
   // What the powers of step s of a key, and of a value's half, multiply by, from LDS.
@@ -188,13 +190,13 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   Raw k[2][2][kSteps], v[2][kHalves][8];
   uint32_t there[2];
   KeyLook next;
-  auto load = [&](auto turn) __attribute__((always_inline)) {
+  auto load = [&](auto turn, auto whole_rows) __attribute__((always_inline)) {
     constexpr int t = decltype(turn)::value;
-    load_keys(k[t], t);
+    load_keys(k[t], t, whole_rows);
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h) load_values(v[t][h], h, t);
+    for (int h = 0; h < kHalves; ++h) load_values(v[t][h], h, t, whole_rows);
   };
-  auto step = [&](int32_t x, auto turn) __attribute__((always_inline)) {
+  auto step = [&](int32_t x, auto turn, auto whole_rows) __attribute__((always_inline)) {
     constexpr int t0 = decltype(turn)::value, t1 = 1 - t0;
     const int32_t j0 = range.block(x) * kFewBlock;
     const uint32_t there_now = there[t0];
@@ -202,9 +204,9 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
       s_power[wave][lane >> 5][lane & 31] = powers;
       wave_lds_order();
     }
-    there[t1] = hand_out(next, t1);
+    there[t1] = hand_out(next, t1, whole_rows);
     next = place_of(x + 2 * kFewWaves);
-    load(std::integral_constant<int, t1>{});
+    load(std::integral_constant<int, t1>{}, whole_rows);
 
     f32x4 s2[2];
 #pragma unroll
@@ -270,36 +272,49 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
           for (int c = 0; c < 4; ++c) odd |= any_not_finite<Q>(vw[i][c]);
         odd = __any(odd);
       }
+      auto products = [&](auto test) __attribute__((always_inline)) {
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const uint32_t sel = t & 1 ? 0x07060302u : 0x05040100u;
-        u32x4 a;
+        for (int t = 0; t < 8; ++t) {
+          const uint32_t sel = t & 1 ? 0x07060302u : 0x05040100u;
+          u32x4 a;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(vw[2 * i + 1][t >> 1], vw[2 * i][t >> 1], sel);
-        if (__builtin_expect(odd, 0)) {
-          u32x4 seen;  // 1 where the row sees the key
+          for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(vw[2 * i + 1][t >> 1], vw[2 * i][t >> 1], sel);
+          if constexpr (decltype(test)::value) {
+            if (__builtin_expect(odd, 0)) {
+              u32x4 seen;  // 1 where the row sees the key
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int at = (i >> 1) * 16 + (i & 1) * 2;
-            seen[i] = Q::pack((float)(sees >> at & 1u), (float)(sees >> (at + 1) & 1u));
+              for (int i = 0; i < 4; ++i) {
+                const int at = (i >> 1) * 16 + (i & 1) * 2;
+                seen[i] = Q::pack((float)(sees >> at & 1u), (float)(sees >> (at + 1) & 1u));
+              }
+              o[h * 8 + t] += not_finite_part<Q>(a, seen);
+              a = finite_only<Q>(a);
+            }
           }
-          o[h * 8 + t] += not_finite_part<Q>(a, seen);
-          a = finite_only<Q>(a);
+          o[h * 8 + t] = Q::mfma16(a, weights, o[h * 8 + t]);
         }
-        o[h * 8 + t] = Q::mfma16(a, weights, o[h * 8 + t]);
-      }
+      };
+      // One test is better than eight, but 16-bit pages' registers do not hold the products twice.
+      if (kMx && __builtin_expect(!odd, 1)) products(std::false_type{});
+      else products(std::true_type{});
     }
   };
-  int32_t x = (int32_t)part.from + wave;
-  there[0] = hand_out(place_of(x), 0);
-  next = place_of(x + kFewWaves);
-  load(std::integral_constant<int, 0>{});
-  while (x < x_end) {
-    step(x, std::integral_constant<int, 0>{});
-    if ((x += kFewWaves) >= x_end) break;
-    step(x, std::integral_constant<int, 1>{});
-    x += kFewWaves;
-  }
+  auto steps = [&](auto whole_rows) __attribute__((always_inline)) {
+    int32_t x = (int32_t)part.from + wave;
+    there[0] = hand_out(place_of(x), 0, whole_rows);
+    next = place_of(x + kFewWaves);
+    load(std::integral_constant<int, 0>{}, whole_rows);
+    while (x < x_end) {
+      step(x, std::integral_constant<int, 0>{}, whole_rows);
+      if ((x += kFewWaves) >= x_end) break;
+      step(x, std::integral_constant<int, 1>{}, whole_rows);
+      x += kFewWaves;
+    }
+  };
+  // A loop of its own where lanes have no elements past D: tests among the loads would make the
+  // compiler wait for all of them.
+  if (kMx && p.D == kSteps * 32 && p.D == kHalves * 128) steps(std::true_type{});
+  else steps(std::false_type{});
 
   // the waves' results, joined
   sum = xor16(xor32(sum, sum_of), sum_of);
