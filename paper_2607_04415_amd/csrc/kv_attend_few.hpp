@@ -119,6 +119,12 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   auto place_of = [&](int32_t x) __attribute__((always_inline)) {
     return key_look(p, w, tile, (x < x_end) & (kMx || lane < kFewBlock), range.block(x) * kFewBlock + (lane & 31), range.end);
   };
+  uint64_t all_powers = 0;  // worked out once: a choice between two arguments would pass through memory
+  if constexpr (kMx) {
+    const uint64_t of_keys = (uint64_t)(uintptr_t)p.key_powers, of_values = (uint64_t)(uintptr_t)p.value_powers;
+    all_powers = lane < kFewBlock ? of_keys : of_values;
+    asm("" : "+v"(all_powers));
+  }
   Powers powers{};  // of a key (lanes 0..31) or value (32..63) of the block whose rows were handed out last
   auto hand_out = [&](const KeyLook &k, int turn, auto whole_rows) __attribute__((always_inline)) -> uint32_t {
     const bool there = key_there(p, k);
@@ -128,8 +134,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
       s_row[wave][turn][1][lane] = there ? (uint64_t)(uintptr_t)p.values + off : zeros;
     }
     if constexpr (kMx) {
-      const uint64_t from = there ? (uint64_t)(uintptr_t)(lane < kFewBlock ? p.key_powers : p.value_powers) + Page::powers(off)
-                                  : zeros;
+      const uint64_t from = there ? all_powers + Page::powers(off) : zeros;
       powers = load_powers<kBlocks, Powers, decltype(whole_rows)::value>(from, p.D / kMxBlock);
     }
     wave_lds_order();

@@ -186,14 +186,14 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
     const uint64_t at = whole || d < p.D ? row + Page::bytes(d) : zeros;
     if constexpr (kMx) {
       const uint64_t one = whole || d < p.D ? power + d / kMxBlock : zeros;
-      powers[kv][i] = *reinterpret_cast<const uint8_t *>(one);
+      powers[kv][i] = load_at<uint8_t>(one);
     }
     if constexpr (kDirect) {
       typedef __attribute__((address_space(1))) const uint32_t global_u32;
       __builtin_amdgcn_global_load_lds((global_u32 *)at, (LdsBytes *)(uintptr_t)(lds + to + (i * kManyWaves + wave) * 1024),
                                        16, 0, 0);
     } else {
-      stage[kv][i] = *reinterpret_cast<const Raw *>(at);
+      stage[kv][i] = load_at<Raw>(at);
     }
   };
   auto load = [&](int32_t x, int kv, uint32_t to) __attribute__((always_inline)) {
