@@ -69,9 +69,17 @@ uint64_t carry_bytes(const gorio_kv_cache &c, const gorio_kv_attention &a) {
 }
 
 // The groups that a call computes the shared positions of.  A window without a prefix hides most
-// of what a long one shares, so such calls read it for each request.
-uint32_t groups_of(const gorio_kv_attention &a, const gorio_kv_sharing *sharing) {
-  return sharing && !(a.window && !a.prefix) ? sharing->groups : 0;
+// of what a long one shares, so such calls read it for each request.  So do calls whose tables have
+// no room for enough: a group's own launches cost 20 to 30 us, which the elements not read have to
+// be worth.  Of the tables' room, in elements of keys and values: 8 requests of 16-bit pages with
+// 8 key heads, 8192 shared positions (134M), take 36 us each for itself and 43 by groups, 16384
+// (268M) 54 and 49; 32 requests of 4-bit pages over 2048 (151M) 30 and 41, over 8192 (550M) 65 and
+// 47; 128 requests of 8 new tokens and one key head over 8192 (275M) 122 and 91.
+constexpr uint64_t kWorthSharing = 200'000'000;
+uint32_t groups_of(const gorio_kv_cache &c, const gorio_kv_attention &a, const gorio_kv_sharing *sharing) {
+  const uint64_t positions = (uint64_t)a.width * c.page_tokens * a.requests;  // below 2^63
+  const bool worth = positions / 64 * (2 * c.heads * c.D) >= kWorthSharing / 64;
+  return sharing && worth && !(a.window && !a.prefix) ? sharing->groups : 0;
 }
 
 // The forms that a call needs, and its workspace, which they use in turn.
@@ -88,7 +96,7 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   const uint64_t others = (a.requests - 1) * most;
   const uint64_t fewest = a.tokens > others ? std::min(a.tokens - others, most) : 1;
   const bool few = fewest * group < kFewUpto, many = most * group >= kFewUpto;
-  const int steps = steps_of(c.D);
+  const int steps = steps_of(c.D, l.pages);
   // The least share and the largest tile that is not cut, in blocks.  Few rows: 8 blocks are one
   // a wave; 8 requests of 250 tokens take 13 us, with shares of 16 blocks 19, of 32 31 us.  Tiles
   // of up to 16 are not cut: 8 requests of 500 tokens take 16 us, cut from 8 on 19; one of 1000
@@ -102,13 +110,16 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   // then (64 requests of 16384 tokens take 451 us, and 454 with twice as many workgroups); for many
   // rows see attend_many.
   if (few) l.few = divide(c, a, kFewRows, kFewBlock, groups ? 4 : 8, 16, groups ? 512 : 256, many);
-  if (many) l.many = divide(c, a, many_rows(steps), kManyBlock, 4, 8, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
+  auto rows = [&](bool brief) { return (uint32_t)many_waves(steps, brief) * 32; };
+  auto all = [&](bool brief) { return steps == 2 ? 768u : steps == 3 || (steps == 4 && brief) ? 512u : 256u; };
+  const bool brief = groups && brief_many(l.pages);
+  if (many) l.many = divide(c, a, rows(brief), kManyBlock, 4, 8, all(brief), false);
   if (few && many) l.few.upto = l.many.from = kFewUpto;
   if (groups) {
     l.few.pad = l.few.whole;
     l.many.pad = l.many.whole;
     l.groups = groups;
-    l.group = divide(c, a, many_rows(steps), kManyBlock, 4, 0, steps == 2 ? 768 : steps == 3 ? 512 : 256, false);
+    l.group = divide(c, a, rows(false), kManyBlock, 4, 0, all(false), false);
   }
   auto room = [&](const AttendForm &f) -> uint64_t {  // of a share and key head: two parts, and which tile is cut
     return f.cuts ? (uint64_t)f.shares * c.heads * (2 * (c.D + 2) * sizeof(float) * f.rows + sizeof(Cut)) : 0;
@@ -137,7 +148,7 @@ gorio_status workspace_of(const gorio_kv_cache *cache, const gorio_kv_attention 
   if (st != GORIO_OK) return st;
   if (!bytes) return fail(GORIO_EINVAL, "bytes is NULL");
   *bytes = 0;
-  if (at.tokens && at.requests) (void)forms_of(c, at, groups_of(at, sharing), bytes);
+  if (at.tokens && at.requests) (void)forms_of(c, at, groups_of(c, at, sharing), bytes);
   return GORIO_OK;
 }
 
@@ -150,7 +161,7 @@ gorio_status attend(const gorio_kv_cache *cache, const gorio_kv_attention *a, co
   st = check_sharing(at, sharing);
   if (st != GORIO_OK) return st;
   if (at.tokens == 0 || at.requests == 0) return GORIO_OK;
-  const uint32_t groups = groups_of(at, sharing);
+  const uint32_t groups = groups_of(c, at, sharing);
   KvDevice dev;
   st = dev.use({{"q", at.q, 16, false},
                 {"out", at.out, 16, false},

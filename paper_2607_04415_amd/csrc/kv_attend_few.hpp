@@ -43,14 +43,15 @@ constexpr int kFewBlock = 32;  // keys
 // The powers of a row's blocks, of which there are `count`, up to kBlocks, or (kAll) as many.
 template <int kBlocks, typename Powers, bool kAll>
 __device__ __forceinline__ Powers load_powers(uint64_t from, uint32_t count) {
-  typedef uint32_t Anywhere __attribute__((aligned(1)));  // a load of any alignment
-  uint32_t w[kBlocks / 4];
-  if constexpr (kAll) {
+  typedef uint32_t Four __attribute__((aligned(1)));  // a load of any alignment
+  typedef uint16_t Two __attribute__((aligned(1)));
+  uint32_t w[(kBlocks + 3) / 4] = {};
+  if constexpr (kAll && kBlocks == 2) {
+    w[0] = load_at<Two>(from);
+  } else if constexpr (kAll) {
 #pragma unroll
-    for (int i = 0; i < kBlocks / 4; ++i) w[i] = load_at<Anywhere>(from + i * 4);
+    for (int i = 0; i < kBlocks / 4; ++i) w[i] = load_at<Four>(from + i * 4);
   } else {  // the last one again for those past it
-#pragma unroll
-    for (int i = 0; i < kBlocks / 4; ++i) w[i] = 0;
 #pragma unroll
     for (int i = 0; i < kBlocks; ++i)
       w[i / 4] |= (uint32_t)load_at<uint8_t>(from + min((uint32_t)i, count - 1)) << (i % 4) * 8;
@@ -65,15 +66,18 @@ template <typename Q, int kPages, int kSteps, bool kMore, int kFewWaves>
 __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
                                          const KeyRange &range, const Part &part, uint32_t head) {
   constexpr int kFewThreads = kFewWaves * 64;
-  constexpr int kHalves = (kSteps + 3) / 4;  // 128 elements of a value
-  constexpr int kDim = kHalves * 128;
-  constexpr int kPad = kDim + 4;
   typedef PageOf<kPages> Page;
   typedef typename Page::Raw Raw;
   constexpr bool kMx = Page::kMx;
+  constexpr int kHalves = (kSteps + 3) / 4;  // 128 elements of a value
+  // Elements of a value in a lane, and products.  (16-bit pages of 64 elements are read as if they had
+  // 128, which costs them nothing while HBM is the bound.)
+  constexpr int kPer = kMx && kSteps == 2 ? 4 : 8;
+  constexpr int kDim = kHalves * 128;
+  constexpr int kPad = kDim + 4;
   // Powers of a row's blocks, a byte each; the lanes that look a key up load them and hand them
   // out a block later.
-  constexpr int kBlocks = kSteps > 4 ? 8 : 4;
+  constexpr int kBlocks = kSteps;
   typedef typename std::conditional<(kSteps > 4), u32x2, uint32_t>::type Powers;
   __shared__ __align__(16) Powers s_power[kMx ? kFewWaves : 1][2][kFewBlock];  // keys, values
   // Elements of a key in a lane, which need not be every fourth eight of them: with powers they
@@ -111,9 +115,9 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   const ScoreChange change(scale, p.cap, kMore && p.slopes ? p.slopes[qhead] : 0.f);
 
   float best = -INFINITY, sum = 0.f;
-  f32x4 o[kHalves * 8];
+  f32x4 o[kHalves * kPer];
 #pragma unroll
-  for (int t = 0; t < kHalves * 8; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < kHalves * kPer; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   // Rows of block x into LDS, and its keys' bits: lanes 0..31 a key each, with powers the others too.
   auto place_of = [&](int32_t x) __attribute__((always_inline)) {
@@ -168,13 +172,15 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
       }
     }
   };
-  auto load_values = [&](Raw (&v)[8], int half, int turn, auto whole_rows) __attribute__((always_inline)) {
-    const uint32_t d = half * 128 + m * 8;
+  typedef typename std::conditional<kPer == 8, Raw, typename std::conditional<kPages == kPagesMx4, uint16_t, uint32_t>::type>::type
+      RawValue;
+  auto load_values = [&](RawValue (&v)[8], int half, int turn, auto whole_rows) __attribute__((always_inline)) {
+    const uint32_t d = half * 128 + m * kPer;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       uint64_t row = s_row[wave][turn][1][(i >> 2) * 16 + g * 4 + (i & 3)];
       asm("" : "+v"(row));
-      v[i] = load_at<Raw>(decltype(whole_rows)::value || d < p.D ? row + Page::bytes(d) : zeros);
+      v[i] = load_at<RawValue>(decltype(whole_rows)::value || d < p.D ? row + Page::bytes(d) : zeros);
     }
   };
   // What the powers of step s of a key, and of a value's half, multiply by, from LDS.
@@ -188,11 +194,13 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   auto value_factor = [&](int i, int half) __attribute__((always_inline)) -> float {
     if constexpr (!kMx) return 1.f;
     const Powers all = s_power[kMx ? wave : 0][1][(i >> 2) * 16 + g * 4 + (i & 3)];
-    if constexpr (kSteps > 4) return power_of((half ? all.y : all.x) >> (m >> 2) * 8 & 255);
-    else return power_of(all >> (m >> 2) * 8 & 255);
+    const uint32_t block = m * kPer / kMxBlock;
+    if constexpr (kSteps > 4) return power_of((half ? all.y : all.x) >> block * 8 & 255);
+    else return power_of(all >> block * 8 & 255);
   };
   // Block x, with the next one's keys and values on their way; the registers alternate.
-  Raw k[2][2][kSteps], v[2][kHalves][8];
+  Raw k[2][2][kSteps];
+  RawValue v[2][kHalves][8];
   uint32_t there[2];
   KeyLook next;
   auto load = [&](auto turn, auto whole_rows) __attribute__((always_inline)) {
@@ -251,7 +259,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
       best = to;
       sum *= keep;
 #pragma unroll
-      for (int t = 0; t < kHalves * 8; ++t) o[t] *= keep;
+      for (int t = 0; t < kHalves * kPer; ++t) o[t] *= keep;
     }
     const float base = best == -INFINITY ? 0.f : best;
     float part = 0.f;
@@ -264,9 +272,12 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     const u32x4 weights = {Q::pack(e[0], e[1]), Q::pack(e[2], e[3]), Q::pack(e[4], e[5]), Q::pack(e[6], e[7])};
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
-      u32x4 vw[8];
+      typename std::conditional<kPer == 8, u32x4, u32x2>::type vw[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) vw[i] = widened<Q>(v[t0][h][i], value_factor(i, h));
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (kPer == 8) vw[i] = widened<Q>(v[t0][h][i], value_factor(i, h));
+        else vw[i] = widened_half<Q>(v[t0][h][i], value_factor(i, h));
+      }
       // A weight of 0 keeps a value out of a row, unless the value is NaN or inf.  Such
       // values in a block that some rows see only in part go in apart from the others.
       bool odd = false;
@@ -274,12 +285,12 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) odd |= any_not_finite<Q>(vw[i][c]);
+          for (int c = 0; c < kPer / 2; ++c) odd |= any_not_finite<Q>(vw[i][c]);
         odd = __any(odd);
       }
       auto products = [&](auto test) __attribute__((always_inline)) {
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
+        for (int t = 0; t < kPer; ++t) {
           const uint32_t sel = t & 1 ? 0x07060302u : 0x05040100u;
           u32x4 a;
 #pragma unroll
@@ -292,11 +303,11 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
                 const int at = (i >> 1) * 16 + (i & 1) * 2;
                 seen[i] = Q::pack((float)(sees >> at & 1u), (float)(sees >> (at + 1) & 1u));
               }
-              o[h * 8 + t] += not_finite_part<Q>(a, seen);
+              o[h * kPer + t] += not_finite_part<Q>(a, seen);
               a = finite_only<Q>(a);
             }
           }
-          o[h * 8 + t] = Q::mfma16(a, weights, o[h * 8 + t]);
+          o[h * kPer + t] = Q::mfma16(a, weights, o[h * kPer + t]);
         }
       };
       // One test is better than eight, but 16-bit pages' registers do not hold the products twice.
@@ -318,7 +329,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   };
   // A loop of its own where lanes have no elements past D: tests among the loads would make the
   // compiler wait for all of them.
-  if (kMx && p.D == kSteps * 32 && p.D == kHalves * 128) steps(std::true_type{});
+  if (kMx && p.D == kSteps * 32) steps(std::true_type{});
   else steps(std::false_type{});
 
   // the waves' results, joined
@@ -328,11 +339,11 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   for (int h = 0; h < kHalves; ++h)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      float *to = &s_o[wave][m][h * 128 + (g * 4 + r) * 8];
+      float *to = &s_o[wave][m][h * 128 + (g * 4 + r) * kPer];
 #pragma unroll
-      for (int t = 0; t < 8; t += 4)
+      for (int t = 0; t < kPer; t += 4)
         *reinterpret_cast<f32x4 *>(to + t) =
-            f32x4{o[h * 8 + t][r], o[h * 8 + t + 1][r], o[h * 8 + t + 2][r], o[h * 8 + t + 3][r]};
+            f32x4{o[h * kPer + t][r], o[h * kPer + t + 1][r], o[h * kPer + t + 2][r], o[h * kPer + t + 3][r]};
     }
   __syncthreads();
   constexpr int kRowThreads = kFewThreads / kFewRows, kOwn = 128 / kRowThreads;  // elements of each 128

@@ -48,8 +48,9 @@ namespace gorio {
 // 2000 took 43 us with four, 51 with eight).  Four for smaller heads: at D = 64 three workgroups
 // fit a CU, and 33 requests of 1000 tokens take 207 us, with eight waves 232.  Four for larger
 // ones, whose blocks fill LDS.
-__host__ __device__ constexpr int many_waves(int steps) { return steps == 4 ? 8 : 4; }
-__host__ __device__ constexpr int many_rows(int steps) { return many_waves(steps) * 32; }
+// brief: of requests whose keys are mostly their group's, few of their own are left, and two
+// workgroups of four waves wait for them together.
+__host__ __device__ constexpr int many_waves(int steps, bool brief) { return steps == 4 && !brief ? 8 : 4; }
 constexpr int kManyBlock = 64;  // keys
 
 // A maximum is kept until a score passes it by 2^8 (weights stay far inside
@@ -61,17 +62,17 @@ constexpr float kSlack = 8.f;
 // own: a branch in those of 2 made these spill up to 40 registers more, for caps of any size).  Pages
 // of blocks with powers, and groups, have no kernels of 1: those of 3 serve biases without a cap as
 // well.  kGroup: the launch's requests are groups (a branch made the others spill 5 to 8 registers).
-template <typename Q, int kPages, int kSteps, int kMore, bool kGroup>
+template <typename Q, int kPages, int kSteps, int kMore, bool kGroup, int kManyWaves>
 __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem &w, Tile tile,
                                           const KeyRange &range, const Part &part, uint32_t head) {
-  constexpr int kManyWaves = many_waves(kSteps), kManyThreads = kManyWaves * 64, kManyRows = kManyWaves * 32;
+  constexpr int kManyThreads = kManyWaves * 64, kManyRows = kManyWaves * 32;
   constexpr int kDim = kSteps * 32, kChunks = kDim / 8;                              // 16-byte pieces of a row
   constexpr int kPasses = kManyBlock * kChunks / kManyThreads;                       // pieces a thread
   static_assert(kPasses * kManyThreads == kManyBlock * kChunks, "pieces divide");
   constexpr bool kTurned = (kChunks & (kChunks - 1)) == 0, kDirect = kTurned && kPages == kPages16;  // see `turned`
   constexpr int kKeyRow = kTurned ? kDim : kDim + 8;                                 // elements
-  constexpr int kValueRow = kDim;
-  static_assert(kTurned || (kDim * 2) % 256 == 192, "rows of values fall on different banks");
+  constexpr int kValueRow = kSteps == 6 ? kDim + 32 : kDim;
+  static_assert(kTurned || (kValueRow * 2) % 256 == 192, "rows of values fall on different banks");
   typedef PageOf<kPages> Page;
   typedef typename Page::Raw Raw;
   constexpr bool kMx = Page::kMx;
@@ -87,6 +88,18 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   __shared__ uint64_t s_odd[2][kDim];
   __shared__ uint32_t s_any_odd[kManyWaves];
 
+  const int32_t x0 = (int32_t)part.from, x_end = min(range.count, (int32_t)part.upto);
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  // Where block x's keys lie: a wave looks up a key a lane; the first blocks' at once, while the
+  // rows are found.
+  auto look_up = [&](int32_t x) __attribute__((always_inline)) {
+    return key_look(p, w, tile, (x >= x0) & (x < x_end), range.block(x) * kManyBlock + lane, range.end);
+  };
+  const KeyLook soon = look_up(wave < 4 ? x0 - 1 + wave : x_end);
+  KeyLook ahead = look_up(x0 + 3 + wave);
+
   __shared__ RowSees s_rows[kGroup ? kManyRows : 1];  // of a group's tile
   // Positions below it are seen by all rows of the tile.  What a group's rows see differs, and
   // w.r.prefix is its end there: no row sees more.
@@ -98,9 +111,6 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
     sure = s.prefix;
   }
 
-  const int32_t x0 = (int32_t)part.from, x_end = min(range.count, (int32_t)part.upto);
-
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 31, g = lane >> 5;
   const uint64_t zeros = (uint64_t)(uintptr_t)kv_zeros;
 
@@ -135,11 +145,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   }
   const ScoreChange change(scale, p.cap, biased ? p.slopes[qhead] : 0.f);
 
-  // Where block x's keys lie: wave 0 looks up a key a lane ...
-  auto look_up = [&](int32_t x) __attribute__((always_inline)) {
-    return key_look(p, w, tile, (x >= x0) & (x < x_end), range.block(x) * kManyBlock + lane, range.end);
-  };
-  // ... and hands its rows to all.
+  // A looked up key's rows for all.
   auto hand_out = [&](const KeyLook &k, int32_t x) __attribute__((always_inline)) {
     const bool there = key_there(p, k);
     const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
@@ -326,7 +332,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   // so the exponentials go between those of S^T.  LDS is read first, all at once, while the
   // products of the 32 keys before are still under way and the maximum is looked for.
   auto both = [&](f32x16 &s, f32x16 &next, int32_t j_next, auto keys, auto values, auto &&prepare) __attribute__((always_inline)) {
-    constexpr int kTiles = kSteps > 4 ? 4 : kSteps, kTurns = kSteps / kTiles;
+    constexpr int kTiles = kSteps == 6 ? 3 : kSteps > 4 ? 4 : kSteps, kTurns = kSteps / kTiles;
     constexpr uint32_t kFrom = decltype(values)::value, kSixteen = 16 * kValueRow * 2;
     constexpr uint32_t kFar = kFrom + kSixteen > 65535 ? kFrom : 0;  // an instruction's offset has 16 bits
     // held as they are: the addresses made of them would cost registers
@@ -389,7 +395,6 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   // is compiled.
   constexpr uint32_t kHalfKeys = 32 * kKeyRow * 2, kHalfValues = 32 * kValueRow * 2;
   f32x16 now, next;
-  KeyLook ahead{};
   auto step = [&](int32_t x, auto turn, auto computes) __attribute__((always_inline)) {
     constexpr int kNow = decltype(turn)::value, kNext = 1 - kNow;
     constexpr uint32_t k_now = kKeys[kNow], k_next = kKeys[kNext], v_now = kValues[kNow], v_next = kValues[kNext];
@@ -462,8 +467,7 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
   };
 
   for (uint32_t i = threadIdx.x; i < 2 * kDim; i += kManyThreads) (&s_odd[0][0])[i] = 0;
-  for (int i = wave; i < 4; i += kManyWaves) hand_out(look_up(x0 - 1 + i), x0 - 1 + i);
-  ahead = look_up(x0 + 3 + wave);
+  if (wave < 4) hand_out(soon, x0 - 1 + wave);
   __syncthreads();
   if (x0 < x_end) {
     load(x0 - 1, 0, kKeys[1]);
@@ -551,20 +555,20 @@ __device__ __forceinline__ void many_part(const AttendParams &p, const WorkItem 
 
 // Workgroups a CU: three for D <= 64, in 168 registers (8 requests of 1000 tokens over 8000: 127
 // us; two workgroups, with room for more registers, 137), two for 96.
-template <typename Q, int kPages, int kSteps, int kMore, bool kGroup>
-__global__ __launch_bounds__(many_waves(kSteps) * 64, kSteps >= 4 ? 1 : kSteps > 2 ? 2 : 3) void attend_many(AttendParams p) {
+template <typename Q, int kPages, int kSteps, int kMore, bool kGroup, int kManyWaves>
+__global__ __launch_bounds__(kManyWaves * 64, kSteps > 4 || kManyWaves > 4 ? 1 : kSteps > 2 ? 2 : 3) void attend_many(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
-  if (!find_item<many_waves(kSteps) * 64, kManyBlock, kGroup>(p, index, w)) return note_cut<many_rows(kSteps)>(p, index, head);
+  if (!find_item<kManyWaves * 64, kManyBlock, kGroup>(p, index, w)) return note_cut<kManyWaves * 32>(p, index, head);
   for (;;) {
     const Tile tile = tile_of(p, w.r, w.tile);
     const KeyRange range = key_range<kManyBlock>(p, w.r, tile.first, tile.last);
     const uint32_t blocks = (uint32_t)max(range.count, 1);
     const Part part = part_of(p, w, blocks, index);
-    if (!part.none) many_part<Q, kPages, kSteps, kMore, kGroup>(p, w, tile, range, part, head);
+    if (!part.none) many_part<Q, kPages, kSteps, kMore, kGroup, kManyWaves>(p, w, tile, range, part, head);
     const uint64_t end = w.begin + max(blocks, p.pad);
     if (end >= (index + 1) * w.share || end >= w.line || !next_item<kGroup>(p, w, end))
-      return note_cut<many_rows(kSteps)>(p, index, head, w, tile, part, blocks);
+      return note_cut<kManyWaves * 32>(p, index, head, w, tile, part, blocks);
     __syncthreads();
   }
 }

@@ -7,6 +7,10 @@
 
 namespace gorio {
 
+// Whether the form for many rows has workgroups of four waves where it has eight: with powers, two of
+// them would not fit LDS.
+constexpr bool brief_many(int pages) { return pages < kPagesMx8; }
+
 // One form's launch: AttendParams' fields for the division of its work.
 struct AttendForm {
   uint32_t rows, from, upto, shares, least, whole, pad;
@@ -33,22 +37,26 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
     p.pad = f.pad;
     p.cuts = f.cuts;
   };
-  auto run_many = [&](const AttendForm &f, void (*kernel)(AttendParams)) {
+  auto run_many = [&](const AttendForm &f, void (*kernel)(AttendParams), auto waves) {
+    constexpr int kWaves = decltype(waves)::value;
     divide(f);
-    kernel<<<f.shares * p.kv_heads, many_waves(kSteps) * 64, 0, s>>>(p);
+    kernel<<<f.shares * p.kv_heads, kWaves * 64, 0, s>>>(p);
     if (f.cuts)
-      attend_join<Q, many_rows(kSteps), (kSteps > 4)><<<dim3((f.shares - 1) * p.kv_heads, many_rows(kSteps) / 16), 256, 0, s>>>(p);
+      attend_join<Q, kWaves * 32, (kSteps > 4)><<<dim3((f.shares - 1) * p.kv_heads, kWaves * 2), 256, 0, s>>>(p);
   };
+  constexpr int kLong = many_waves(kSteps, false);
+  constexpr int kBrief = many_waves(kSteps, brief_many(kPages));
   if (l.group.shares) {
     p.grouped = true;
     p.requests = l.groups;
-    run_many(l.group, attend_many<Q, kPages, kSteps, kMore == 1 ? 3 : kMore, true>);
+    run_many(l.group, attend_many<Q, kPages, kSteps, kMore == 1 ? 3 : kMore, true, kLong>, std::integral_constant<int, kLong>{});
     p.grouped = false;
     p.requests = p.all_requests;
   }
   if (l.few.shares) {
     divide(l.few);
-    constexpr int kFew = PageOf<kPages>::kMx && kSteps == 3 ? 4 : kSteps;  // a key's lanes take equal numbers of eights
+    // a key's lanes take equal numbers of eights
+    constexpr int kFew = kSteps == 6 ? 8 : PageOf<kPages>::kMx && kSteps == 3 ? 4 : kSteps;
     constexpr int kWaves = few_waves(kFew, false), kShort = few_waves(kFew, true);
     if (l.group.shares)
       attend_few<Q, kPages, kFew, (kMore > 0), kShort><<<l.few.shares * p.kv_heads, kShort * 64, 0, s>>>(p);
@@ -56,7 +64,10 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
       attend_few<Q, kPages, kFew, (kMore > 0), kWaves><<<l.few.shares * p.kv_heads, kWaves * 64, 0, s>>>(p);
     if (l.few.cuts) attend_join<Q, kFewRows, (kSteps > 4)><<<(l.few.shares - 1) * p.kv_heads, 256, 0, s>>>(p);
   }
-  if (l.many.shares) run_many(l.many, attend_many<Q, kPages, kSteps, kMore, false>);
+  if (l.many.shares) {
+    if (l.group.shares) run_many(l.many, attend_many<Q, kPages, kSteps, kMore, false, kBrief>, std::integral_constant<int, kBrief>{});
+    else run_many(l.many, attend_many<Q, kPages, kSteps, kMore, false, kLong>, std::integral_constant<int, kLong>{});
+  }
   return hipGetLastError();
 }
 
@@ -71,12 +82,18 @@ hipError_t launch_steps(const AttendParams &p, const AttendLaunch &l, hipStream_
   }
 }
 
-// 32-element steps of the kernels for a head of D elements.
-inline int steps_of(uint32_t D) { return D <= 64 ? 2 : D <= 96 ? 3 : D <= 128 ? 4 : 8; }
+// 32-element steps of the kernels for a head of D elements.  Heads of 129..192 have kernels of their
+// own where elements have powers, which take registers on their way into LDS: 4096 tokens of 160
+// elements over 16384 took 2981 us from MX8 pages as 256 elements.
+inline int steps_of(uint32_t D, int pages) {
+  return D <= 64 ? 2 : D <= 96 ? 3 : D <= 128 ? 4 : D <= 192 && pages >= kPagesMx8 ? 6 : 8;
+}
 
 template <typename Q, int kPages>
 hipError_t launch_pages(const AttendParams &p, const AttendLaunch &l, hipStream_t s) {
-  switch (steps_of(p.D)) {
+  if constexpr (PageOf<kPages>::kMx)
+    if (steps_of(p.D, kPages) == 6) return launch_steps<Q, kPages, 6>(p, l, s);
+  switch (steps_of(p.D, kPages)) {
     case 2: return launch_steps<Q, kPages, 2>(p, l, s);
     case 3: return launch_steps<Q, kPages, 3>(p, l, s);
     case 4: return launch_steps<Q, kPages, 4>(p, l, s);
