@@ -110,14 +110,18 @@ __device__ __forceinline__ u32x4 widened(uint32_t r, float by) {
   return u32x4{Q::template widen4<0>(r, by), Q::template widen4<1>(r, by), Q::template widen4<2>(r, by),
                Q::template widen4<3>(r, by)};
 }
-// Four of them.
+// The first four of them.
 template <typename Q>
-__device__ __forceinline__ u32x2 widened_half(uint32_t r, float by) {
-  return u32x2{Q::template widen<false>(r, by), Q::template widen<true>(r, by)};
+__device__ __forceinline__ u32x4 widened_half(u32x2 r, float by) {
+  return u32x4{Q::template widen<false>(r.x, by), Q::template widen<true>(r.x, by), 0, 0};
 }
 template <typename Q>
-__device__ __forceinline__ u32x2 widened_half(uint16_t r, float by) {
-  return u32x2{Q::template widen4<0>(r, by), Q::template widen4<1>(r, by)};
+__device__ __forceinline__ u32x4 widened_half(uint32_t r, float by) {
+  return u32x4{Q::template widen4<0>(r, by), Q::template widen4<1>(r, by), 0, 0};
+}
+template <typename Q>
+__device__ __forceinline__ u32x4 widened_half(u32x4 r, float) {  // 16-bit pages have no halves
+  return r;
 }
 // A power's byte as such a factor.
 __device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }

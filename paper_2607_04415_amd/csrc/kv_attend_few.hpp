@@ -40,27 +40,21 @@ __host__ __device__ constexpr int few_waves(int steps, bool brief) { return step
 constexpr int kFewRows = 16;
 constexpr int kFewBlock = 32;  // keys
 
-// The powers of a row's blocks, of which there are `count`, up to kBlocks, or (kAll) as many.
-template <int kBlocks, typename Powers, bool kAll>
+// The powers of a row's blocks, of which there are `count`: kBlocks or one less.  Two loads, the
+// second up to the last of them, and of any alignment.
+template <int kBlocks, typename Powers>
 __device__ __forceinline__ Powers load_powers(uint64_t from, uint32_t count) {
-  typedef uint32_t Four __attribute__((aligned(1)));  // a load of any alignment
+  typedef uint32_t Four __attribute__((aligned(1)));
   typedef uint16_t Two __attribute__((aligned(1)));
-  uint32_t w[(kBlocks + 3) / 4] = {};
-  if constexpr (kAll && kBlocks == 2) {
-    w[0] = load_at<Two>(from);
-  } else if constexpr (kAll) {
-#pragma unroll
-    for (int i = 0; i < kBlocks / 4; ++i) w[i] = load_at<Four>(from + i * 4);
-  } else {  // the last one again for those past it
-#pragma unroll
-    for (int i = 0; i < kBlocks; ++i)
-      w[i / 4] |= (uint32_t)load_at<uint8_t>(from + min((uint32_t)i, count - 1)) << (i % 4) * 8;
-  }
-  if constexpr (kBlocks == 8) return Powers{w[0], w[1]};
-  else return w[0];
+  static_assert(kBlocks == 2 || kBlocks == 4 || kBlocks == 6 || kBlocks == 8, "pairs of blocks");
+  const uint32_t less = kBlocks - count;
+  if constexpr (kBlocks == 2) return load_at<uint8_t>(from) | (uint32_t)load_at<uint8_t>(from + count - 1) << (count - 1) * 8;
+  else if constexpr (kBlocks == 4) return load_at<Two>(from) | (uint32_t)load_at<Two>(from + count - 2) << (count - 2) * 8;
+  else if constexpr (kBlocks == 6) return Powers{load_at<Four>(from), (uint32_t)load_at<Two>(from + count - 2) >> less * 8};
+  else return Powers{load_at<Four>(from), load_at<Four>(from + count - 4) >> less * 8};
 }
 
-// kSteps: 32-element steps of a head, D <= 32 kSteps (2, 4 or 8 with powers).  kPages: a PageKind.
+// kSteps: 32-element steps of a head, D <= 32 kSteps (2, 4, 6 or 8 with powers).  kPages: a PageKind.
 // kMore: scores are capped or biased.
 template <typename Q, int kPages, int kSteps, bool kMore, int kFewWaves>
 __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &w, const Tile &tile,
@@ -69,11 +63,12 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   typedef PageOf<kPages> Page;
   typedef typename Page::Raw Raw;
   constexpr bool kMx = Page::kMx;
-  constexpr int kHalves = (kSteps + 3) / 4;  // 128 elements of a value
-  // Elements of a value in a lane, and products.  (16-bit pages of 64 elements are read as if they had
-  // 128, which costs them nothing while HBM is the bound.)
-  constexpr int kPer = kMx && kSteps == 2 ? 4 : 8;
-  constexpr int kDim = kHalves * 128;
+  // A value in runs of 128 elements, eight to a lane, of which as many products come; with powers the
+  // last run may be 64, four to a lane.  (16-bit pages of 64 elements are read as if they had 128, which
+  // costs them nothing while HBM is the bound.)
+  constexpr int kRuns = (kSteps + 3) / 4, kFull = kMx ? kSteps / 4 : kRuns;
+  constexpr auto per = [](int h) { return h < kFull ? 8 : 4; };
+  constexpr int kProducts = kFull * 8 + (kRuns - kFull) * 4, kDim = kProducts * 16;
   constexpr int kPad = kDim + 4;
   // Powers of a row's blocks, a byte each; the lanes that look a key up load them and hand them
   // out a block later.
@@ -82,7 +77,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   __shared__ __align__(16) Powers s_power[kMx ? kFewWaves : 1][2][kFewBlock];  // keys, values
   // Elements of a key in a lane, which need not be every fourth eight of them: with powers they
   // follow one another, so that they are one load, or few, and their powers one or two.
-  constexpr int kWords = kPages == kPagesMx4 ? kSteps : kSteps * 2, kLoad = kWords < 4 ? kWords : 4;
+  constexpr int kWords = kPages == kPagesMx4 ? kSteps : kSteps * 2, kLoad = kWords % 4 ? 2 : 4;
   typedef typename std::conditional<kLoad == 2, u32x2, u32x4>::type Load;
   auto element = [](int s, int g) __attribute__((always_inline)) -> uint32_t { return kMx ? g * 8 * kSteps + s * 8 : s * 32 + g * 8; };
   __shared__ uint64_t s_row[kFewWaves][2][2][kFewBlock];  // wave, turn, keys or values
@@ -115,9 +110,9 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   const ScoreChange change(scale, p.cap, kMore && p.slopes ? p.slopes[qhead] : 0.f);
 
   float best = -INFINITY, sum = 0.f;
-  f32x4 o[kHalves * kPer];
+  f32x4 o[kProducts];
 #pragma unroll
-  for (int t = 0; t < kHalves * kPer; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < kProducts; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   // Rows of block x into LDS, and its keys' bits: lanes 0..31 a key each, with powers the others too.
   auto place_of = [&](int32_t x) __attribute__((always_inline)) {
@@ -130,7 +125,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     asm("" : "+v"(all_powers));
   }
   Powers powers{};  // of a key (lanes 0..31) or value (32..63) of the block whose rows were handed out last
-  auto hand_out = [&](const KeyLook &k, int turn, auto whole_rows) __attribute__((always_inline)) -> uint32_t {
+  auto hand_out = [&](const KeyLook &k, int turn) __attribute__((always_inline)) -> uint32_t {
     const bool there = key_there(p, k);
     const uint64_t off = (uint64_t)(uint32_t)k.page * p.page_stride + head * p.head_stride + k.place * p.token_stride;
     if (lane < kFewBlock) {
@@ -139,7 +134,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     }
     if constexpr (kMx) {
       const uint64_t from = there ? all_powers + Page::powers(off) : zeros;
-      powers = load_powers<kBlocks, Powers, decltype(whole_rows)::value>(from, p.D / kMxBlock);
+      powers = load_powers<kBlocks, Powers>(from, p.D / kMxBlock);
     }
     wave_lds_order();
     return (uint32_t)__ballot(there);
@@ -172,18 +167,19 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
       }
     }
   };
-  typedef typename std::conditional<kPer == 8, Raw, typename std::conditional<kPages == kPagesMx4, uint16_t, uint32_t>::type>::type
-      RawValue;
-  auto load_values = [&](RawValue (&v)[8], int half, int turn, auto whole_rows) __attribute__((always_inline)) {
-    const uint32_t d = half * 128 + m * kPer;
+  auto load_values = [&](Raw (&v)[8], int h, int turn, auto whole_rows) __attribute__((always_inline)) {
+    const uint32_t d = h * 128 + m * per(h);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       uint64_t row = s_row[wave][turn][1][(i >> 2) * 16 + g * 4 + (i & 3)];
       asm("" : "+v"(row));
-      v[i] = load_at<RawValue>(decltype(whole_rows)::value || d < p.D ? row + Page::bytes(d) : zeros);
+      const uint64_t at = decltype(whole_rows)::value || d < p.D ? row + Page::bytes(d) : zeros;
+      if (h < kFull) v[i] = load_at<Raw>(at);
+      else if constexpr (kPages == kPagesMx4) v[i] = load_at<uint16_t>(at);
+      else if constexpr (kPages == kPagesMx8) v[i] = u32x2{load_at<uint32_t>(at), 0};
     }
   };
-  // What the powers of step s of a key, and of a value's half, multiply by, from LDS.
+  // What the powers of step s of a key, and of a value's run, multiply by, from LDS.
   auto key_factor = [&](int i, int s) __attribute__((always_inline)) -> float {
     if constexpr (!kMx) return 1.f;
     const Powers all = s_power[kMx ? wave : 0][0][i * 16 + m];
@@ -191,23 +187,23 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     if constexpr (kSteps > 4) return power_of((block < 4 ? all.x : all.y) >> (block & 3) * 8 & 255);
     else return power_of(all >> block * 8 & 255);
   };
-  auto value_factor = [&](int i, int half) __attribute__((always_inline)) -> float {
+  auto value_factor = [&](int i, int h) __attribute__((always_inline)) -> float {
     if constexpr (!kMx) return 1.f;
     const Powers all = s_power[kMx ? wave : 0][1][(i >> 2) * 16 + g * 4 + (i & 3)];
-    const uint32_t block = m * kPer / kMxBlock;
-    if constexpr (kSteps > 4) return power_of((half ? all.y : all.x) >> block * 8 & 255);
+    const uint32_t block = m * per(h) / kMxBlock;
+    if constexpr (kSteps > 4) return power_of((h ? all.y : all.x) >> block * 8 & 255);
     else return power_of(all >> block * 8 & 255);
   };
   // Block x, with the next one's keys and values on their way; the registers alternate.
   Raw k[2][2][kSteps];
-  RawValue v[2][kHalves][8];
+  Raw v[2][kRuns][8];
   uint32_t there[2];
   KeyLook next;
   auto load = [&](auto turn, auto whole_rows) __attribute__((always_inline)) {
     constexpr int t = decltype(turn)::value;
     load_keys(k[t], t, whole_rows);
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h) load_values(v[t][h], h, t, whole_rows);
+    for (int h = 0; h < kRuns; ++h) load_values(v[t][h], h, t, whole_rows);
   };
   auto step = [&](int32_t x, auto turn, auto whole_rows) __attribute__((always_inline)) {
     constexpr int t0 = decltype(turn)::value, t1 = 1 - t0;
@@ -217,7 +213,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
       s_power[wave][lane >> 5][lane & 31] = powers;
       wave_lds_order();
     }
-    there[t1] = hand_out(next, t1, whole_rows);
+    there[t1] = hand_out(next, t1);
     next = place_of(x + 2 * kFewWaves);
     load(std::integral_constant<int, t1>{}, whole_rows);
 
@@ -259,7 +255,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
       best = to;
       sum *= keep;
 #pragma unroll
-      for (int t = 0; t < kHalves * kPer; ++t) o[t] *= keep;
+      for (int t = 0; t < kProducts; ++t) o[t] *= keep;
     }
     const float base = best == -INFINITY ? 0.f : best;
     float part = 0.f;
@@ -271,11 +267,11 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
     sum += part;
     const u32x4 weights = {Q::pack(e[0], e[1]), Q::pack(e[2], e[3]), Q::pack(e[4], e[5]), Q::pack(e[6], e[7])};
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h) {
-      typename std::conditional<kPer == 8, u32x4, u32x2>::type vw[8];
+    for (int h = 0; h < kRuns; ++h) {
+      u32x4 vw[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if constexpr (kPer == 8) vw[i] = widened<Q>(v[t0][h][i], value_factor(i, h));
+        if (h < kFull) vw[i] = widened<Q>(v[t0][h][i], value_factor(i, h));
         else vw[i] = widened_half<Q>(v[t0][h][i], value_factor(i, h));
       }
       // A weight of 0 keeps a value out of a row, unless the value is NaN or inf.  Such
@@ -285,12 +281,12 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int c = 0; c < kPer / 2; ++c) odd |= any_not_finite<Q>(vw[i][c]);
+          for (int c = 0; c < per(h) / 2; ++c) odd |= any_not_finite<Q>(vw[i][c]);
         odd = __any(odd);
       }
       auto products = [&](auto test) __attribute__((always_inline)) {
 #pragma unroll
-        for (int t = 0; t < kPer; ++t) {
+        for (int t = 0; t < per(h); ++t) {
           const uint32_t sel = t & 1 ? 0x07060302u : 0x05040100u;
           u32x4 a;
 #pragma unroll
@@ -303,11 +299,11 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
                 const int at = (i >> 1) * 16 + (i & 1) * 2;
                 seen[i] = Q::pack((float)(sees >> at & 1u), (float)(sees >> (at + 1) & 1u));
               }
-              o[h * kPer + t] += not_finite_part<Q>(a, seen);
+              o[h * 8 + t] += not_finite_part<Q>(a, seen);
               a = finite_only<Q>(a);
             }
           }
-          o[h * kPer + t] = Q::mfma16(a, weights, o[h * kPer + t]);
+          o[h * 8 + t] = Q::mfma16(a, weights, o[h * 8 + t]);
         }
       };
       // One test is better than eight, but 16-bit pages' registers do not hold the products twice.
@@ -317,7 +313,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   };
   auto steps = [&](auto whole_rows) __attribute__((always_inline)) {
     int32_t x = (int32_t)part.from + wave;
-    there[0] = hand_out(place_of(x), 0, whole_rows);
+    there[0] = hand_out(place_of(x), 0);
     next = place_of(x + kFewWaves);
     load(std::integral_constant<int, 0>{}, whole_rows);
     while (x < x_end) {
@@ -336,14 +332,14 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   sum = xor16(xor32(sum, sum_of), sum_of);
   if (g == 0) s_m[wave][m] = best, s_l[wave][m] = sum;
 #pragma unroll
-  for (int h = 0; h < kHalves; ++h)
+  for (int h = 0; h < kRuns; ++h)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      float *to = &s_o[wave][m][h * 128 + (g * 4 + r) * kPer];
+      float *to = &s_o[wave][m][h * 128 + (g * 4 + r) * per(h)];
 #pragma unroll
-      for (int t = 0; t < kPer; t += 4)
+      for (int t = 0; t < per(h); t += 4)
         *reinterpret_cast<f32x4 *>(to + t) =
-            f32x4{o[h * kPer + t][r], o[h * kPer + t + 1][r], o[h * kPer + t + 2][r], o[h * kPer + t + 3][r]};
+            f32x4{o[h * 8 + t][r], o[h * 8 + t + 1][r], o[h * 8 + t + 2][r], o[h * 8 + t + 3][r]};
     }
   __syncthreads();
   constexpr int kRowThreads = kFewThreads / kFewRows, kOwn = 128 / kRowThreads;  // elements of each 128
@@ -375,7 +371,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
   const float norm = divided ? 1.f : all != 0.f ? vs / all : 0.f;
   const uint64_t slot = ((uint64_t)part.slot * p.kv_heads + head) * kFewRows + row;
 #pragma unroll
-  for (int h = 0; h < kHalves; ++h) {
+  for (int h = 0; h < kRuns; ++h) {
     const uint32_t d = h * 128 + at * kOwn;
     if (d >= p.D) break;
 #pragma unroll

@@ -252,14 +252,15 @@ def test_attend_shapes(torch, kind, type, H, KV, D, page):
     dict(prefix=[100, 90, 80, 70], window=5), dict(fills=True, prefix=[96, 0, 64, 200], slopes=True, cap=30.0, window=33),
     dict(absent=0.5), dict(absent=1.0), dict(fills=True, absent=0.3, prefix=[2**31 - 1, -5, 3, 0], slopes=True),
     dict(slopes=True, cap=100.0), dict(scale=-0.3, slopes=True), dict(scale=0.0), dict(scale=0.0, slopes=True)])
-def test_attend_masks(torch, kind, type, news, opts):
+@pytest.mark.parametrize("D", [64, 160])
+def test_attend_masks(torch, kind, type, news, opts, D):
     """Windows, prefixes, caps, biases, factors, pages that end early or are missing, rows that see nothing."""
-    a = small(torch, kind, 3, type, 4, 2, 64, 16, news, [120, 97, 203, 71], **opts)
+    a = small(torch, kind, 3, type, 4, 2, D, 16, news, [120, 97, 203, 71], **opts)
     holds(torch, a, call(torch, a, max_new=max(news)))
 
 
 @pytest.mark.parametrize("kind", ["mx8", "mx4"])
-@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 192, 224, 256])
 @pytest.mark.parametrize("news,lens,H,KV", [([1], [5000], 2, 1), ([2, 1, 1], [2600, 3, 1300], 4, 2), ([20, 1], [2100, 700], 2, 2),
                                             ([9, 40], [2600, 1500], 2, 1)])
 def test_attend_long(torch, kind, D, news, lens, H, KV):
@@ -278,12 +279,13 @@ def test_attend_token_major(torch, kind, news):
 @pytest.mark.parametrize("kind", ["mx8", "mx4"])
 @pytest.mark.parametrize("type", ["bf16", "f16"])
 @pytest.mark.parametrize("news", [[3], [100]])
-def test_attend_nan_blocks(torch, kind, type, news):
+@pytest.mark.parametrize("D", [64, 96, 128, 192, 256])
+def test_attend_nan_blocks(torch, kind, type, news, D):
     """A block of a later token's values is NaN: rows that do not see it are as without, those that do
     are NaN at its elements.  And a block of keys: those that see it are NaN throughout."""
     n = news[0]
     for side in (3, 1):
-        a = small(torch, kind, 10, type, 4, 2, 64, 16, news, [150], poison=False)
+        a = small(torch, kind, 10, type, 4, 2, D, 16, news, [150], poison=False)
         cache = a["cache"]
         bad = 150 - n // 2                                  # visible to the last n // 2 rows only
         page, place = a["tables"][0, bad // 16], bad % 16
@@ -292,8 +294,8 @@ def test_attend_nan_blocks(torch, kind, type, news):
         w_out, _, bound, _ = ref.attend(a)
         x = out.double().cpu().numpy()
         sees = np.arange(n) >= n - n // 2
-        hit = np.zeros((n, 4, 64), bool)
-        hit[sees, 2:, 32 if side == 3 else 0:] = True
+        hit = np.zeros((n, 4, D), bool)
+        hit[sees, 2:, 32 if side == 3 else 0:64 if side == 3 else D] = True
         assert np.isnan(x[hit]).all()
         assert (np.abs(x - w_out)[~hit] <= bound[~hit]).all()
 
