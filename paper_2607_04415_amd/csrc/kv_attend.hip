@@ -95,7 +95,11 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   const uint64_t most = a.max_new ? std::min<uint64_t>(a.max_new, a.tokens) : a.tokens;
   const uint64_t others = (a.requests - 1) * most;
   const uint64_t fewest = a.tokens > others ? std::min(a.tokens - others, most) : 1;
-  const bool few = fewest * group < kFewUpto, many = most * group >= kFewUpto;
+  const bool many = most * group >= kFewUpto;
+  // Behind a shared prefix a request's own keys are few, and its rows of either form wait for latency:
+  // where most requests have chunks, the others go with them rather than in a launch of their own.
+  const bool together = groups && many && a.tokens * group >= 2 * kFewUpto * a.requests;
+  const bool few = fewest * group < kFewUpto && !together;
   const int steps = steps_of(c.D, l.pages);
   // The least share and the largest tile that is not cut, in blocks.  Few rows: 8 blocks are one
   // a wave; 8 requests of 250 tokens take 13 us, with shares of 16 blocks 19, of 32 31 us.  Tiles
