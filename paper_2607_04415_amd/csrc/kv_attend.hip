@@ -78,7 +78,8 @@ uint64_t carry_bytes(const gorio_kv_cache &c, const gorio_kv_attention &a) {
 constexpr uint64_t kWorthSharing = 200'000'000;
 uint32_t groups_of(const gorio_kv_cache &c, const gorio_kv_attention &a, const gorio_kv_sharing *sharing) {
   const uint64_t positions = (uint64_t)a.width * c.page_tokens * a.requests;  // below 2^63
-  const bool worth = positions / 64 * (2 * c.heads * c.D) >= kWorthSharing / 64;
+  const uint64_t row = 2ull * c.heads * c.D;
+  const bool worth = positions >= (kWorthSharing + row - 1) / row;
   return sharing && worth && !(a.window && !a.prefix) ? sharing->groups : 0;
 }
 

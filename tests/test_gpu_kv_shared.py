@@ -1,15 +1,19 @@
 """Attention of a batch whose requests share their first pages: as without sharing, by kv_reference.attend."""
+import ctypes
+
 import numpy as np
 import pytest
 
 import kv_reference as ref
 import mx_reference as mx
 import paper_2607_04415_amd as g
+from paper_2607_04415_amd import kv
 from test_gpu_kv import call, holds, ints, setup
 from test_gpu_kv_mx import small
 
 pytestmark = pytest.mark.gpu
 NAN = float("nan")
+ROOM = 200_000_000         # elements of keys and values that tables have room for, from which groups are computed
 
 
 @pytest.fixture(scope="module")
@@ -24,6 +28,8 @@ def inputs(torch, seed, type, cache, H, KV, D, page, groups, news, own, shared, 
     of = np.repeat(np.arange(len(groups)), groups)
     shared = np.array(shared)[of] // page * page
     lens = np.array(own) + shared
+    # calls whose tables have room for little are computed without groups: these have room for more
+    more.setdefault("width", ROOM // (2 * KV * D * page * len(lens)) + 1 + int(lens.max()) // page)
     make = (lambda *a, **k: small(torch, cache, *a, **k)) if cache in mx.KINDS else \
         (lambda seed, type, *a, **k: setup(torch, seed, type, cache, *a, **k))
     a = make(seed, type, H, KV, D, page, news, np.maximum(lens, 0), poison=False, **more)
@@ -35,8 +41,8 @@ def inputs(torch, seed, type, cache, H, KV, D, page, groups, news, own, shared, 
             a["fills"][b, :n] = a["fills"][lead, :n]
     a["first"], a["shared"] = first, shared
     if poison:
-        kv = a["cache"]
-        pages = kv.keys.shape[0]
+        c = a["cache"]
+        pages = c.keys.shape[0]
         seen = np.zeros((pages, page), bool)
         for b in range(len(lens)):
             for i in range(news[b]):
@@ -44,16 +50,29 @@ def inputs(torch, seed, type, cache, H, KV, D, page, groups, news, own, shared, 
                 seen[a["tables"][b, j // page], j % page] = True
         bad = torch.from_numpy(~seen).cuda()
         if cache in mx.KINDS:
-            for x in (kv.key_scale, kv.value_scale):
+            for x in (c.key_scale, c.value_scale):
                 x.view(torch.uint8).permute(0, 2, 1, 3)[bad] = 255
         elif cache == "e4m3":
-            for x in (kv.keys, kv.values):
+            for x in (c.keys, c.values):
                 x.view(torch.uint8).permute(0, 2, 1, 3)[bad] = 127
         else:
-            for x in (kv.keys, kv.values):
+            for x in (c.keys, c.values):
                 x.permute(0, 2, 1, 3)[bad] = NAN
                 x.permute(0, 2, 1, 3)[..., ::2][bad] = float("inf")
     return a
+
+
+def grouped(a):
+    """Whether such a call has room for the sums over shared positions."""
+    T, H, D = a["q"].shape
+    B, width = a["tables"].shape
+    desc = kv.AttentionDesc(dtype=kv.BF16 if a["type"] == "bf16" else kv.F16, heads=H, requests=B, width=width, tokens=T,
+                            prefix=None if a.get("prefix") is None else 64, window=a["window"], scale=1.0)
+    share, n = kv.SharingDesc(groups=B), [ctypes.c_uint64() for _ in range(2)]
+    L, c = g.lib(), a["cache"]._ref
+    assert L.gorio_kv_workspace(c, ctypes.byref(desc), ctypes.byref(n[0])) == g.OK
+    assert L.gorio_kv_workspace_shared(c, ctypes.byref(desc), ctypes.byref(share), ctypes.byref(n[1])) == g.OK
+    return n[0].value != n[1].value
 
 
 def sharing(torch, a, first=None):
@@ -63,6 +82,7 @@ def sharing(torch, a, first=None):
 def check(torch, a, want=None, **more):
     want = ref.attend(a) if want is None else want
     holds(torch, a, call(torch, a, sharing=sharing(torch, a), **more), want)
+    assert grouped(a) == (not a["window"] or a.get("prefix") is not None)
     return want
 
 
@@ -135,6 +155,7 @@ def test_groups_as_found(torch):
     got = g.kv_share(ints(torch, a["tables"]), ints(torch, held), 16, least=64)
     assert got.first.tolist() == [0, 3, 4, 6, 6, 6, 6] and got.shared.tolist() == [320, 320, 320, 0, 640, 640]
     holds(torch, a, call(torch, a, sharing=got), want)
+    assert grouped(a)
     holds(torch, a, call(torch, a, sharing=got, max_new=30), want)
     alone = g.KVSharing(ints(torch, np.arange(7)), ints(torch, a["shared"]))
     holds(torch, a, call(torch, a, sharing=alone), want)
@@ -152,6 +173,17 @@ def test_values_out_of_range_stay_inside(torch):
         out, lse = call(torch, a, sharing=g.KVSharing(ints(torch, first), ints(torch, shared)))
         torch.cuda.synchronize()
         assert out.shape == (35, 4, 64) and lse.shape == (35, 4)
+
+
+def test_tables_with_little_room(torch):
+    """The same result, without the groups' own launches; and with a width right at the border."""
+    D, KV, page, B = 64, 2, 16, 5
+    border = -(-ROOM // (2 * KV * D * page * B))
+    for width in (30, border - 1, border):
+        a = inputs(torch, 7, "bf16", "bf16", 4, KV, D, page, [3, 2], [1, 1, 2, 1, 30], [40, 50, 20, 9, 77], [256, 160],
+                   width=width)
+        holds(torch, a, call(torch, a, sharing=sharing(torch, a)))
+        assert grouped(a) == (width == border)
 
 
 def test_rows_past_the_last_start_and_strides(torch):

@@ -61,13 +61,15 @@ def test_share_refusals(lib, requests, width, page, least, text):  # noqa: F811
 
 
 def test_sharing(lib):  # noqa: F811
-    c, a = cache(dtype=kv.MX4), attention(requests=5, tokens=7)
+    c, a = cache(dtype=kv.MX4), attention(requests=5, tokens=7, width=1 << 20)
     n, s = ctypes.c_uint64(), kv.SharingDesc(groups=2)
     need = lambda share: lib.gorio_kv_workspace_shared(ctypes.byref(c), ctypes.byref(a), share, ctypes.byref(n))
     assert need(ctypes.byref(s)) == g.OK
     assert n.value >= 7 * 4 * (64 + 2) * 4                      # of each row its sums, a maximum and a sum of weights
-    a.window = 10                                               # nothing is shared then
-    assert need(ctypes.byref(s)) == g.OK and n.value == workspace(lib, c, a)[1]
+    for more in (dict(window=10), dict(window=0, width=9000)):  # nothing is shared then, or not worth it
+        for k, v in more.items():
+            setattr(a, k, v)
+        assert need(ctypes.byref(s)) == g.OK and n.value == workspace(lib, c, a)[1]
     assert need(None) == g.EINVAL and b"sharing is NULL" in lib.gorio_last_error()
     for groups in (0, 6, 2**32 - 1):
         s.groups = groups
