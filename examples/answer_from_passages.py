@@ -9,10 +9,16 @@ then the answer token by token.  The "model" is one attention layer with random
 weights; what a program with a trained one would change is where its queries,
 keys and values come from.
 
-    python examples/answer_from_passages.py
+Each question may be answered several times over.  Its answers read the same
+passages, so their requests follow one another in the batch, and attention is
+told which first pages they have in common.  Pages hold 16 bits an element, or 4
+with a power of two for each 32.
+
+    python examples/answer_from_passages.py [--pages mx4] [--answers 3]
 """
 from __future__ import annotations
 
+import argparse
 import sys
 from pathlib import Path
 
@@ -44,7 +50,17 @@ class Layer:
         return rows[:, :HEADS], rows[:, HEADS:-KV_HEADS], rows[:, -KV_HEADS:]
 
 
-def run(nodes: int = 3000, questions: int = 4, found: int = 5, answer: int = 8, seed: int = 0) -> dict:
+def empty_cache(pages: int, type: str) -> g.KVCache:
+    shape = (pages, KV_HEADS, PAGE)
+    if type == "bf16":
+        return g.KVCache(*(torch.zeros((*shape, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    halves = [torch.zeros((*shape, D // 2), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    powers = [torch.zeros((*shape, D // 32), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    return g.KVCache(*(x.view(torch.float4_e2m1fn_x2) for x in halves), *(x.view(torch.float8_e8m0fnu) for x in powers))
+
+
+def run(nodes: int = 3000, questions: int = 4, found: int = 5, answer: int = 8, seed: int = 0, pages: str = "bf16",
+        answers: int = 1) -> dict:
     rng = np.random.default_rng(seed)
     gen = torch.Generator().manual_seed(seed)
     text = lambda n: torch.randn(n, HIDDEN, generator=gen).bfloat16().cuda()   # embedded tokens
@@ -55,12 +71,11 @@ def run(nodes: int = 3000, questions: int = 4, found: int = 5, answer: int = 8, 
     arrays = index_arrays(spec, use_cache=False)
     index = g.Index(arrays["x"], arrays["graph"])
     tokens = rng.integers(5, 61, nodes).astype(np.int32)
-    pages = -(-tokens // PAGE)
-    first_page = (np.cumsum(pages) - pages).astype(np.int32)
-    free = torch.arange(int(pages.sum()), int(pages.sum()) + 256, dtype=torch.int32, device="cuda")
-    shape = (int(pages.sum()) + 256, KV_HEADS, PAGE, D)
-    cache = g.KVCache(torch.zeros(shape, dtype=torch.bfloat16, device="cuda"),
-                      torch.zeros(shape, dtype=torch.bfloat16, device="cuda"))
+    held = -(-tokens // PAGE)
+    first_page = (np.cumsum(held) - held).astype(np.int32)
+    spare = 256 * answers
+    free = torch.arange(int(held.sum()), int(held.sum()) + spare, dtype=torch.int32, device="cuda")
+    cache = empty_cache(int(held.sum()) + spare, pages)
     at = np.concatenate([f * PAGE + np.arange(t) for f, t in zip(first_page, tokens)])
     _, k, v = layer.project(text(int(tokens.sum())))
     cache.store(k, v, torch.from_numpy(at).cuda())
@@ -68,30 +83,37 @@ def run(nodes: int = 3000, questions: int = 4, found: int = 5, answer: int = 8, 
     # the questions: what the search finds becomes each one's prefix
     ids, _, _ = index.search(torch.from_numpy(query_array(spec, QuerySpec(questions, 7))).cuda(), k=found, L=32, W=4,
                              stats=False)
+    ids = ids.repeat_interleave(answers, 0)          # a question's requests follow one another
     width = found * 4 + 16
     tables, fills, lens, _ = g.kv_attach(ids, torch.from_numpy(first_page).cuda(), torch.from_numpy(tokens).cuda(),
                                          PAGE, width, limit=found * 4)
     prefix = lens.clone()
-    new = torch.from_numpy(rng.integers(3, 30, questions).astype(np.int32))
+    new = torch.from_numpy(rng.integers(3, 30, questions).astype(np.int32)).repeat_interleave(answers)
     outputs = []
     x = text(int(new.sum()))
+    # what the requests have in common does not change from step to step: the passages
+    sharing = g.kv_share(tables, lens, PAGE, fills=fills, least=64) if answers > 1 else None
     for step in range(1 + answer):
         plan = g.kv_plan(lens, new.cuda(), free, tables, PAGE, len(x))
         q, k, v = layer.project(x)
         cache.store(k, v, plan.slots)
-        out = cache.attend(q, plan.starts, plan.lens, tables, fills=fills, prefix=prefix, max_new=int(new.max()))
+        out = cache.attend(q, plan.starts, plan.lens, tables, fills=fills, prefix=prefix, max_new=int(new.max()),
+                           sharing=sharing)
         y = out.reshape(len(x), HEADS * D) @ layer.out
         outputs.append(y)
-        last = dict(q=q, starts=plan.starts, lens=plan.lens, out=out)
+        last = dict(q=q, starts=plan.starts, lens=plan.lens, out=out, slots=plan.slots, sharing=sharing)
         free, lens = free[int(plan.taken):], plan.lens
         # the next token of each answer comes from the last row of its request
         x = torch.nn.functional.normalize(y[(plan.starts[1:] - 1).long()].float(), dim=1).mul(HIDDEN ** 0.5).bfloat16()
-        new = torch.ones(questions, dtype=torch.int32)
+        new = torch.ones(questions * answers, dtype=torch.int32)
     return dict(ids=ids, tables=tables, fills=fills, prefix=prefix, cache=cache, outputs=outputs, **last)
 
 
 if __name__ == "__main__":
-    r = run()
+    args = argparse.ArgumentParser()
+    args.add_argument("--pages", choices=("bf16", "mx4"), default="bf16")
+    args.add_argument("--answers", type=int, default=1)
+    r = run(**vars(args.parse_args()))
     torch.cuda.synchronize()
-    print(f"{len(r['prefix'])} questions, {r['prefix'].tolist()} positions of passages, "
+    print(f"{len(r['prefix'])} requests, {r['prefix'].tolist()} positions of passages, "
           f"{r['lens'].tolist()} in all after {len(r['outputs'])} steps")

@@ -254,3 +254,34 @@ def test_nothing_new_and_refusals(torch):
     out = a["cache"].attend(a["q_gpu"][:0], ints(torch, [0, 0, 0]), ints(torch, [130, 128]), ints(torch, a["tables"]),
                             sharing=sharing(torch, a))
     assert out.shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("type,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "mx4"), ("f16", "mx8")])
+@pytest.mark.parametrize("D", [64, 96, 128, 192])
+def test_shared_values_that_some_rows_see(torch, type, cache, D):
+    """NaN and inf among shared values that one request's prefix hides and another's shows."""
+    a = inputs(torch, 10, type, cache, 4, 2, D, 16, [3], [1, 2, 20], [30, 40, 50], [320], prefix=[320, 100, 320], poison=False)
+    # request 1 sees all up to its own tokens; it and the first end before the shared positions do
+    a["lens"] = np.array([350, 160, 370])
+    bad, c = 200, a["cache"]
+    page, place = a["tables"][0, bad // 16], bad % 16
+    hit = np.zeros((23, 4, D), bool)
+    sees = np.array([True] + [False] * 2 + [True] * 20)
+    if cache in mx.KINDS:
+        c.value_scale.view(torch.uint8)[page, 1, place, 1] = 255
+        hit[sees, 2:, 32:64] = True
+        signs = None
+    else:
+        c.values[page, 0, place, 3], c.values[page, 1, place, 5] = NAN, float("inf")
+        c.values[page, 1, place, D - 1] = float("-inf")
+        hit[sees, :2, 3], hit[sees, 2:, 5], hit[sees, 2:, D - 1] = True, True, True
+        signs = ((slice(2, 4), 5, np.inf), (slice(2, 4), D - 1, -np.inf))
+    assert grouped(a)
+    want, _, bound, _ = ref.attend(a)
+    out, _ = call(torch, a, sharing=sharing(torch, a))
+    x = out.double().cpu().numpy()
+    assert (np.abs(x - want)[~hit] <= bound[~hit]).all()
+    assert not np.isfinite(x[hit]).any()
+    if signs:
+        for heads, d, value in signs:
+            assert (x[sees][:, heads, d] == value).all()
