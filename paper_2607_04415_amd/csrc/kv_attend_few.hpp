@@ -430,12 +430,12 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 4 && kSteps <= 4 ? 2 : 1) vo
 // (750 cut tiles of 128 rows, 64 elements: 50 MB in 14 us).
 template <typename Q, int kRows, bool kWide>
 __global__ __launch_bounds__(256) void attend_join(AttendParams p) {
-  const uint32_t s0 = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - s0 * p.kv_heads;
-  const Cut cut = cuts_of<kRows>(p)[blockIdx.x];
+  const uint32_t s0 = fastdiv(blockIdx.y, p.by_kv), head = blockIdx.y - s0 * p.kv_heads;
+  const Cut cut = cuts_of<kRows>(p)[blockIdx.y];
   const uint32_t parts = cut.parts, slot0 = cut.slot, lane = threadIdx.x & 15;  // slot0: of the first part
   const float *ml = p.parts + (uint64_t)p.shares * 2 * p.kv_heads * kRows * p.D;
   const float vs = p.value_scale ? p.value_scale[head] : 1.f;
-  const uint32_t row = blockIdx.y * 16 + (threadIdx.x >> 4);
+  const uint32_t row = blockIdx.x * 16 + (threadIdx.x >> 4);
   if (parts && row < cut.rows) {
     auto slot = [&](uint32_t i) {
       return ((uint64_t)(i ? (s0 + i) * 2 : slot0) * p.kv_heads + head) * kRows + row;

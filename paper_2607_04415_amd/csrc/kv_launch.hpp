@@ -42,7 +42,7 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
     divide(f);
     kernel<<<f.shares * p.kv_heads, kWaves * 64, 0, s>>>(p);
     if (f.cuts)
-      attend_join<Q, kWaves * 32, (kSteps > 4)><<<dim3((f.shares - 1) * p.kv_heads, kWaves * 2), 256, 0, s>>>(p);
+      attend_join<Q, kWaves * 32, (kSteps > 4)><<<dim3(kWaves * 2, (f.shares - 1) * p.kv_heads), 256, 0, s>>>(p);
   };
   constexpr int kLong = many_waves(kSteps, false);
   constexpr int kBrief = many_waves(kSteps, brief_many(kPages));
@@ -62,7 +62,7 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
       attend_few<Q, kPages, kFew, (kMore > 0), kShort><<<l.few.shares * p.kv_heads, kShort * 64, 0, s>>>(p);
     else
       attend_few<Q, kPages, kFew, (kMore > 0), kWaves><<<l.few.shares * p.kv_heads, kWaves * 64, 0, s>>>(p);
-    if (l.few.cuts) attend_join<Q, kFewRows, (kSteps > 4)><<<(l.few.shares - 1) * p.kv_heads, 256, 0, s>>>(p);
+    if (l.few.cuts) attend_join<Q, kFewRows, (kSteps > 4)><<<dim3(1, (l.few.shares - 1) * p.kv_heads), 256, 0, s>>>(p);
   }
   if (l.many.shares) {
     if (l.group.shares) run_many(l.many, attend_many<Q, kPages, kSteps, kMore, false, kBrief>, std::integral_constant<int, kBrief>{});
