@@ -97,9 +97,11 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   const uint64_t others = (a.requests - 1) * most;
   const uint64_t fewest = a.tokens > others ? std::min(a.tokens - others, most) : 1;
   const bool many = most * group >= kFewUpto;
-  // Behind a shared prefix a request's own keys are few, and its rows of either form wait for latency:
-  // where most requests have chunks, the others go with them rather than in a launch of their own.
-  const bool together = groups && many && a.tokens * group >= 2 * kFewUpto * a.requests;
+  // Where most requests have chunks, the others go with them rather than in a launch of their own:
+  // behind a shared prefix, where a request's own keys are few and its rows of either form wait for
+  // latency (100 questions of 2 to 40 tokens over 8000 shared ones take 299 us, in two forms 320), and
+  // over pages with powers, for the two launches less (4 chunks of up to 500 tokens 133 us and 136).
+  const bool together = (groups || l.pages >= kPagesMx8) && many && a.tokens * group >= 2 * kFewUpto * a.requests;
   const bool few = fewest * group < kFewUpto && !together;
   const int steps = steps_of(c.D, l.pages);
   // The least share and the largest tile that is not cut, in blocks.  Few rows: 8 blocks are one
@@ -114,7 +116,10 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   // Workgroups: as many as run at once, a CU each for few rows, which has 128 KB of loads under way
   // then (64 requests of 16384 tokens take 451 us, and 454 with twice as many workgroups); for many
   // rows see attend_many.
-  if (few) l.few = divide(c, a, kFewRows, kFewBlock, groups ? 4 : 8, 16, groups ? 512 : 256, many);
+  if (few) {
+    const bool small = few_small(l.pages, steps);  // three workgroups a CU
+    l.few = divide(c, a, kFewRows, kFewBlock, groups ? 4 : 8, 16, small ? 768 : groups ? 512 : 256, many);
+  }
   auto rows = [&](bool brief) { return (uint32_t)many_waves(steps, brief) * 32; };
   auto all = [&](bool brief) { return steps == 2 ? 768u : steps == 3 || (steps == 4 && brief) ? 512u : 256u; };
   const bool brief = groups && brief_many(l.pages);

@@ -37,6 +37,9 @@ namespace gorio {
 // Waves of a workgroup: 64 requests of 16384 tokens take 235 us at D = 64 and 451 at 128 with
 // eight, 256 and 456 with four.  256 elements take the registers of twice as many.
 __host__ __device__ constexpr int few_waves(int steps, bool brief) { return steps > 4 || brief ? 4 : 8; }
+// Small heads from pages with powers take the registers and the LDS for three workgroups of four waves a
+// CU: 64 requests of 16384 tokens at D = 64 from MX4 pages take 114 us, as one of eight 131.
+__host__ __device__ constexpr bool few_small(int pages, int steps) { return pages >= kPagesMx8 && steps == 2; }
 constexpr int kFewRows = 16;
 constexpr int kFewBlock = 32;  // keys
 
@@ -404,7 +407,7 @@ __device__ __forceinline__ void few_part(const AttendParams &p, const WorkItem &
 }
 
 template <typename Q, int kPages, int kSteps, bool kMore, int kWaves>
-__global__ __launch_bounds__(kWaves * 64, kWaves == 4 && kSteps <= 4 ? 2 : 1) void attend_few(AttendParams p) {
+__global__ __launch_bounds__(kWaves * 64, kWaves == 4 && kSteps <= 4 ? (few_small(kPages, kSteps) ? 3 : 2) : 1) void attend_few(AttendParams p) {
   const uint32_t index = fastdiv(blockIdx.x, p.by_kv), head = blockIdx.x - index * p.kv_heads;
   WorkItem w;
   if (!find_item<kWaves * 64, kFewBlock, false>(p, index, w)) return note_cut<kFewRows>(p, index, head);

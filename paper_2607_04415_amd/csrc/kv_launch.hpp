@@ -58,7 +58,7 @@ hipError_t launch_forms(AttendParams p, const AttendLaunch &l, hipStream_t s) {
     // a key's lanes take equal numbers of eights
     constexpr int kFew = PageOf<kPages>::kMx && kSteps == 3 ? 4 : kSteps;
     constexpr int kWaves = few_waves(kFew, false), kShort = few_waves(kFew, true);
-    if (l.group.shares)
+    if (l.group.shares || few_small(kPages, kFew))
       attend_few<Q, kPages, kFew, (kMore > 0), kShort><<<l.few.shares * p.kv_heads, kShort * 64, 0, s>>>(p);
     else
       attend_few<Q, kPages, kFew, (kMore > 0), kWaves><<<l.few.shares * p.kv_heads, kWaves * 64, 0, s>>>(p);
