@@ -108,8 +108,8 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   // a wave; 8 requests of 250 tokens take 13 us, with shares of 16 blocks 19, of 32 31 us.  Tiles
   // of up to 16 are not cut: 8 requests of 500 tokens take 16 us, cut from 8 on 19; one of 1000
   // takes the same 20 us either way.  Tiles of fewer blocks than the least share are packed into
-  // one, though, and run one after the other: 64 requests of 20 tokens take 41 us, of 60 25, of
-  // 100 17, where 16 of 250 take 12.  Many rows: 128 new tokens over 500 take 33 us, with shares
+  // one, though, and run one after the other: 64 requests of 20 tokens take 38 us, of 60 23, of
+  // 100 15, where 16 of 250 take 12.  Many rows: 128 new tokens over 500 take 33 us, with shares
   // of 8 blocks 54 us, 64 over 250 in 8 requests 23 and 40; of 2 blocks, over 2000, 68 instead of
   // 50 us.  Tiles of up to 8 are not cut: one of 500 keys takes 33 us, cut from 4 on 43; up to 16,
   // 8 requests of 64 over 1000 tokens take 47 instead of 42 us.
@@ -125,6 +125,10 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   const bool brief = groups && brief_many(l.pages);
   if (many) l.many = divide(c, a, rows(brief), kManyBlock, 4, 8, all(brief), false);
   if (few && many) l.few.upto = l.many.from = kFewUpto;
+  // Behind a shared prefix a tile counts for as many blocks as one that is not cut may have, so that
+  // tiles go to workgroups one by one while there are enough (64 requests of up to 500 own keys: 24 us,
+  // with what they have 31).  A group's tiles are cut at 4 blocks: at 1 and 2, 2048 shared positions of
+  // 32 requests take as long, and one key head's 16384 longer (70 and 50 us, 43 at 4).
   if (groups) {
     l.few.pad = l.few.whole;
     l.many.pad = l.many.whole;

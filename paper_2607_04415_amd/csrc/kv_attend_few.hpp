@@ -19,13 +19,25 @@
 // a key, a block before the loads, and handed to the others through LDS.
 // Weights are rounded to q's type for the second product, the sum adds them
 // before that rounding.
+// Elements with powers (MX8, MX4) are widened by the conversions that take a
+// power of two, so it costs nothing there; but the powers are a byte for 32
+// elements, and to have them where they are needed is what costs.  The lane
+// that looks a key up loads its powers, all in two loads, and the lanes get
+// them through LDS a block later.  A lane's elements of a key follow one
+// another: one 16-byte load of 4-bit ones, one power.
+// Loads are written as loads of memory (load_at) and without tests among them:
+// else waits for LDS, or for a table entry, wait for keys and values as well
+// (4-bit pages 300 us in the first form, byte by byte; 195; 155 now).
 //
 // Measured, 64 requests of up to 16384 tokens, 8 key heads: 5.8 TB/s of keys
 // and values at D = 128 (449 us), 5.6 at 64, 5.9 at 256; from 8-bit pages 5.4
-// at 128 and 4.1 at 64, where a row is 64 bytes.
+// at 128 and 4.1 at 64, where a row is 64 bytes; from MX8 pages 5.4 at 128, 5.0
+// at 96, 4.8 at 64, 4.9 at 160, 5.6 at 256; from MX4 pages, 0.53 bytes an
+// element, 4.5 at 128 (155 us, 2.9 times as fast as from 16 bits), 3.1 at 96
+// and 64, 2.7 at 160, 4.2 at 256: 20 vector instructions to a matrix
+// instruction, a wave issues 43% of its time and waits 41%.
 // A copy on the same card moves 4.8 TB/s.  One request: 10 us for 64 tokens,
-// 16 for 1000, 42 for 32000 (59 with two key heads, whose 125 parts the join
-// adds up one after the other), of which the first 10 are the wait for
+// 16 for 1000, 35 for 32000, of which the first 10 are the wait for
 // lengths, table and keys, one after the other, and of the longer ones 3 to 5
 // the joining kernel.
 #pragma once
@@ -35,7 +47,9 @@
 namespace gorio {
 
 // Waves of a workgroup: 64 requests of 16384 tokens take 235 us at D = 64 and 451 at 128 with
-// eight, 256 and 456 with four.  256 elements take the registers of twice as many.
+// eight, 256 and 456 with four.  256 elements take the registers of twice as many.  brief: behind a
+// shared prefix a request's own keys are few, and two workgroups of four waves a CU, a tile each, wait
+// for them together (64 requests of 125 to 500 own keys: 24 us, with one of eight 35).
 __host__ __device__ constexpr int few_waves(int steps, bool brief) { return steps > 4 || brief ? 4 : 8; }
 // Small heads from pages with powers take the registers and the LDS for three workgroups of four waves a
 // CU: 64 requests of 16384 tokens at D = 64 from MX4 pages take 114 us, as one of eight 131.
@@ -424,10 +438,12 @@ __global__ __launch_bounds__(kWaves * 64, kWaves == 4 && kSteps <= 4 ? (few_smal
   }
 }
 
-// Joins the parts of divided tiles, of a group's into what its rows carry: a workgroup a share and head, for the tile that begins in the
-// share and is cut at its end; 16 rows, 16 threads a row (64 rows a workgroup, four after the other:
-// 128 new tokens over 2000 took 54 us in all, now 41).  A row's parts are added in order, and those
-// of eight are loaded together.  kWide: heads of more than 128 elements.
+// Joins the parts of divided tiles, of a group's into what its rows carry: a workgroup a share and
+// head, for the tile that begins in the share and is cut at its end; 16 rows, 16 threads a row (64 rows
+// a workgroup, four after the other: 128 new tokens over 2000 took 54 us in all, now 41).  A row's
+// parts are added in order, and eight are loaded together: 31 parts of 2048 rows take 10 us, one after
+// the other 18, sixteen together 14, a wave a row 13.  A tile's workgroups are neighbours in the
+// launch, so that the few that have work begin together.  kWide: heads of more than 128 elements.
 //   out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over the parts i
 // Bound by the latency of two dependent loads, 4 us, and for many tiles by reading the parts
 // (750 cut tiles of 128 rows, 64 elements: 50 MB in 14 us).

@@ -20,8 +20,20 @@
 // Keys and values of 16 bits go straight from memory into LDS, where a wave's
 // 64 pieces of 16 bytes lie one after the other; which piece a lane asks for is
 // turned by its key (see `turned`), so that neighbouring keys' reads fall on
-// different banks.  Pages of 8 bits are widened in registers on the way, and
-// rows of 96 elements padded by 16 bytes instead.
+// different banks.  Pages of 8 and 4 bits are widened in registers on the way,
+// with powers (a byte that each piece's thread loads beside it) by conversions
+// that multiply; and rows of 96 and 192 elements are padded instead of turned.
+//
+// Shared prefixes (kGroup): a group of requests stands for one, whose rows are
+// those of all its requests' tokens and whose keys are the shared positions.
+// What a row sees goes by its own request's position, prefix and length, which
+// are found once a tile; what it leaves is its sums, which the requests' own
+// launches take in when they write a row.  Rows of single tokens fill tiles
+// that way: 64 tokens over 16384 shared ones take 39 us for the group, 10 for
+// its parts, 24 for up to 500 own keys each, 78 in all; each for itself 351.
+// Of the 39, 20 are the eight blocks of a workgroup; 11 go by before them, a
+// chain of waits (lengths and the share 4, the rows' requests 3, keys 4), and
+// the sums' way to memory takes 5 (33 MB).
 //
 // Weights are rounded to q's type for the second product, the nearest value
 // that the matrix units take; the sum adds them before that rounding.
@@ -29,12 +41,16 @@
 // Measured, 4096 new tokens after 12288, two heads of queries to each of 8:
 // 689 TF at D = 64, 723 at 96, 913 at 128, 485 at 192, 648 at 256 (heads past
 // 128 are computed as 256 elements); from 8-bit pages 671, 747, 900, 359 and
-// 479; with a cap, an exponential and a reciprocal more a score, 752 at 128,
-// with one past 64 550.  A large matrix product reaches 1210.
-// Vector registers are spilled at D <= 64 from 8-bit pages (10 to 13 of them)
-// and under caps (9 to 33), at D <= 128 from 8-bit pages under caps (14, 15)
-// and under caps past 64 (2), at 96 under these (1), and past 128 (5 to 14, from
-// 8-bit pages 54 to 62).
+// 479; from MX8 pages 544, 689, 855, 493 (heads of 129..192 have kernels of
+// their own there) and 283, from MX4 pages 562, 695, 883, 517 and 409;
+// with a cap, an exponential and a reciprocal more a score, 752 at 128,
+// with one past 64 550 (MX4: 696 and 460).  A large matrix product reaches 1210.
+// Vector registers are spilled at D <= 64 from 8-bit pages (13 to 15 of them,
+// with powers 17 to 23) and under caps (10 to 35, with powers 44 to 57), at D <=
+// 128 from 8-bit pages under caps (16, 19), with powers (3 to 6, under caps 20 to
+// 23), and under caps past 64 (3), at 96 under these (1), past 128 (6 to 18,
+// from 8-bit pages 56 to 63, with powers 72 to 95, up to 192 5), in groups up
+// to 16 more, and in the four-wave form at 97..128 up to 18 more.
 // Counters at D = 128: the matrix units work 43% of the time, and a SIMD
 // issues 72% of it, 6.7 vector instructions beside each matrix instruction.
 #pragma once
@@ -49,7 +65,8 @@ namespace gorio {
 // fit a CU, and 33 requests of 1000 tokens take 207 us, with eight waves 232.  Four for larger
 // ones, whose blocks fill LDS.
 // brief: of requests whose keys are mostly their group's, few of their own are left, and two
-// workgroups of four waves wait for them together.
+// workgroups of four waves wait for them together (100 chunks of up to 40 tokens over up to 400 own
+// keys: 58 us, with one of eight 67).
 __host__ __device__ constexpr int many_waves(int steps, bool brief) { return steps == 4 && !brief ? 8 : 4; }
 constexpr int kManyBlock = 64;  // keys
 

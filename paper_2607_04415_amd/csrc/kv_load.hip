@@ -2,6 +2,9 @@
 //
 // The store's copy the other way: a thread moves 8 elements of a key and of its
 // value, neighbouring threads neighbouring parts of a row, widened on the way.
+// Bound by HBM where there are many: 16384 tokens of 8 heads of 128 take 17.7 us
+// from MX8 pages (102 MB, 5.8 TB/s; a large copy moves 4.8) and 14.7 from MX4
+// (85 MB); 2000 tokens 5.8 us, the latency of a slot and then of a row.
 #include "kv.hpp"
 #include "kv_mx.hpp"
 
