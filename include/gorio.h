@@ -373,14 +373,17 @@ void gorio_free_index(gorio_index *ix);
  * What a search finds is read next: a program that answers from the nodes
  * found keeps the attention keys and values of each node's text in pages in
  * HBM, beside the index, and runs its model's new tokens over the pages of the
- * nodes that the search returned.  Four calls do that, once a step (attach,
- * plan) and once a layer (store, attend):
+ * nodes that the search returned.  These calls do that, once a step (attach,
+ * plan, share) and once a layer (store, attend):
  *
  *   gorio_kv_attach  a search's ids -> each request's table of pages
  *   gorio_kv_plan    request lengths -> starts, positions and slots of the new
  *                    tokens, and the tables grown by pages of a free list
  *   gorio_kv_store   the new tokens' keys and values -> their slots
  *   gorio_kv_attend  attention of the new tokens over the pages
+ *   gorio_kv_load    rows of the pages at given slots
+ *   gorio_kv_share, gorio_kv_attend_shared  for batches in which neighbouring
+ *                    requests' tables begin with the same pages
  *
  * A request's tokens have virtual positions 0, 1, ...; position j is place
  * j % page_tokens of the page that entry j / page_tokens of the request's row

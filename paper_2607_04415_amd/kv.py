@@ -8,6 +8,11 @@ values are kept in pages in HBM:
     plan = g.kv_plan(prefix, new_lengths, free_pages, tables, cache.page_tokens, total_new)
     cache.store(k, v, plan.slots)                       # in every layer
     out = cache.attend(q, plan.starts, plan.lens, tables, fills=fills, prefix=prefix)
+    k, v = cache.load(slots)                            # rows of the pages back
+
+Pages hold 16, 8 or 4 bits an element (KVCache).  Where neighbouring requests'
+tables begin with the same pages, g.kv_share finds how far, and attend, told so,
+reads those once for all of them.
 
 Argument marshalling only; the work is done by the library's HIP kernels, on
 torch's current stream of the tensors' device.  Nothing waits for the GPU.
@@ -346,16 +351,19 @@ class KVCache:
         code = self._codes.get(dtype)
         if code is None:
             raise TypeError(f"rows are bfloat16 or float16, not {dtype}")
-        rows = [keys, values]
-        for i, name in enumerate(("keys", "values")):
-            if rows[i] is None:
-                rows[i] = torch.empty((T, self.heads, self.D), dtype=dtype, device=self.device)
-            got, stride = self._rows(name, rows[i], self.heads)
-            if got != code or rows[i].shape[0] != T:
-                raise ValueError(f"{name} must be {T} rows of {dtype}")
+        rows = []
+        for name, x in (("keys", keys), ("values", values)):
+            stride = 0                                                 # packed
+            if x is None:
+                x = torch.empty((T, self.heads, self.D), dtype=dtype, device=self.device)
+            else:
+                got, stride = self._rows(name, x, self.heads)
+                if got != code or x.shape[0] != T:
+                    raise ValueError(f"{name} must be {T} rows of {dtype}")
+                if x.requires_grad and torch.is_grad_enabled():
+                    _no_gradients()
+            rows.append(x)
             at.append(stride)
-        if any(x.requires_grad for x in rows) and torch.is_grad_enabled():
-            _no_gradients()
         if T:
             _done(L.gorio_kv_load(self._ref, code, slots.data_ptr(), T, rows[0].data_ptr(), rows[1].data_ptr(), *at,
                                   _stream(self.device)))
