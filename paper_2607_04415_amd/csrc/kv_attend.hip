@@ -97,12 +97,14 @@ AttendLaunch forms_of(const gorio_kv_cache &c, const gorio_kv_attention &a, uint
   const uint64_t others = (a.requests - 1) * most;
   const uint64_t fewest = a.tokens > others ? std::min(a.tokens - others, most) : 1;
   const bool many = most * group >= kFewUpto;
-  // Where most requests have chunks, the others go with them rather than in a launch of their own:
-  // behind a shared prefix, where a request's own keys are few and its rows of either form wait for
-  // latency (100 questions of 2 to 40 tokens over 8000 shared ones take 299 us, in two forms 320), and
-  // over pages with powers, for the two launches less (4 chunks of up to 500 tokens 133 us and 136).
-  const bool together = (groups || l.pages >= kPagesMx8) && many && a.tokens * group >= 2 * kFewUpto * a.requests;
-  const bool few = fewest * group < kFewUpto && !together;
+  // Requests of few rows never go with the chunks beside them, though that would save two launches:
+  // a tile of chunks takes 2 us a block however few rows it has.  64 single tokens over up to 16384
+  // beside a prompt of 600 take 674 us as chunks and 217 in a form of their own from MX4 pages; behind
+  // 2048 shared positions and with 64 of their own, beside 32 chunks of 40, 151 and 132.  Where most
+  // requests have chunks it is the other way around, but their lengths are on the GPU (100 questions of 2
+  // to 40 tokens over 8000 shared ones take 293 us as chunks and 319 in two forms, 4 chunks of up to
+  // 500 tokens 129 and 136 from MX8 pages).
+  const bool few = fewest * group < kFewUpto;
   const int steps = steps_of(c.D, l.pages);
   // The least share and the largest tile that is not cut, in blocks.  Few rows: 8 blocks are one
   // a wave; 8 requests of 250 tokens take 13 us, with shares of 16 blocks 19, of 32 31 us.  Tiles
