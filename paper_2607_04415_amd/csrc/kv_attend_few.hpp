@@ -57,18 +57,26 @@ __host__ __device__ constexpr bool few_small(int pages, int steps) { return page
 constexpr int kFewRows = 16;
 constexpr int kFewBlock = 32;  // keys
 
+// Memory at any byte: a struct keeps its alignment as a template's argument, a typedef does not.
+template <typename T>
+struct __attribute__((packed)) Anywhere {
+  T value;
+};
+template <typename T>
+__device__ __forceinline__ uint32_t load_anywhere(uint64_t address) {
+  return ((const __attribute__((address_space(1))) Anywhere<T> *)(uintptr_t)address)->value;
+}
+
 // The powers of a row's blocks, of which there are `count`: kBlocks or one less.  Two loads, the
-// second up to the last of them, and of any alignment.
+// second up to the last of them.
 template <int kBlocks, typename Powers>
 __device__ __forceinline__ Powers load_powers(uint64_t from, uint32_t count) {
-  typedef uint32_t Four __attribute__((aligned(1)));
-  typedef uint16_t Two __attribute__((aligned(1)));
   static_assert(kBlocks == 2 || kBlocks == 4 || kBlocks == 6 || kBlocks == 8, "pairs of blocks");
   const uint32_t less = kBlocks - count;
   if constexpr (kBlocks == 2) return load_at<uint8_t>(from) | (uint32_t)load_at<uint8_t>(from + count - 1) << (count - 1) * 8;
-  else if constexpr (kBlocks == 4) return load_at<Two>(from) | (uint32_t)load_at<Two>(from + count - 2) << (count - 2) * 8;
-  else if constexpr (kBlocks == 6) return Powers{load_at<Four>(from), (uint32_t)load_at<Two>(from + count - 2) >> less * 8};
-  else return Powers{load_at<Four>(from), load_at<Four>(from + count - 4) >> less * 8};
+  else if constexpr (kBlocks == 4) return load_anywhere<uint16_t>(from) | load_anywhere<uint16_t>(from + count - 2) << (count - 2) * 8;
+  else if constexpr (kBlocks == 6) return Powers{load_anywhere<uint32_t>(from), load_anywhere<uint16_t>(from + count - 2) >> less * 8};
+  else return Powers{load_anywhere<uint32_t>(from), load_anywhere<uint32_t>(from + count - 4) >> less * 8};
 }
 
 // kSteps: 32-element steps of a head, D <= 32 kSteps (2, 4, 6 or 8 with powers).  kPages: a PageKind.
