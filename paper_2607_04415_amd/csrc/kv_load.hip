@@ -83,6 +83,22 @@ __global__ __launch_bounds__(256) void load_kernel(LoadParams p) {
   }
 }
 
+// Whether a row of keys and one of values share a byte; rows of one array do not.  All in bytes.
+bool rows_meet(uintptr_t keys, uint64_t key_step, uintptr_t values, uint64_t value_step, uint64_t row, uint64_t tokens) {
+  if (keys >= values + (tokens - 1) * value_step + row || values >= keys + (tokens - 1) * key_step + row) return false;
+  if (key_step == value_step) {  // parts of one wider row: how far behind a key's row the next value's begins
+    const uint64_t behind = values >= keys ? (values - keys) % key_step : key_step - 1 - (keys - values - 1) % key_step;
+    return behind < row || key_step - behind < row;
+  }
+  for (uint64_t i = 0, j = 0; i < tokens && j < tokens;) {
+    const uintptr_t k = keys + i * key_step, v = values + j * value_step;
+    if (k < v + row && v < k + row) return true;
+    if (k < v) ++i;
+    else ++j;
+  }
+  return false;
+}
+
 }  // namespace
 
 extern "C" gorio_status gorio_kv_load(const gorio_kv_cache *cache, gorio_kv_dtype dtype, const int64_t *slots,
@@ -138,11 +154,11 @@ extern "C" gorio_status gorio_kv_load(const gorio_kv_cache *cache, gorio_kv_dtyp
   p.parts = tokens * p.per_token.d;
   const uint64_t grid = (p.parts + kParts - 1) / kParts;  // a launch has less than 2^32 threads
   if (grid >= 1ull << 24) return fail(GORIO_EINVAL, "tokens=%llu too large", (unsigned long long)tokens);
-  // rows that are written overlap neither one another, where one is inside the other's stride they
-  // may alternate, nor the slots
-  const uint64_t upto = ((tokens - 1) * key_stride + row) * 2, upto_values = ((tokens - 1) * value_stride + row) * 2;
-  st = kv_apart({{"keys", keys, key_stride == row ? upto : 0, true},
-                 {"values", values, value_stride == row ? upto_values : 0, true},
+  // rows that are written overlap neither one another, though keys and values may alternate, nor the slots
+  if (rows_meet((uintptr_t)keys, key_stride * 2, (uintptr_t)values, value_stride * 2, row * 2, tokens))
+    return fail(GORIO_EINVAL, "keys and values overlap");
+  st = kv_apart({{"keys", keys, key_stride == row ? tokens * row * 2 : 0, true},
+                 {"values", values, value_stride == row ? tokens * row * 2 : 0, true},
                  {"slots", slots, tokens * 8, false}});
   if (st != GORIO_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
