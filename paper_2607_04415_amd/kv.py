@@ -340,12 +340,13 @@ class KVCache:
 
     def load(self, slots, dtype=None, keys=None, values=None):
         """(keys, values): the rows of the pages at `slots` (int64), tokens x heads x
-        D each, of the pages' type, or bfloat16 or float16 as `dtype` says where
-        they hold 8 or 4 bits; zeros where a slot is below 0 or past the pages.
+        D each, of the pages' type, or bfloat16 or float16 as `dtype` (or else the
+        rows given) says where they hold 8 or 4 bits; zeros where a slot is below 0 or past the pages.
         keys, values: rows to write to (they may be parts of wider ones)."""
         torch, L = _bind()
         if dtype is None:
-            dtype = keys.dtype if keys is not None else self.keys.dtype if self._code <= F16 else torch.bfloat16
+            given = keys if keys is not None else values
+            dtype = given.dtype if given is not None else self.keys.dtype if self._code <= F16 else torch.bfloat16
         _need("slots", slots, torch.int64, (slots.numel(),), self.device)
         T, at = slots.numel(), []
         code = self._codes.get(dtype)
