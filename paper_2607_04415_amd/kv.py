@@ -205,7 +205,7 @@ class KVSharing(NamedTuple):
     groups' first requests, and shared (requests), the positions that a request
     shares with its group; common (requests), those it shares with the request
     before it.  A program that knows its groups makes first (groups + 1) and
-    shared by itself."""
+    shared by itself; a group's rows of the tables name the same pages so far."""
     first: object
     shared: object
     common: object = None
