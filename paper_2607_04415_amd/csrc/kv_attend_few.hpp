@@ -34,8 +34,10 @@
 // at 128 and 4.1 at 64, where a row is 64 bytes; from MX8 pages 5.4 at 128, 5.0
 // at 96, 4.8 at 64, 4.9 at 160, 5.6 at 256; from MX4 pages, 0.53 bytes an
 // element, 4.5 at 128 (155 us, 2.9 times as fast as from 16 bits), 3.1 at 96
-// and 64, 2.7 at 160, 4.2 at 256: 20 vector instructions to a matrix
-// instruction, a wave issues 43% of its time and waits 41%.
+// and 64, 2.7 at 160, 4.2 at 256: latency, 0.12 to 0.13 TB/s for each KB that a
+// CU has under way (a block a wave: 35, 26, 22 and 35 KB; from MX8 pages 42 to 68,
+// which HBM bounds).  Beside it 20 vector instructions to a matrix instruction:
+// a wave issues 43% of its time and waits 41%.
 // A copy on the same card moves 4.8 TB/s.  One request: 10 us for 64 tokens,
 // 16 for 1000, 35 for 32000, of which the first 10 are the wait for
 // lengths, table and keys, one after the other, and of the longer ones 3 to 5

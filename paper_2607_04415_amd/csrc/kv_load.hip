@@ -2,9 +2,11 @@
 //
 // The store's copy the other way: a thread moves 8 elements of a key and of its
 // value, neighbouring threads neighbouring parts of a row, widened on the way.
-// Bound by HBM where there are many: 16384 tokens of 8 heads of 128 take 17.7 us
-// from MX8 pages (102 MB, 5.8 TB/s; a large copy moves 4.8) and 14.7 from MX4
-// (85 MB); 2000 tokens 5.8 us, the latency of a slot and then of a row.
+// Bound by HBM where there are many: 16384 rows of 8 heads of 128 that no cache
+// holds take 21.4 us from MX8 pages (102 MB, 4.75 TB/s; a large copy moves 4.85),
+// 19.7 from MX4 (85 MB, 4.3), 25.2 from 16-bit pages (134 MB, 5.3) and 20.5 from
+// e4m3 (101 MB, 4.9), 131072 rows 162, 143, 211 and 159 us (4.8 to 5.1 TB/s); 2000
+// rows 5.8 us, the latency of a slot and then of a row.
 #include "kv.hpp"
 #include "kv_mx.hpp"
 
