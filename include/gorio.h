@@ -600,9 +600,10 @@ typedef struct {
  * looked up in the row of the group's first request or in the request's own.
  * The result is that of gorio_kv_attend beyond rounding, whatever else the call
  * asks for: what a row sees of the shared positions goes by its own position,
- * prefix, window and length.  Groups take launches of their own, 10 to 40 us,
- * also where nothing is shared.  A call with a window and without a prefix, or
- * whose tables have little room, is computed as by gorio_kv_attend.
+ * prefix, window and length.  Groups take launches of their own: up to 12 us
+ * where nothing is shared, 20 to 40 where little is.  A call with a window and
+ * without a prefix, or whose tables have little room, is computed as by
+ * gorio_kv_attend.
  *   workspace: gorio_kv_workspace_shared bytes, about tokens * heads * (D + 2)
  *              floats more than without (545 MB for 32768 tokens of 32 heads of
  *              128): the sums over the shared positions.

@@ -75,7 +75,7 @@ uint64_t carry_bytes(const gorio_kv_cache &c, const gorio_kv_attention &a) {
 // 8 key heads, 8192 shared positions (134M), take 36 us each for itself and 43 by groups, 16384
 // (268M) 54 and 49; 32 requests of 4-bit pages over 2048 (151M) 30 and 41, over 8192 (550M) 65 and
 // 47; 128 requests of 8 new tokens and one key head over 8192 (275M) 122 and 91.  How much is shared is
-// on the GPU: where nothing is, a call with room takes 5 to 12 us more than it would each for itself,
+// on the GPU: where nothing is, a call with room takes up to 12 us more than each for itself,
 // where 256 of 16000 positions are, 25 to 36.
 constexpr uint64_t kWorthSharing = 200'000'000;
 uint32_t groups_of(const gorio_kv_cache &c, const gorio_kv_attention &a, const gorio_kv_sharing *sharing) {
